@@ -259,6 +259,105 @@ cola_status_t cola_bwd_down_gated(const cola_desc_t* desc, const void* M, const 
 cola_status_t cola_recompute_up(const cola_desc_t* desc, int32_t count, const void* Z_cat, const void* const* B,
                                 void* const* Y, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- the vocabulary end of the model ----
+ * What a model of CoLA layers learns from and answers with: its rows of
+ * vocabulary logits x [n x vocab] (one row per token; the product with the
+ * output embedding, which the paper leaves full-rank, is the caller's).  The
+ * paper trains by cross entropy (Sec. 5.1) and has no counterpart to the
+ * distillation, whose teacher would be the full-rank model that a CoLA model
+ * stands in for.
+ *
+ * With temperature T and z = x / T:  logp_j = z_j - log sum exp(z), p = exp(logp),
+ * H = - sum p logp.  Sums, maxima and statistics are held in fp32; gradients are
+ * rounded once, to the logits' type.  Results are deterministic.
+ *
+ * Conventions, next to the ones at the top of this file:
+ *   - logits and dlogits: device pointers aligned to their element, rows of
+ *     any pitch >= vocab (rows on 16-byte boundaries, and dlogits with the
+ *     logits' offset from them, run fastest); token ids int64; other values
+ *     fp32; stats 16-byte aligned.  No workspace.
+ *   - dlogits may be the logits themselves (same pointer and pitch).
+ *   - Token ids outside [0, vocab) are legal and name no token: such a target
+ *     is ignored (logp 0, no gradient), such a list entry absent.
+ *   - -inf logits are tokens of probability 0.  A row of nothing but -inf has
+ *     logp -inf, H 0 and gradient 0.  A NaN or +inf in a row makes that row's
+ *     results NaN.  A row whose upstream gradients are 0 has gradient 0,
+ *     whatever it holds.
+ *   - Limits: vocab <= 2^20, k <= 256 and <= vocab, 1e-4 <= temperatures <= 1e4,
+ *     n < 2^28. */
+typedef enum {
+    COLA_DTYPE_BF16 = 0,
+    COLA_DTYPE_F32 = 1
+} cola_dtype_t;
+
+typedef struct {
+    int64_t n;                  /* rows (tokens) */
+    int64_t vocab;              /* logits of a row */
+    int64_t ld;                 /* row pitch of the logits in elements (0: vocab) */
+    int64_t ld_grad;            /* row pitch of dlogits (0: vocab) */
+    float temperature;          /* T */
+    float teacher_temperature;  /* distillation: what t_vals are divided by */
+    int32_t dtype;              /* cola_dtype_t of logits and dlogits */
+    int32_t k;                  /* alternatives per row (0: none); entries of a teacher's list */
+    int32_t rest;               /* distillation: 1 counts the tokens outside the list as one more entry */
+    int32_t reserved;           /* must be 0 */
+} cola_vocab_desc_t;
+
+/* Log probabilities of given tokens, with entropy and top alternatives.
+ *   targets [n], logp [n]: log probability of the given token of each row
+ *     (both or neither NULL).
+ *   entropy [n]: H of each row (NULL: not wanted).
+ *   top_ids, top_logp [n x k]: the k most likely tokens, most likely first,
+ *     ties to the lower id (a NaN counts as the largest), and their log
+ *     probabilities; NULL exactly when desc->k is 0.
+ *   stats [n x 4]: {max x, log sum exp((x - max x) / T), H, 0} for the backward
+ *     (NULL: not wanted). */
+cola_status_t cola_token_logprob_fwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                     float* logp, float* entropy, int64_t* top_ids, float* top_logp, float* stats,
+                                     void* stream);
+
+/* Its backward, from the upstream gradients g = dlogp [n] and h = dentropy [n]
+ * (one of them may be NULL: 0) and the forward's stats:
+ *   dlogits_j = (1 / T) (g ([j = target] - p_j) - h p_j (logp_j + H)).
+ * Cross entropy averaged over N tokens is g = -1 / N.  targets may be NULL when
+ * dlogp is. */
+cola_status_t cola_token_logprob_bwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                     const float* stats, const float* dlogp, const float* dentropy, void* dlogits,
+                                     void* stream);
+
+/* Both in one call, for upstream gradients that do not depend on the results
+ * (cross entropy): logp and entropy (each NULL: not wanted) and dlogits. */
+cola_status_t cola_token_logprob_step(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                      const float* dlogp, const float* dentropy, float* logp, float* entropy,
+                                      void* dlogits, void* stream);
+
+/* Distillation from a teacher's top logits.  Each row has a list of k entries:
+ * t_ids [n x k], distinct tokens, and t_vals [n x k]; u = t_vals / teacher_temperature.
+ *   rest = 0: the teacher is q = softmax(u) over the list (t_vals may be logits
+ *     or log probabilities; t_lse is not read).
+ *   rest = 1: q = exp(u - t_lse) with t_lse [n] the teacher's log sum exp over
+ *     its whole vocabulary at that temperature (NULL: 0, the u being log
+ *     probabilities, as top_logp above), and the rest of the vocabulary is one
+ *     more entry, q_R = max(0, 1 - sum q) against p_R = sum of p outside the
+ *     list; it is left out where the student masks all of it or there is none.
+ *   loss [n] = T^2 (sum q (log q - log p) + q_R (log q_R - log p_R)); a list
+ *     without any entry has loss 0 and gradient 0.
+ *   stats [n x 4]: {max, log sum} of the row and of its tokens outside the list,
+ *     for the backward (NULL: not wanted). */
+cola_status_t cola_topk_distill_fwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                    const float* t_vals, const float* t_lse, float* loss, float* stats, void* stream);
+
+/* Its backward, from w = dloss [n] and the forward's stats, with Q = sum q + q_R:
+ *   dlogits_k = w T (Q p_k - q_k) on the list,  w T p_j (Q - q_R / p_R) outside it. */
+cola_status_t cola_topk_distill_bwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                    const float* t_vals, const float* t_lse, const float* stats, const float* dloss,
+                                    void* dlogits, void* stream);
+
+/* Both in one call, for weights dloss that do not depend on the loss. */
+cola_status_t cola_topk_distill_step(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                     const float* t_vals, const float* t_lse, const float* dloss, float* loss,
+                                     void* dlogits, void* stream);
+
 /* Synchronise `stream`, read and clear the workspace status word.
  * Returns COLA_OK, or COLA_ERR_DEVICE_TIMEOUT if a kernel that used this
  * workspace gave up on a wait since the last check (*code_out, if not NULL,
@@ -393,8 +492,10 @@ typedef enum {
                                     (n, r, d_in) and (n, d_out, r) */
     COLA_KERNEL_BWD_FUSED = 9,   /* dZ = (dY B) * sigma'(Z), dX = dZ A in one kernel, count 2:
                                     (n, r, d_out) and (n, d_in, r) */
-    COLA_KERNEL_REPACK = 10      /* A copied to an aligned pitch in the workspace, ahead of a large
+    COLA_KERNEL_REPACK = 10,     /* A copied to an aligned pitch in the workspace, ahead of a large
                                     GEMM that reads it            (M=rows, N=d_in, K=0) */
+    COLA_KERNEL_TOKEN_LOGPROB = 11, /* cola_token_logprob_*                 (M=n, N=vocab, K=k) */
+    COLA_KERNEL_TOPK_DISTILL = 12   /* cola_topk_distill_*                  (M=n, N=vocab, K=k) */
 } cola_kernel_t;
 
 typedef struct {

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libcola.so")
 
 SIGMA = {"identity": 0, "silu": 1, "gelu": 2}
 MODE = {"cola": 0, "cola_m": 1, "infer": 2}
+DTYPE = {"bf16": 0, "f32": 1, torch.bfloat16: 0, torch.float32: 1}
 STATUS = {0: "COLA_OK", 1: "COLA_ERR_INVALID", 2: "COLA_ERR_ALIGN", 3: "COLA_ERR_UNSUPPORTED",
           4: "COLA_ERR_WORKSPACE", 5: "COLA_ERR_LAUNCH", 6: "COLA_ERR_DEVICE_TIMEOUT"}
 
@@ -28,10 +29,12 @@ SYMBOLS = ("cola_workspace_size", "cola_workspace_init", "cola_fwd", "cola_bwd",
            "cola_selftest_wait_timeout_cluster", "cola_selftest_wait_timeout_thin",
            "cola_trace_attach", "cola_trace_detach", "cola_set_fused_forward", "cola_set_fused_backward",
            "cola_set_cluster_splitk",
+           "cola_token_logprob_fwd", "cola_token_logprob_bwd", "cola_token_logprob_step",
+           "cola_topk_distill_fwd", "cola_topk_distill_bwd", "cola_topk_distill_step",
            "cola_status_string")
 STATIC_SCRATCH_BYTES = 64 * 1024 * 1024
 KERNELS = {0: "fwd_zh", 1: "fwd_y", 2: "bwd_dz", 3: "wgrad", 4: "reduce", 5: "bwd_dx", 6: "sigma", 7: "fwd_glu", 8: "fwd_fused",
-           9: "bwd_fused", 10: "repack"}
+           9: "bwd_fused", 10: "repack", 11: "token_logprob", 12: "topk_distill"}
 
 
 class ColaError(RuntimeError):
@@ -45,6 +48,12 @@ class cola_desc_t(ctypes.Structure):
                 ("r", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
                 ("ld_a", ctypes.c_int64), ("sigma", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("wgrad_fp32", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class cola_vocab_desc_t(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
+                ("temperature", ctypes.c_float), ("teacher_temperature", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("k", ctypes.c_int32), ("rest", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class cola_trace_slot_t(ctypes.Structure):
@@ -114,6 +123,12 @@ def lib():
         l.cola_set_fused_backward.restype = st
         l.cola_set_cluster_splitk.argtypes = [ctypes.c_int32]
         l.cola_set_cluster_splitk.restype = st
+        V = ctypes.POINTER(cola_vocab_desc_t)
+        for name, count in (("cola_token_logprob_fwd", 7), ("cola_token_logprob_bwd", 6), ("cola_token_logprob_step", 7),
+                            ("cola_topk_distill_fwd", 6), ("cola_topk_distill_bwd", 7), ("cola_topk_distill_step", 7)):
+            f = getattr(l, name)
+            f.argtypes = [V] + [_vp] * (count + 1)
+            f.restype = st
         l.cola_status_string.argtypes = [ctypes.c_int]
         l.cola_status_string.restype = ctypes.c_char_p
         _lib = l
@@ -224,6 +239,55 @@ def cola_bwd_down_gated(d, M, A, B, dY, Z_save, H_save, Y_gate, Y_up, dY_gate, d
 def cola_recompute_up(d, Z_cat, Bs, Ys, ws, stream=None):
     _check(lib().cola_recompute_up(ctypes.byref(d), len(Bs), _ptr(Z_cat), _ptr_array(Bs), _ptr_array(Ys), _ptr(ws),
                                    _nbytes(ws), _stream(stream)), "cola_recompute_up")
+
+
+def vocab_desc(n, vocab, ld=0, ld_grad=0, dtype="bf16", temperature=1.0, k=0, rest=False, teacher_temperature=1.0):
+    """Rows of vocabulary logits: n rows of `vocab` logits at pitch ld, gradients
+    at pitch ld_grad (0: vocab), both of `dtype` ("bf16", "f32" or the torch type)."""
+    d = cola_vocab_desc_t()
+    d.n, d.vocab, d.ld, d.ld_grad = int(n), int(vocab), int(ld), int(ld_grad)
+    d.temperature, d.teacher_temperature = float(temperature), float(teacher_temperature)
+    d.dtype = DTYPE.get(dtype, -1) if not isinstance(dtype, int) else dtype
+    d.k, d.rest, d.reserved = int(k), int(bool(rest)), 0
+    return d
+
+
+def cola_token_logprob_fwd(d, logits, targets, logp, entropy, top_ids, top_logp, stats, stream=None):
+    """Log probability of one given token per row, the row's entropy, its d.k
+    most likely tokens, and the statistics the backward reads."""
+    _check(lib().cola_token_logprob_fwd(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(logp), _ptr(entropy),
+                                        _ptr(top_ids), _ptr(top_logp), _ptr(stats), _stream(stream)),
+           "cola_token_logprob_fwd")
+
+
+def cola_token_logprob_bwd(d, logits, targets, stats, dlogp, dentropy, dlogits, stream=None):
+    _check(lib().cola_token_logprob_bwd(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(stats), _ptr(dlogp),
+                                        _ptr(dentropy), _ptr(dlogits), _stream(stream)), "cola_token_logprob_bwd")
+
+
+def cola_token_logprob_step(d, logits, targets, dlogp, dentropy, logp, entropy, dlogits, stream=None):
+    """Forward and backward in one call, the upstream gradients being known."""
+    _check(lib().cola_token_logprob_step(ctypes.byref(d), _ptr(logits), _ptr(targets), _ptr(dlogp), _ptr(dentropy),
+                                         _ptr(logp), _ptr(entropy), _ptr(dlogits), _stream(stream)),
+           "cola_token_logprob_step")
+
+
+def cola_topk_distill_fwd(d, logits, t_ids, t_vals, t_lse, loss, stats, stream=None):
+    """T^2 KL(teacher || student) per row, the teacher given by its d.k most
+    likely tokens."""
+    _check(lib().cola_topk_distill_fwd(ctypes.byref(d), _ptr(logits), _ptr(t_ids), _ptr(t_vals), _ptr(t_lse), _ptr(loss),
+                                       _ptr(stats), _stream(stream)), "cola_topk_distill_fwd")
+
+
+def cola_topk_distill_bwd(d, logits, t_ids, t_vals, t_lse, stats, dloss, dlogits, stream=None):
+    _check(lib().cola_topk_distill_bwd(ctypes.byref(d), _ptr(logits), _ptr(t_ids), _ptr(t_vals), _ptr(t_lse),
+                                       _ptr(stats), _ptr(dloss), _ptr(dlogits), _stream(stream)), "cola_topk_distill_bwd")
+
+
+def cola_topk_distill_step(d, logits, t_ids, t_vals, t_lse, dloss, loss, dlogits, stream=None):
+    """Forward and backward in one call, the weights dloss being known."""
+    _check(lib().cola_topk_distill_step(ctypes.byref(d), _ptr(logits), _ptr(t_ids), _ptr(t_vals), _ptr(t_lse),
+                                        _ptr(dloss), _ptr(loss), _ptr(dlogits), _stream(stream)), "cola_topk_distill_step")
 
 
 def cola_selftest_wait_timeout(ws, stream=None):

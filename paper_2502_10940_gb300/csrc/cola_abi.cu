@@ -15,6 +15,7 @@
 #include "fused_layer.cuh"
 #include "gemm_launch.cuh"
 #include "host_plan.cuh"
+#include "vocab.cuh"
 
 namespace cola {
 namespace {
@@ -1584,6 +1585,169 @@ cola_status_t cola_selftest_wait_timeout_thin(void* ws, size_t ws_bytes, void* s
     const int64_t mnk[1][3] = {{n, M, K}};
     return launched(traced(COLA_KERNEL_FWD_Y, 1, mnk, b.S, TRACE_CLUSTER, static_cast<cudaStream_t>(stream),
                            [&] { return launch_thin(b, THIN_STORE, SIG_IDENTITY, static_cast<cudaStream_t>(stream)); }));
+}
+
+// ------------------------------------------------------- vocabulary operators
+}  // extern "C"
+
+namespace cola {
+namespace {
+
+bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// The checks every vocabulary call shares, and what its kernels take from the
+// descriptor.  `grad`: the call writes dlogits.
+cola_status_t vocab_params(const cola_vocab_desc_t* d, const void* logits, void* dlogits, bool grad, VocabParams* p)
+{
+    if (!d || !logits || (grad && !dlogits)) return COLA_ERR_INVALID;
+    if (d->n < 1 || d->vocab < 1 || d->ld < 0 || d->ld_grad < 0 || d->k < 0 || d->reserved != 0) return COLA_ERR_INVALID;
+    if (d->dtype != COLA_DTYPE_BF16 && d->dtype != COLA_DTYPE_F32) return COLA_ERR_INVALID;
+    if (d->rest != 0 && d->rest != 1) return COLA_ERR_INVALID;
+    for (float t : {d->temperature, d->teacher_temperature})
+        if (!(t >= 1e-4f && t <= 1e4f)) return COLA_ERR_INVALID;
+    *p = VocabParams{};
+    p->ld = d->ld ? d->ld : d->vocab;
+    p->ld_d = d->ld_grad ? d->ld_grad : d->vocab;
+    if (p->ld < d->vocab || p->ld_d < d->vocab || d->k > d->vocab) return COLA_ERR_INVALID;
+    const int64_t lim = (int64_t(1) << 31) - 256;
+    if (d->vocab > VOCAB_MAX || d->k > VOCAB_MAX_K || d->n > lim / 8 || p->ld > lim || p->ld_d > lim)
+        return COLA_ERR_UNSUPPORTED;
+    const size_t e = d->dtype == COLA_DTYPE_BF16 ? 2 : 4;
+    if (!aligned_to(logits, e) || (grad && !aligned_to(dlogits, e))) return COLA_ERR_ALIGN;
+    p->logits = logits;
+    p->dlogits = dlogits;
+    p->n = d->n;
+    p->vocab = static_cast<int>(d->vocab);
+    p->k = d->k;
+    p->rest = d->rest;
+    p->temperature = d->temperature;
+    p->c = static_cast<float>(1.0 / d->temperature);
+    p->c2 = static_cast<float>(1.4426950408889634 / d->temperature);
+    p->t_c = static_cast<float>(1.0 / d->teacher_temperature);
+    return COLA_OK;
+}
+
+// Token ids are 8-byte, statistics 16-byte and other per-row values 4-byte aligned.
+cola_status_t vocab_align(std::initializer_list<const void*> ids, const void* stats, std::initializer_list<const void*> floats)
+{
+    bool ok = aligned_to(stats, 16);
+    for (const void* q : ids) ok = ok && aligned_to(q, 8);
+    for (const void* q : floats) ok = ok && aligned_to(q, 4);
+    return ok ? COLA_OK : COLA_ERR_ALIGN;
+}
+
+cola_status_t run_vocab(const cola_vocab_desc_t* d, const VocabParams& p, bool distill, int pass, void* stream)
+{
+    int sms = 0;
+    COLA_TRY(device_info(&sms));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t mnk[1][3] = {{p.n, p.vocab, p.k}};
+    const int kind = distill ? COLA_KERNEL_TOPK_DISTILL : COLA_KERNEL_TOKEN_LOGPROB;
+    return launched(traced(kind, 1, mnk, 1, 0, st, [&] {
+        return distill ? launch_topk_distill(p, d->dtype, pass, st) : launch_token_logprob(p, d->dtype, pass, st);
+    }));
+}
+
+}  // namespace
+}  // namespace cola
+
+extern "C" {
+
+cola_status_t cola_token_logprob_fwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                     float* logp, float* entropy, int64_t* top_ids, float* top_logp, float* stats,
+                                     void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, nullptr, false, &p));
+    if ((targets != nullptr) != (logp != nullptr) || (top_ids != nullptr) != (top_logp != nullptr) ||
+        (top_ids != nullptr) != (desc->k > 0) || (!logp && !entropy && !top_ids && !stats))
+        return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({targets, top_ids}, stats, {logp, entropy, top_logp}));
+    p.targets = reinterpret_cast<const long long*>(targets);
+    p.logp = logp;
+    p.entropy = entropy;
+    p.top_ids = reinterpret_cast<long long*>(top_ids);
+    p.top_logp = top_logp;
+    p.stats = stats;
+    return run_vocab(desc, p, false, VOCAB_FWD, stream);
+}
+
+cola_status_t cola_token_logprob_bwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                     const float* stats, const float* dlogp, const float* dentropy, void* dlogits,
+                                     void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, dlogits, true, &p));
+    if (!stats || (!dlogp && !dentropy) || (dlogp && !targets)) return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({targets}, stats, {dlogp, dentropy}));
+    p.targets = reinterpret_cast<const long long*>(targets);
+    p.stats = const_cast<float*>(stats);
+    p.dlogp = dlogp;
+    p.dentropy = dentropy;
+    return run_vocab(desc, p, false, VOCAB_BWD, stream);
+}
+
+cola_status_t cola_token_logprob_step(const cola_vocab_desc_t* desc, const void* logits, const int64_t* targets,
+                                      const float* dlogp, const float* dentropy, float* logp, float* entropy,
+                                      void* dlogits, void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, dlogits, true, &p));
+    if ((!dlogp && !dentropy) || ((dlogp || logp) && !targets)) return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({targets}, nullptr, {dlogp, dentropy, logp, entropy}));
+    p.targets = reinterpret_cast<const long long*>(targets);
+    p.dlogp = dlogp;
+    p.dentropy = dentropy;
+    p.logp = logp;
+    p.entropy = entropy;
+    return run_vocab(desc, p, false, VOCAB_STEP, stream);
+}
+
+cola_status_t cola_topk_distill_fwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                    const float* t_vals, const float* t_lse, float* loss, float* stats, void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, nullptr, false, &p));
+    if (desc->k < 1 || !t_ids || !t_vals || !loss) return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({t_ids}, stats, {t_vals, t_lse, loss}));
+    p.t_ids = reinterpret_cast<const long long*>(t_ids);
+    p.t_vals = t_vals;
+    p.t_lse = t_lse;
+    p.loss = loss;
+    p.stats = stats;
+    return run_vocab(desc, p, true, VOCAB_FWD, stream);
+}
+
+cola_status_t cola_topk_distill_bwd(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                    const float* t_vals, const float* t_lse, const float* stats, const float* dloss,
+                                    void* dlogits, void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, dlogits, true, &p));
+    if (desc->k < 1 || !t_ids || !t_vals || !stats || !dloss) return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({t_ids}, stats, {t_vals, t_lse, dloss}));
+    p.t_ids = reinterpret_cast<const long long*>(t_ids);
+    p.t_vals = t_vals;
+    p.t_lse = t_lse;
+    p.stats = const_cast<float*>(stats);
+    p.dloss = dloss;
+    return run_vocab(desc, p, true, VOCAB_BWD, stream);
+}
+
+cola_status_t cola_topk_distill_step(const cola_vocab_desc_t* desc, const void* logits, const int64_t* t_ids,
+                                     const float* t_vals, const float* t_lse, const float* dloss, float* loss,
+                                     void* dlogits, void* stream)
+{
+    VocabParams p;
+    COLA_TRY(vocab_params(desc, logits, dlogits, true, &p));
+    if (desc->k < 1 || !t_ids || !t_vals || !dloss || !loss) return COLA_ERR_INVALID;
+    COLA_TRY(vocab_align({t_ids}, nullptr, {t_vals, t_lse, dloss, loss}));
+    p.t_ids = reinterpret_cast<const long long*>(t_ids);
+    p.t_vals = t_vals;
+    p.t_lse = t_lse;
+    p.dloss = dloss;
+    p.loss = loss;
+    return run_vocab(desc, p, true, VOCAB_STEP, stream);
 }
 
 cola_status_t cola_check_status(void* ws, void* stream, uint32_t* code_out)
