@@ -1644,7 +1644,7 @@ cola_status_t run_vocab(const cola_vocab_desc_t* d, const VocabParams& p, bool d
     const int64_t mnk[1][3] = {{p.n, p.vocab, p.k}};
     const int kind = distill ? COLA_KERNEL_TOPK_DISTILL : COLA_KERNEL_TOKEN_LOGPROB;
     return launched(traced(kind, 1, mnk, 1, 0, st, [&] {
-        return distill ? launch_topk_distill(p, d->dtype, pass, st) : launch_token_logprob(p, d->dtype, pass, st);
+        return distill ? launch_topk_distill(p, d->dtype, pass, sms, st) : launch_token_logprob(p, d->dtype, pass, sms, st);
     }));
 }
 
