@@ -3,77 +3,123 @@
 #include "vocab.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace cola {
 namespace {
 
-template <class K>
-cudaError_t launch_rows(K kern, const VocabParams& p, int threads, int rows, bool cluster, cudaStream_t stream)
+// How a row is shared: `threads` of a CTA (32: a warp, four rows a CTA) and `parts` CTAs.
+struct Plan {
+    int threads, parts;
+};
+
+// A warp or four warps where their registers hold the row (NV vectors a
+// thread), else sixteen.  A step writes the row that it has read: it takes as
+// many CTAs as hold it in registers, up to a portable cluster's eight; the other
+// passes read tile after tile.  All take more CTAs where there are fewer rows
+// than CTAs that the device runs at once (two per SM), down to a vector per thread.
+Plan plan(const VocabParams& p, int e, int pass, int least, int sms)
 {
+    const int nvec = (p.vocab + e - 1) / e;
+    if (least <= 32 && nvec <= 32 * NV) return {32, 1};
+    if (least <= 128 && nvec <= 128 * NV) return {128, 1};
+    const int hold = pass == VOCAB_STEP ? (nvec + 512 * NV - 1) / (512 * NV) : 1;
+    const int fill = static_cast<int>(std::min<long long>(2ll * sms / p.n, nvec / 512));
+    return {512, std::min(CLUSTER_MAX, std::max({1, hold, fill}))};
+}
+
+template <class K>
+cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, cudaStream_t stream)
+{
+    const int rows = s.threads == 32 ? 4 : 1;
+    p.each = (p.vocab / e + s.parts - 1) / s.parts;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned int>((p.n + rows - 1) / rows * p.parts));
-    cfg.blockDim = dim3(threads);
+    cfg.gridDim = dim3(static_cast<unsigned int>((p.n + rows - 1) / rows), s.parts);
+    cfg.blockDim = dim3(s.threads * rows);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
-    if (cluster && p.parts > 1) {
+    if (cluster && s.parts > 1) {
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = p.parts;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[0].val.clusterDim.y = s.parts;
+        attr[0].val.clusterDim.x = attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
     }
     return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-// Threads per row: a warp where its registers hold the row (NV vectors a
-// thread), four warps likewise, else sixteen, by themselves or as one of
-// `parts` CTAs: as many as hold the row in registers, up to a portable
-// cluster's eight; more where there are fewer rows than CTAs the device runs at
-// once (two per SM), down to a vector per thread.
-int plan(VocabParams* p, int e, int least, int sms)
+template <class T, bool ENT>
+cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
-    const int nvec = (p->vocab + 2 * e - 2) / e;
-    p->parts = 1;
-    if (least <= 32 && nvec <= 32 * NV) return 32;
-    if (least <= 128 && nvec <= 128 * NV) return 128;
-    const int hold = (nvec + 512 * NV - 1) / (512 * NV);
-    const int fill = static_cast<int>(std::min<long long>(2ll * sms / p->n, nvec / 512));
-    p->parts = std::min(CLUSTER_MAX, std::max({1, hold, fill}));
-    return 512;
+    constexpr int E = Elem<T>::E;
+    const Plan s = plan(p, E, VOCAB_FWD, p.k <= 64 ? 128 : 512, sms);
+    return s.threads == 128 ? launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, stream)
+                            : launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, stream);
 }
 
-template <class T, int PASS>
-cudaError_t logprob(VocabParams p, int sms, cudaStream_t stream)
+template <class T, int PASS, bool ENT>
+cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
+    constexpr int E = Elem<T>::E;
     const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    if (PASS == VOCAB_FWD && p.k > 0) {
-        if (plan(&p, Elem<T>::E, p.k <= 64 ? 128 : 512, sms) == 128)
-            return launch_rows(token_logprob_top_kernel<T, 128>, p, 128, 1, cluster, stream);
-        return launch_rows(token_logprob_top_kernel<T, 512>, p, 512, 1, cluster, stream);
+    const Plan s = plan(p, E, PASS, 32, sms);
+    switch (s.threads) {
+    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, stream);
+    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, stream);
+    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT>, p, E, s, cluster, 0, stream);
     }
-    switch (plan(&p, Elem<T>::E, 32, sms)) {
-    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32>, p, 128, 4, cluster, stream);
-    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128>, p, 128, 1, cluster, stream);
-    default: return launch_rows(token_logprob_kernel<T, PASS, 512>, p, 512, 1, cluster, stream);
+}
+
+template <class T>
+cudaError_t logprob_pass(VocabParams p, int pass, int sms, cudaStream_t stream)
+{
+    if (pass == VOCAB_FWD) {
+        const bool ent = p.entropy || p.stats;
+        if (p.k > 0) return ent ? logprob_top<T, true>(p, sms, stream) : logprob_top<T, false>(p, sms, stream);
+        return ent ? logprob<T, VOCAB_FWD, true>(p, sms, stream) : logprob<T, VOCAB_FWD, false>(p, sms, stream);
     }
+    if (pass == VOCAB_STEP)
+        return p.entropy || p.dentropy ? logprob<T, VOCAB_STEP, true>(p, sms, stream)
+                                       : logprob<T, VOCAB_STEP, false>(p, sms, stream);
+    return p.dentropy ? logprob<T, VOCAB_BWD, true>(p, sms, stream) : logprob<T, VOCAB_BWD, false>(p, sms, stream);
+}
+
+template <class T, int PASS, int GT>
+cudaError_t distill_rows(VocabParams& p, const Plan& s, cudaStream_t stream)
+{
+    constexpr int E = Elem<T>::E;
+    auto kern = topk_distill_kernel<T, PASS, GT>;
+    size_t smem = 0;
+    if (PASS != VOCAB_BWD) {   // a word of bits per thread and tile
+        const int each = (p.vocab / E + s.parts - 1) / s.parts;
+        const int tiles = (each + GT * NV - 1) / (GT * NV);
+        smem = static_cast<size_t>(std::max(tiles, 1)) * Group<GT>::THREADS * sizeof(Bits<T>);
+        // beyond what a launch may have without asking for more (the static arrays take up to 6 KB)
+        if (smem > 40 * 1024) {
+            static std::atomic<unsigned long long> configured{0};   // bit d: set on device d
+            int dev = 0;
+            cudaError_t e = cudaGetDevice(&dev);
+            if (e != cudaSuccess) return e;
+            if (dev >= 64 || !((configured.load(std::memory_order_acquire) >> dev) & 1ull)) {
+                e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, VOCAB_MAX / 8 + 8192);
+                if (e != cudaSuccess) return e;
+                if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_acq_rel);
+            }
+        }
+    }
+    return launch_rows(kern, p, E, s, true, smem, stream);
 }
 
 template <class T, int PASS>
 cudaError_t distill(VocabParams p, int sms, cudaStream_t stream)
 {
-    switch (plan(&p, Elem<T>::E, 32, sms)) {
-    case 32: return launch_rows(topk_distill_kernel<T, PASS, 32>, p, 128, 4, true, stream);
-    case 128: return launch_rows(topk_distill_kernel<T, PASS, 128>, p, 128, 1, true, stream);
-    default: return launch_rows(topk_distill_kernel<T, PASS, 512>, p, 512, 1, true, stream);
+    const Plan s = plan(p, Elem<T>::E, PASS, 32, sms);
+    switch (s.threads) {
+    case 32: return distill_rows<T, PASS, 32>(p, s, stream);
+    case 128: return distill_rows<T, PASS, 128>(p, s, stream);
+    default: return distill_rows<T, PASS, 512>(p, s, stream);
     }
-}
-
-template <class T>
-cudaError_t logprob_pass(const VocabParams& p, int pass, int sms, cudaStream_t stream)
-{
-    return pass == VOCAB_FWD    ? logprob<T, VOCAB_FWD>(p, sms, stream)
-           : pass == VOCAB_STEP ? logprob<T, VOCAB_STEP>(p, sms, stream)
-                                : logprob<T, VOCAB_BWD>(p, sms, stream);
 }
 
 template <class T>

@@ -30,7 +30,7 @@ struct VocabParams {
     void* dlogits;
     long long n, ld, ld_d;
     int vocab, k, rest;
-    int parts;                // CTAs of a row
+    int each;                 // 16-byte vectors of a row per CTA (the grid's y: CTAs of a row)
     float temperature;
     float c;                  // 1 / temperature
     float c2;                 // log2(e) / temperature
@@ -127,6 +127,7 @@ struct Elem;
 template <>
 struct Elem<float> {
     static constexpr int E = 4;
+    using Bits = unsigned int;                       // one per element of NV vectors
     static constexpr uint32_t FILL = 0xff800000u;   // -inf
     __device__ static float get(const float* p) { return *p; }
     __device__ static void put(float* p, float x) { *p = x; }
@@ -147,6 +148,21 @@ struct Elem<float> {
                                    max_nan(__uint_as_float(d[j].z), __uint_as_float(d[j].w))));
         return m;
     }
+    // a bit for each element that reaches `limit` (or is NaN), and the place of a bit's element in its tile
+    static constexpr float LOWEST = -3.402823466e38f;
+    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], float limit)
+    {
+        unsigned int bits = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float x[4];
+            unpack(d[j], x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bits |= x[e] < limit ? 0u : 1u << (j * 4 + e);
+        }
+        return bits;
+    }
+    __device__ __forceinline__ static int place(int bit) { return bit; }
     // the elements whose bits are set := -inf
     __device__ __forceinline__ static void ban(uint4& u, uint32_t bits)
     {
@@ -160,6 +176,7 @@ struct Elem<float> {
 template <>
 struct Elem<__nv_bfloat16> {
     static constexpr int E = 8;
+    using Bits = unsigned long long;
     static constexpr uint32_t FILL = 0xff80ff80u;
     __device__ static float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     __device__ static void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
@@ -182,6 +199,25 @@ struct Elem<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    // as above; a word's two elements compared at once, the bits of words 0..15 and 16..31 in
+    // halves: low elements, then high ones
+    static constexpr float LOWEST = -3.38953139e38f;
+    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], float limit)
+    {
+        const __nv_bfloat162 l = __float2bfloat162_rn(limit);   // exact: an element's value
+        uint32_t bits[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t w[4] = {d[j].x, d[j].y, d[j].z, d[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t below = __hlt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), l);
+                bits[j / 4] |= ~below & (0x00010001u << (j % 4 * 4 + i));
+            }
+        }
+        return static_cast<unsigned long long>(bits[1]) << 32 | bits[0];
+    }
+    __device__ __forceinline__ static int place(int bit) { return (bit >> 5) * 32 + (bit & 15) * 2 + (bit >> 4 & 1); }
     __device__ __forceinline__ static uint32_t max_pair(uint32_t a, uint32_t b)
     {
         const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
@@ -206,67 +242,54 @@ struct Elem<__nv_bfloat16> {
 };
 
 // ------------------------------------------------------------- rows in memory
-// A row of `vocab` elements as 16-byte vectors at 16-byte boundaries: vector v
-// holds elements v E - off .. v E - off + E - 1; those outside the row read as
-// -inf and are never stored.  Pitch and base need the element's alignment only.
+// A row of `vocab` elements: the 16-byte vectors at 16-byte boundaries, and up
+// to E - 1 single elements before and after them (its edges).  Pitch and base
+// need the element's alignment only.
 template <class T>
 struct Row {
     static constexpr int E = Elem<T>::E;
     const T* p;
-    int off, nvec, vocab;
+    int vocab, head, full, tail;   // elements before the vectors, vectors, elements after them
 
     __device__ Row(const T* row, int v) : p(row), vocab(v)
     {
-        off = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
-        nvec = (off + vocab + E - 1) / E;
+        const int over = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
+        head = min((E - over) % E, v);
+        full = (v - head) / E;
+        tail = v - head - full * E;
     }
-    __device__ __forceinline__ int first(int v) const { return v * E - off; }
-    __device__ __forceinline__ uint4 load(int v) const
-    {
-        const int j = first(v);
-        if (j >= 0 && j + E <= vocab) return *reinterpret_cast<const uint4*>(p + j);
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = j + e >= 0 && j + e < vocab ? Elem<T>::get(p + j + e) : NEG_INF;
-        return Elem<T>::pack(x);
-    }
-    // x into the same elements of `out`; `same`: out has this row's offset from a 16-byte boundary
-    __device__ __forceinline__ void store(T* out, bool same, int v, const float (&x)[E]) const
-    {
-        const int j = first(v);
-        if (same && j >= 0 && j + E <= vocab) {
-            *reinterpret_cast<uint4*>(out + j) = Elem<T>::pack(x);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (j + e >= 0 && j + e < vocab) Elem<T>::put(out + j + e, x[e]);
-        }
-    }
+    __device__ __forceinline__ int edges() const { return head + tail; }
+    __device__ __forceinline__ int edge(int i) const { return i < head ? i : vocab - tail + i - head; }
+    __device__ __forceinline__ const uint4* vec() const { return reinterpret_cast<const uint4*>(p + head); }
 };
 
 // The GT threads that work on one row in one CTA: a warp (four rows a CTA) or
-// the whole CTA, of `parts` that share the row as a cluster.
+// the whole CTA; the row's CTAs lie along the grid's y, and form a cluster
+// where they exchange anything.
 template <int GT>
 struct Group {
     static constexpr int ROWS = GT == 32 ? 4 : 1, THREADS = GT * ROWS, W = GT / 32, TILE = GT * NV;
     static constexpr int CTAS = GT == 32 ? 6 : 1024 / THREADS;   // an SM's, for the registers a thread may have
     long long row;
-    int rank, tid, lane, warp, slot;
+    int rank, parts, tid, lane, warp, slot;
 
-    __device__ explicit Group(int parts)
+    __device__ Group()
     {
         tid = GT == 32 ? threadIdx.x & 31 : threadIdx.x;
         lane = threadIdx.x & 31;
         warp = tid >> 5;
         slot = GT == 32 ? threadIdx.x >> 5 : 0;
-        row = GT == 32 ? blockIdx.x * 4ll + slot : blockIdx.x / static_cast<unsigned int>(parts);
-        rank = GT == 32 ? 0 : blockIdx.x % static_cast<unsigned int>(parts);
+        row = GT == 32 ? blockIdx.x * 4ll + slot : blockIdx.x;
+        rank = GT == 32 ? 0 : blockIdx.y;
+        parts = GT == 32 ? 1 : gridDim.y;
     }
     __device__ __forceinline__ static void sync()
     {
         if (GT == 32) __syncwarp();
         else __syncthreads();
     }
+    // the one warp that has the row's edges, an element per lane
+    __device__ __forceinline__ bool has_edges() const { return rank == 0 && warp == W - 1; }
 };
 
 // The vectors of one CTA of a row, in tiles of GT x NV.
@@ -274,25 +297,29 @@ template <class T, int GT>
 struct Part {
     int begin, end, tiles;
 
-    __device__ Part(const Row<T>& row, const Group<GT>& g, int parts)
+    __device__ Part(const Row<T>& row, const Group<GT>& g, int each)
     {
-        const int each = (row.nvec + parts - 1) / parts;
-        begin = min(g.rank * each, row.nvec);
-        end = min(begin + each, row.nvec);
+        begin = min(g.rank * each, row.full);
+        end = min(begin + each, row.full);
         tiles = (end - begin + Group<GT>::TILE - 1) / Group<GT>::TILE;
     }
-    __device__ __forceinline__ int at(const Group<GT>& g, int tile, int j) const
-    {
-        return begin + tile * Group<GT>::TILE + j * GT + g.tid;
-    }
+    // this thread's first vector of a tile; vector j lies GT j after it and is there where left > GT j
+    __device__ __forceinline__ int at(const Group<GT>& g, int tile) const { return begin + tile * Group<GT>::TILE + g.tid; }
+    __device__ __forceinline__ int left(const Group<GT>& g, int tile) const { return end - at(g, tile); }
     __device__ __forceinline__ void load(const Row<T>& row, const Group<GT>& g, int tile, uint4 (&d)[NV]) const
     {
+        const uint4* q = row.vec() + at(g, tile);
+        const int n = left(g, tile);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int v = at(g, tile, j);
             d[j] = make_uint4(Elem<T>::FILL, Elem<T>::FILL, Elem<T>::FILL, Elem<T>::FILL);
-            if (v < end) d[j] = row.load(v);
+            if (n > j * GT) d[j] = q[j * GT];
         }
+    }
+    // the thread that holds vector v
+    __device__ __forceinline__ bool owns(const Group<GT>& g, int v) const
+    {
+        return v >= begin && v < end && (v - begin) % GT == g.tid;
     }
 };
 
@@ -315,7 +342,7 @@ __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v)
 }
 
 // -------------------------------------------------------- softmax statistics
-// m = max x, s = sum 2^y, t = sum 2^y y with y = c2 (x - m), in fp32.
+// m = max x, s = sum 2^y, t = sum 2^y y with y = c2 (x - m), in fp32 (t where ENT).
 // Nothing seen: m = -inf, s = t = 0.  A NaN, or +inf, makes s NaN.
 struct Acc {
     float m, s, t;
@@ -326,24 +353,33 @@ __device__ __forceinline__ Acc acc_none() { return Acc{NEG_INF, 0.f, 0.f}; }
 // Moves a's sums to a maximum m that is not below a's.  Differences are held
 // above FLOOR: a sum times the distance from a mask of the type's lowest value
 // would overflow where its weight is 0.
+template <bool ENT>
 __device__ __forceinline__ Acc acc_to(const Acc& a, float m, float c2)
 {
     const float d = a.s == 0.f ? 0.f : fmaxf((a.m - m) * c2, FLOOR), f = ex2(d);
-    return Acc{m, a.s * f, f * (a.t + a.s * d)};
+    return Acc{m, a.s * f, ENT ? f * (a.t + a.s * d) : 0.f};
 }
 
+template <bool ENT>
 __device__ __forceinline__ Acc acc_merge(const Acc& a, const Acc& b, float c2)
 {
     const float m = max_nan(a.m, b.m);
-    const Acc x = acc_to(a, m, c2), y = acc_to(b, m, c2);
+    const Acc x = acc_to<ENT>(a, m, c2), y = acc_to<ENT>(b, m, c2);
     return Acc{m, x.s + y.s, x.t + y.t};
 }
 
+template <bool ENT>
 __device__ __forceinline__ Acc acc_warp(const Acc& a, float c2)
 {
     const float m = max_nan_warp(a.m);
-    const Acc x = acc_to(a, m, c2);
-    return Acc{m, sum_warp(x.s), sum_warp(x.t)};
+    const Acc x = acc_to<ENT>(a, m, c2);
+    return Acc{m, sum_warp(x.s), ENT ? sum_warp(x.t) : 0.f};
+}
+
+// One element of maximum x.
+__device__ __forceinline__ Acc acc_one(float x)
+{
+    return Acc{x, x == NEG_INF ? 0.f : x - x == 0.f ? 1.f : __int_as_float(0x7fffffff), 0.f};
 }
 
 // y = c2 x - b with b = c2 m rounded takes one fused operation per element and
@@ -354,76 +390,77 @@ struct Base {
     __device__ __forceinline__ Base(float m, float c2) : b(m * c2), delta(fmaf(m, c2, -(m * c2))) {}
 };
 
-// The statistics of the elements of one tile that a thread holds; ENT: with t.
-template <class T, bool ENT>
-__device__ __forceinline__ Acc acc_tile(const uint4 (&d)[NV], float m, float c2)
+// The statistics of the elements of one tile that a thread holds.  FAR: for
+// maxima whose exponent rounds coarsely (masks of the lowest value, +inf, NaN),
+// the difference from the maximum first, as an operation of its own.
+template <class T, bool ENT, bool FAR>
+__device__ __forceinline__ Acc acc_tile_from(const uint4 (&d)[NV], float m, float c2)
 {
     constexpr int E = Elem<T>::E;
-    Acc a{m, 0.f, 0.f};
-    if (m == NEG_INF) return a;
-    if (fabsf(m * c2) < NEAR) {
-        const Base base(m, c2);
-        const Pair cc = pair(c2, c2), nb = pair(-base.b, -base.b);
-        Pair s2[2] = {0, 0}, t2[2] = {0, 0};
+    const Base base(FAR ? 0.f : m, c2);
+    const Pair cc = pair(c2, c2), nb = pair(-base.b, -base.b), nm = pair(-m, -m);
+    Pair s2[2] = {0, 0}, t2[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float x[E];
-            Elem<T>::unpack(d[j], x);
+    for (int j = 0; j < NV; ++j) {
+        float x[E];
+        Elem<T>::unpack(d[j], x);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                float y0, y1;
-                split(fma2(pair(x[e], x[e + 1]), cc, nb), y0, y1);
-                const Pair w = pair(ex2(y0), ex2(y1));
-                s2[e >> 1 & 1] = add2(s2[e >> 1 & 1], w);
-                if (ENT) t2[e >> 1 & 1] = fma2(w, pair(fmaxf(y0, FLOOR), fmaxf(y1, FLOOR)), t2[e >> 1 & 1]);
-            }
+        for (int e = 0; e < E; e += 2) {
+            const Pair v = pair(x[e], x[e + 1]);
+            float y0, y1;
+            split(FAR ? mul2(add2(v, nm), cc) : fma2(v, cc, nb), y0, y1);
+            const Pair w = pair(ex2(y0), ex2(y1));
+            s2[e >> 1 & 1] = add2(s2[e >> 1 & 1], w);
+            if (ENT) t2[e >> 1 & 1] = fma2(w, pair(fmaxf(y0, FLOOR), fmaxf(y1, FLOOR)), t2[e >> 1 & 1]);
         }
-        float lo, hi;
-        split(add2(s2[0], s2[1]), lo, hi);
-        const float s = lo + hi, f = ex2(-base.delta);
-        a.s = s * f;
-        if (ENT) {
-            split(add2(t2[0], t2[1]), lo, hi);
-            a.t = f * (lo + hi - base.delta * s);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float x[E];
-            Elem<T>::unpack(d[j], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float y = (x[e] - m) * c2, w = ex2(y);
-                a.s += w;
-                a.t += w * fmaxf(y, FLOOR);
-            }
-        }
+    }
+    float lo, hi;
+    split(add2(s2[0], s2[1]), lo, hi);
+    const float s = lo + hi, f = FAR ? 1.f : ex2(-base.delta);
+    Acc a{m, s * f, 0.f};
+    if (ENT) {
+        split(add2(t2[0], t2[1]), lo, hi);
+        a.t = f * (lo + hi - base.delta * s);
     }
     return a;
 }
 
-// The row's statistics in every thread, from those of each thread; slots: one
-// per warp of each CTA of the row.
-template <int GT>
-__device__ __forceinline__ Acc acc_row(Acc a, float c2, const Group<GT>& g, int parts, float4* slots)
+template <class T, bool ENT>
+__device__ __forceinline__ Acc acc_tile(const uint4 (&d)[NV], float m, float c2)
 {
-    a = acc_warp(a, c2);
-    if (GT == 32) return a;
-    const float4 mine = make_float4(a.m, a.s, a.t, 0.f);
-    if (parts == 1) {
+    if (m == NEG_INF) return acc_none();
+    if (fabsf(m * c2) < NEAR) return acc_tile_from<T, ENT, false>(d, m, c2);
+    return acc_tile_from<T, ENT, true>(d, m, c2);
+}
+
+// Every warp's statistics to every CTA of the row; the barrier of the exchange.
+template <int GT>
+__device__ __forceinline__ void exchange(const Acc& a, float extra, const Group<GT>& g, float4* slots)
+{
+    const float4 mine = make_float4(a.m, a.s, a.t, extra);
+    if (g.parts == 1) {
         if (g.lane == 0) slots[g.warp] = mine;
         __syncthreads();
     } else {
         cluster_wait();   // every CTA of the row runs
-        if (g.lane < parts) st_cluster_f4(mapa_shared(smem_u32(slots + g.rank * Group<GT>::W + g.warp), g.lane), mine);
+        if (g.lane < g.parts) st_cluster_f4(mapa_shared(smem_u32(slots + g.rank * Group<GT>::W + g.warp), g.lane), mine);
         cluster_sync();
     }
-    a = acc_none();
-    for (int i = g.lane; i < Group<GT>::W * parts; i += 32) {
-        const float4 o = slots[i];
-        a = acc_merge(a, Acc{o.x, o.y, o.z}, c2);
+}
+
+template <int GT, bool ENT>
+__device__ __forceinline__ Acc acc_slots(const float4* slots, int count, const Group<GT>& g, float c2)
+{
+    Acc a = acc_none();
+    if (g.lane < count) {
+        const float4 o = slots[g.lane];
+        a = Acc{o.x, o.y, o.z};
     }
-    return acc_warp(a, c2);
+    for (int i = g.lane + 32; i < count; i += 32) {
+        const float4 o = slots[i];
+        a = acc_merge<ENT>(a, Acc{o.x, o.y, o.z}, c2);
+    }
+    return acc_warp<ENT>(a, c2);
 }
 
 // --------------------------------------------------------------- top k of a row
@@ -444,292 +481,418 @@ __device__ __forceinline__ unsigned long long token_key(float x, int j)
     return static_cast<unsigned long long>(value_key(x)) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
 }
 
-constexpr int TOP_MAX_VALUES = VOCAB_MAX_K + CLUSTER_MAX * 16;
-
+// The candidates of a row's top k, in the first of its CTAs.
 struct TopShared {
     unsigned long long key[CAND_MAX];
-    uint32_t value[TOP_MAX_VALUES];     // the largest thread maxima of each warp
+    int id[CAND_MAX];                   // a share of it for each CTA of the row
     unsigned int hist[256];
-    unsigned int count, digit, above, bound;
+    unsigned int counts[CLUSTER_MAX];
+    unsigned int count, digit, above, bound, local;
+    float m0, logs;
 };
 
 // Gathers at least k and at most CAND_MAX keys of a row in memory, the k
 // largest among them, by a radix search from the top digit that stops as soon
-// as few enough are left: for rows whose largest tokens are not spread over the threads.
+// as few enough are left: for rows whose largest tokens are not spread over the
+// threads, or tie in great number.
 template <class T, int GT>
-__device__ void top_radix(const Row<T>& row, int k, const Group<GT>& g, TopShared& sh)
+__device__ __noinline__ void top_radix(const T* p, int vocab, unsigned int k, TopShared& sh)
 {
-    constexpr int E = Elem<T>::E;
     unsigned long long bound = 0;
     unsigned int taken = 0;              // keys above the digits found so far
     for (int shift = 56; shift >= 0; shift -= 8) {
-        g.sync();
-        for (int i = g.tid; i < 256; i += GT) sh.hist[i] = 0;
-        g.sync();
-        for (int v = g.tid; v < row.nvec; v += GT) {
-            float x[E];
-            Elem<T>::unpack(row.load(v), x);
-            for (int e = 0; e < E; ++e) {
-                const int j = row.first(v) + e;
-                if (j < 0 || j >= row.vocab) continue;
-                const unsigned long long key = token_key(x[e], j);
-                if (shift == 56 || key >> (shift + 8) == bound >> (shift + 8))
-                    atomicAdd(&sh.hist[key >> shift & 255u], 1u);
-            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 256; i += GT) sh.hist[i] = 0;
+        __syncthreads();
+        for (int j = threadIdx.x; j < vocab; j += GT) {
+            const unsigned long long key = token_key(Elem<T>::get(p + j), j);
+            if (shift == 56 || key >> (shift + 8) == bound >> (shift + 8)) atomicAdd(&sh.hist[key >> shift & 255u], 1u);
         }
-        g.sync();
-        if (g.tid == 0) {
+        __syncthreads();
+        if (threadIdx.x == 0) {
             unsigned int above = taken;
             int d = 255;
-            while (d > 0 && above + sh.hist[d] < static_cast<unsigned int>(k)) above += sh.hist[d--];
+            while (d > 0 && above + sh.hist[d] < k) above += sh.hist[d--];
             sh.digit = d;
             sh.above = above;
             sh.count = 0;
         }
-        g.sync();
+        __syncthreads();
         taken = sh.above;
         bound |= static_cast<unsigned long long>(sh.digit) << shift;
-        if (taken + sh.hist[sh.digit] <= CAND_MAX) break;
+        if (taken + sh.hist[sh.digit] <= min(CAND_MAX, 2u * k + 64u)) break;
     }
-    for (int v = g.tid; v < row.nvec; v += GT) {
-        float x[E];
-        Elem<T>::unpack(row.load(v), x);
-        for (int e = 0; e < E; ++e) {
-            const int j = row.first(v) + e;
-            if (j < 0 || j >= row.vocab) continue;
-            const unsigned long long key = token_key(x[e], j);
-            if (key >= bound) sh.key[atomicAdd(&sh.count, 1u)] = key;
+    for (int j = threadIdx.x; j < vocab; j += GT) {
+        const unsigned long long key = token_key(Elem<T>::get(p + j), j);
+        if (key >= bound) sh.key[atomicAdd(&sh.count, 1u)] = key;
+    }
+    __syncthreads();
+}
+
+// Sorts key[0 .. count), padded to R x 32 with zeros (below every key), falling,
+// in one warp: element r 32 + lane in register r.
+template <int R>
+__device__ __forceinline__ void sort_warp(unsigned long long (&key)[R], int lane)
+{
+#pragma unroll
+    for (int size = 2; size <= 32 * R; size *= 2) {
+#pragma unroll
+        for (int step = size / 2; step; step /= 2) {
+            if (step >= 32) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int o = r ^ step / 32;
+                    if (o > r) {
+                        const bool falling = (r * 32 & size) == 0;
+                        const unsigned long long a = key[r], b = key[o];
+                        const bool swap = falling ? a < b : a > b;
+                        key[r] = swap ? b : a;
+                        key[o] = swap ? a : b;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const unsigned long long o = __shfl_xor_sync(~0u, key[r], step);
+                    const int i = r * 32 + lane;
+                    const bool larger = ((i & size) == 0) == ((i & step) == 0);   // this lane keeps the larger
+                    key[r] = (key[r] > o) == larger ? key[r] : o;
+                }
+            }
         }
     }
-    g.sync();
+}
+
+// Sorts key[0 .. n), n a power of two, falling, by the whole CTA.
+template <int GT>
+__device__ __noinline__ void sort_block(unsigned long long* key, int n)
+{
+    for (int size = 2; size <= n; size *= 2) {
+        for (int step = size / 2; step; step /= 2) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n / 2; i += GT) {
+                const int a = i / step * 2 * step + i % step, b = a + step;
+                const unsigned long long x = key[a], y = key[b];
+                if ((a & size) == 0 ? x < y : x > y) key[a] = y, key[b] = x;
+            }
+        }
+    }
+    __syncthreads();
 }
 
 // ------------------------------------------------- token log probabilities
-template <class T, int PASS, int GT>
+// The gradient of one CTA's share of a row.  H: with the entropy's term,
+//   c p (-g - h (logp + H)) = 2^y (A + B y),   y = c2 x - base.b.
+template <class T, int PASS, int GT, bool ENT>
+__device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>& row, const Part<T, GT>& part, const Group<GT>& g,
+                                             float m, float inv_s, float logs, float H, float up_g, float up_h, int y, float xe,
+                                             uint4 (&d)[NV])
+{
+    constexpr int E = Elem<T>::E;
+    T* out = static_cast<T*>(P.dlogits) + g.row * P.ld_d;
+    uint4* vout = reinterpret_cast<uint4*>(out + row.head);
+    const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
+    const bool live = (up_g != 0.f || up_h != 0.f) && m != NEG_INF, near = fabsf(m * P.c2) < NEAR;
+    const Base base(m, P.c2);
+    const float scale = -P.c * inv_s * ex2(-base.delta);
+    const float A = scale * (up_g + (ENT ? up_h * (H - logs - LN2 * base.delta) : 0.f)), B = ENT ? scale * up_h * LN2 : 0.f;
+    const auto one = [&](float x) -> float {   // without the target's own term
+        if (!live) return 0.f;
+        const float l = (x - m) * P.c2, p = inv_s * ex2(l);
+        return -P.c * p * (up_g + (ENT ? up_h * (LN2 * fmaxf(l, FLOOR) - logs + H) : 0.f));
+    };
+    for (int t = part.tiles - 1; t >= 0; --t) {
+        const int first = part.at(g, t), left = part.left(g, t);
+        if (live && near && same) {
+            if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
+            const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A), B2 = pair(B, B);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float x[E];
+                Elem<T>::unpack(d[j], x);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float y0, y1;
+                    split(fma2(pair(x[e], x[e + 1]), cc, nb), y0, y1);
+                    const Pair w = pair(ex2(y0), ex2(y1));
+                    split(mul2(w, ENT ? fma2(pair(fmaxf(y0, FLOOR), fmaxf(y1, FLOOR)), B2, A2) : A2), x[e], x[e + 1]);
+                }
+                if (left > j * GT) vout[first + j * GT] = Elem<T>::pack(x);
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j * GT < left && j < NV; ++j) {
+                float x[E] = {};
+                if (live) Elem<T>::unpack(row.vec()[first + j * GT], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = one(x[e]);
+                if (same) {
+                    vout[first + j * GT] = Elem<T>::pack(x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) Elem<T>::put(out + row.head + (first + j * GT) * E + e, x[e]);
+                }
+            }
+        }
+    }
+    if (g.has_edges() && g.lane < row.edges()) {
+        const int id = row.edge(g.lane);
+        Elem<T>::put(out + id, one(xe) + (live && id == y ? P.c * up_g : 0.f));
+    }
+}
+
+template <class T, int PASS, int GT, bool ENT>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
     using G = Group<GT>;
     __shared__ float4 slots[PASS == VOCAB_BWD || GT == 32 ? 1 : CLUSTER_MAX * G::W];
-    const G g(P.parts);
+    const G g;
     if (GT == 32 && g.row >= P.n) return;
-    const int parts = GT == 32 ? 1 : P.parts;
-    const bool cluster = PASS != VOCAB_BWD && GT != 32 && parts > 1;
-    if (cluster) cluster_arrive();
+    if (PASS != VOCAB_BWD && g.parts > 1) cluster_arrive();
     const Row<T> row(static_cast<const T*>(P.logits) + g.row * P.ld, P.vocab);
-    const Part<T, GT> part(row, g, parts);
+    const Part<T, GT> part(row, g, P.each);
     uint4 d[NV];
     part.load(row, g, 0, d);
-    const long long y = P.targets ? P.targets[g.row] : -1;
-    const bool there = y >= 0 && y < P.vocab;
-    float up_g = 0.f, up_h = 0.f, xy = 0.f;
+    const long long target = P.targets ? P.targets[g.row] : -1;
+    const bool there = target >= 0 && target < P.vocab;
+    const int y = there ? static_cast<int>(target) : -1;
+    // the target's logit: for its log probability, and its own gradient (the
+    // thread that holds its vector)
+    const int vy = y >= row.head && y < row.head + row.full * E ? (y - row.head) / E : -1;
+    const bool owner = PASS != VOCAB_FWD && part.owns(g, vy);
+    float xy = 0.f, xe = NEG_INF, up_g = 0.f, up_h = 0.f;
+    if (there && (owner || (PASS != VOCAB_BWD && g.rank == 0 && g.tid == 0))) xy = Elem<T>::get(row.p + y);
+    if (g.has_edges() && g.lane < row.edges()) xe = Elem<T>::get(row.p + row.edge(g.lane));
     if (PASS != VOCAB_FWD) {
         up_g = there && P.dlogp ? P.dlogp[g.row] : 0.f;
-        up_h = P.dentropy ? P.dentropy[g.row] : 0.f;
+        up_h = ENT && P.dentropy ? P.dentropy[g.row] : 0.f;
     }
-    float m, logs, H;
+    float m, s, logs = 0.f, H = 0.f;
     if (PASS == VOCAB_BWD) {
         const float4 st = reinterpret_cast<const float4*>(P.stats)[g.row];
-        m = st.x, logs = st.y, H = st.z;
+        m = st.x, logs = st.y, H = st.z, s = expf(logs);
     } else {
-        if (P.logp && there && g.rank == 0 && g.tid == 0) xy = Elem<T>::get(row.p + y);
-        const bool ent = P.entropy || P.stats || (PASS == VOCAB_STEP && P.dentropy);
         Acc a = acc_none();
         for (int t = 0; t < part.tiles; ++t) {
             if (t > 0) part.load(row, g, t, d);
-            const float mt = Elem<T>::max_of(d);
-            const Acc b = ent ? acc_tile<T, true>(d, mt, P.c2) : acc_tile<T, false>(d, mt, P.c2);
-            a = t > 0 ? acc_merge(a, b, P.c2) : b;
+            const Acc b = acc_tile<T, ENT>(d, Elem<T>::max_of(d), P.c2);
+            a = t > 0 ? acc_merge<ENT>(a, b, P.c2) : b;
         }
-        a = acc_row(a, P.c2, g, parts, slots);
-        m = a.m;
-        logs = m == NEG_INF ? 0.f : logf(a.s);
-        H = m == NEG_INF ? 0.f : logs - LN2 * (a.t / a.s);
+        if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
+        a = acc_warp<ENT>(a, P.c2);
+        if (GT != 32) {
+            exchange(a, 0.f, g, slots);
+            if (PASS == VOCAB_FWD && (g.rank != 0 || g.warp != 0)) return;
+            a = acc_slots<GT, ENT>(slots, G::W * g.parts, g, P.c2);
+        }
+        m = a.m, s = a.s;
+        if (ENT || (g.rank == 0 && g.warp == 0)) {
+            logs = m == NEG_INF ? 0.f : logf(s);
+            H = ENT && m != NEG_INF ? logs - LN2 * (a.t / s) : 0.f;
+        }
     }
-    const float m0 = m == NEG_INF ? 0.f : m;
     if (PASS != VOCAB_BWD && g.rank == 0 && g.tid == 0) {
-        if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
-        if (P.entropy) P.entropy[g.row] = H;
+        if (P.logp) P.logp[g.row] = there ? (xy - (m == NEG_INF ? 0.f : m)) * P.c - logs : 0.f;
+        if (ENT && P.entropy) P.entropy[g.row] = H;
         if (PASS == VOCAB_FWD && P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
     }
     if constexpr (PASS != VOCAB_FWD) {
-        T* out = static_cast<T*>(P.dlogits) + g.row * P.ld_d;
-        const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
-        const bool live = (up_g != 0.f || up_h != 0.f) && m != NEG_INF;
-        const bool near = fabsf(m * P.c2) < NEAR;
-        const Base base(m0, P.c2);
-        const float scale = -P.c * ex2(-base.delta - logs * LOG2E);   // - c / s, to the base's power
-        const float A = scale * (up_g + up_h * (H - logs - LN2 * base.delta)), B = scale * up_h * LN2;
-        const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A), B2 = pair(B, B);
-        const int vy = there ? (static_cast<int>(y) + row.off) / E : -1, ey = (static_cast<int>(y) + row.off) % E;
-        for (int t = part.tiles - 1; t >= 0; --t) {
-            if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int v = part.at(g, t, j);
-                if (v >= part.end) break;
-                float x[E];
-                Elem<T>::unpack(d[j], x);
-                if (!live) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = 0.f;
-                } else if (near) {
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        float y0, y1;
-                        split(fma2(pair(x[e], x[e + 1]), cc, nb), y0, y1);
-                        const Pair w = pair(ex2(y0), ex2(y1));
-                        const Pair r = up_h == 0.f ? mul2(w, A2) : mul2(w, fma2(pair(fmaxf(y0, FLOOR), fmaxf(y1, FLOOR)), B2, A2));
-                        split(r, x[e], x[e + 1]);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float l = (x[e] - m0) * P.c - logs, p = ex2(l * LOG2E);
-                        x[e] = -P.c * p * (up_g + up_h * (fmaxf(l, FLOOR) + H));
-                    }
-                }
-                if (live && v == vy) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (e == ey) x[e] += P.c * up_g;
-                }
-                row.store(out, same, v, x);
-            }
+        const float inv_s = 1.f / s;
+        if (!ENT || up_h == 0.f) emit_logprob<T, PASS, GT, false>(P, row, part, g, m, inv_s, logs, H, up_g, 0.f, y, xe, d);
+        else emit_logprob<T, PASS, GT, true>(P, row, part, g, m, inv_s, logs, H, up_g, up_h, y, xe, d);
+        if (owner && m != NEG_INF && (up_g != 0.f || up_h != 0.f)) {   // over its own store of that vector
+            const float l = (xy - m) * P.c2, p = inv_s * ex2(l);
+            const float r = P.c * (up_g - p * (up_g + up_h * (LN2 * fmaxf(l, FLOOR) - logs + H)));
+            Elem<T>::put(static_cast<T*>(P.dlogits) + g.row * P.ld_d + y, r);
         }
     }
 }
 
-// The forward with the k most likely tokens.  A bound that at least k tokens
-// reach is the k-th largest of thread maxima, of which each warp gives its
-// `each` largest (each x warps >= k): one barrier more than the statistics.
-// Tokens of this value and above (few more than k, when the largest are spread
-// over the threads) are gathered from the registers, and ranked.
-template <class T, int GT>
+// The forward with the k most likely tokens.  Each warp gives, with its
+// statistics, the `each`-th largest of its threads' maxima; at least k tokens
+// reach the ceil(k / each)-th largest of those, and few more than k do where the
+// largest are spread over the threads (`each` a little above k over the number of
+// warps: 105 at k = 64 of 32000 in random order, where each = k / warps gives
+// 170 and larger ones more barriers' worth of work).  These are gathered, by
+// their bits, from the registers, and sorted in one warp.
+template <class T, int GT, bool ENT>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_top_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
     using G = Group<GT>;
-    static_assert(GT > 32, "a warp's rows have no candidates list of their own");
+    static_assert(GT > 32, "one list of candidates per CTA");
     __shared__ float4 slots[CLUSTER_MAX * G::W];
     __shared__ TopShared top;
-    const G g(P.parts);
-    const bool cluster = P.parts > 1;
-    if (g.tid == 0) top.count = 0;
-    __syncwarp();
-    if (cluster) cluster_arrive();   // this CTA runs, its count is set
+    const G g;
+    const bool cluster = g.parts > 1;
+    if (cluster) cluster_arrive();
     const Row<T> row(static_cast<const T*>(P.logits) + g.row * P.ld, P.vocab);
-    const Part<T, GT> part(row, g, P.parts);
+    const Part<T, GT> part(row, g, P.each);
     uint4 d[NV];
     part.load(row, g, 0, d);
+    if (g.tid == 0) top.local = 0;
     const long long y = P.targets ? P.targets[g.row] : -1;
     const bool there = y >= 0 && y < P.vocab;
-    float xy = 0.f;
+    float xy = 0.f, xe = NEG_INF;
     if (there && g.rank == 0 && g.tid == 0) xy = Elem<T>::get(row.p + y);
-    const bool ent = P.entropy || P.stats;
+    const bool edge = g.has_edges() && g.lane < row.edges();
+    if (edge) xe = Elem<T>::get(row.p + row.edge(g.lane));
     Acc a = acc_none();
     for (int t = 0; t < part.tiles; ++t) {
         if (t > 0) part.load(row, g, t, d);
-        const float mt = Elem<T>::max_of(d);
-        const Acc b = ent ? acc_tile<T, true>(d, mt, P.c2) : acc_tile<T, false>(d, mt, P.c2);
-        a = t > 0 ? acc_merge(a, b, P.c2) : b;
+        const Acc b = acc_tile<T, ENT>(d, Elem<T>::max_of(d), P.c2);
+        // (acc_tile gives acc_none for a tile of nothing but -inf)
+        a = t > 0 ? acc_merge<ENT>(a, b, P.c2) : b;
     }
+    if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
     const uint32_t mine = value_key(a.m);   // of this thread
-    if (cluster) cluster_wait();
-    // each warp's largest thread maxima, to every CTA of the row
-    const int full = (row.nvec + P.parts - 1) / P.parts;
-    const int warps = min(G::W, (full + 31) / 32) * P.parts;   // warps of the row that hold tokens
-    const int each = (P.k + warps - 1) / warps;
-    const int values = each * G::W * P.parts;
-    const bool bounded = each <= 32 && values <= TOP_MAX_VALUES;
+    a = acc_warp<ENT>(a, P.c2);
+    const int warps = G::W * g.parts;
+    // one and a half times k over the warps, one where there are as many warps
+    const int each = P.k <= warps ? 1 : (3 * P.k + 2 * warps - 1) / (2 * warps);
+    const bool bounded = each <= 24;
     if (bounded) {
-        uint32_t left = mine;
+        uint32_t left = mine, best = 0;
         for (int i = 0; i < each; ++i) {
-            const uint32_t best = __reduce_max_sync(~0u, left);
-            const uint32_t at = (g.rank * G::W + g.warp) * each + i;
-            if (!cluster) {
-                if (g.lane == 0) top.value[at] = best;
-            } else if (g.lane < P.parts) {
-                st_shared_cluster_u32(mapa_shared(smem_u32(top.value + at), g.lane), best);
-            }
+            best = __reduce_max_sync(~0u, left);
             if (g.lane == __ffs(__ballot_sync(~0u, left == best)) - 1) left = 0;
         }
-    }
-    {
-        a = acc_warp(a, P.c2);
-        const float4 o = make_float4(a.m, a.s, a.t, 0.f);
-        if (!cluster) {
-            if (g.lane == 0) slots[g.warp] = o;
-            __syncthreads();
+        exchange(a, __uint_as_float(best), g, slots);
+        // the value with `before` = ceil(k / each) - 1 before it
+        const unsigned int before = (P.k + each - 1) / each - 1;
+        uint32_t bound;
+        if (!cluster) {   // at most 16 values: every warp for itself
+            const uint32_t v = g.lane < G::W ? __float_as_uint(slots[g.lane].w) : 0u;
+            unsigned int n = 0;
+#pragma unroll
+            for (int i = 0; i < G::W; ++i) {
+                const uint32_t o = __shfl_sync(~0u, v, i);
+                n += o > v || (o == v && i < g.lane);
+            }
+            bound = __shfl_sync(~0u, v, __ffs(__ballot_sync(~0u, n == before)) - 1);
         } else {
-            if (g.lane < P.parts) st_cluster_f4(mapa_shared(smem_u32(slots + g.rank * G::W + g.warp), g.lane), o);
-            cluster_sync();
+            for (int i = g.warp; i < warps; i += G::W) {
+                const uint32_t v = __float_as_uint(slots[i].w);
+                unsigned int n = 0;
+                for (int q = g.lane; q < warps; q += 32) {
+                    const uint32_t o = __float_as_uint(slots[q].w);
+                    n += o > v || (o == v && q < i);
+                }
+                if (__reduce_add_sync(~0u, n) == before && g.lane == 0) top.bound = v;
+            }
+            __syncthreads();
+            bound = top.bound;
         }
-        a = acc_none();
-        for (int i = g.lane; i < G::W * P.parts; i += 32) {
-            const float4 s = slots[i];
-            a = acc_merge(a, Acc{s.x, s.y, s.z}, P.c2);
-        }
-        a = acc_warp(a, P.c2);
-    }
-    const float m = a.m, m0 = m == NEG_INF ? 0.f : m;
-    const float logs = m == NEG_INF ? 0.f : logf(a.s);
-    const float H = m == NEG_INF ? 0.f : logs - LN2 * (a.t / a.s);
-    if (g.rank == 0 && g.tid == 0) {
-        if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
-        if (P.entropy) P.entropy[g.row] = H;
-        if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
-    }
-    if (bounded) {
-        // the k-th largest value: the one with k - 1 before it
-        for (int i = g.warp; i < values; i += G::W) {
-            const uint32_t v = top.value[i];
-            unsigned int before = 0;
-            for (int q = g.lane; q < values; q += 32) before += top.value[q] > v || (top.value[q] == v && q < i);
-            if (__reduce_add_sync(~0u, before) == P.k - 1u && g.lane == 0) top.bound = v;
-        }
-        __syncthreads();
-        const uint32_t bound = top.bound;
-        const uint32_t count_at = cluster ? mapa_shared(smem_u32(&top.count), 0) : smem_u32(&top.count);
-        const uint32_t key_at = cluster ? mapa_shared(smem_u32(top.key), 0) : smem_u32(top.key);
+        // a bound of -inf: what lies above it here; the first of the -inf tokens follow below
+        const float limit = bound <= value_key(NEG_INF) ? Elem<T>::LOWEST : key_value(bound);
+        const int share = CAND_MAX / g.parts;
+        const uint32_t list = cluster ? mapa_shared(smem_u32(top.id + g.rank * share), 0) : smem_u32(top.id);
+        const auto take = [&](int id) {
+            const int at = atomicAdd(&top.local, 1u);
+            if (at < share) {
+                if (cluster) st_shared_cluster_u32(list + 4 * at, id);
+                else top.id[at] = id;
+            }
+        };
         if (mine >= bound) {
-            const float limit = key_value(bound);
             for (int t = part.tiles - 1; t >= 0; --t) {
                 if (t < part.tiles - 1) part.load(row, g, t, d);
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    float x[E];
-                    Elem<T>::unpack(d[j], x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int id = row.first(part.at(g, t, j)) + e;
-                        // not below: a NaN is a candidate too
-                        if (!(x[e] < limit) && part.at(g, t, j) < part.end && id >= 0 && id < row.vocab) {
-                            const uint32_t at = cluster ? add_cluster_u32(count_at, 1) : atomicAdd(&top.count, 1u);
-                            if (at < CAND_MAX) {
-                                if (cluster) st_cluster_u64(key_at + 8 * at, token_key(x[e], id));
-                                else top.key[at] = token_key(x[e], id);
-                            }
-                        }
-                    }
+                unsigned long long bits = Elem<T>::reach(d, limit);
+                while (bits) {
+                    const int b = Elem<T>::place(__ffsll(bits) - 1);
+                    bits &= bits - 1;
+                    take(row.head + (part.at(g, t) + b / E * GT) * E + b % E);
                 }
             }
         }
-        if (cluster) cluster_sync();
-        else __syncthreads();
-    }
-    if (g.rank != 0) return;
-    if (!bounded || top.count > CAND_MAX) top_radix(row, P.k, g, top);
-    const unsigned int count = top.count;
-    for (unsigned int i = g.warp; i < count; i += G::W) {
-        const unsigned long long key = top.key[i];
-        unsigned int before = 0;
-        for (unsigned int q = g.lane; q < count; q += 32) before += top.key[q] > key;
-        before = __reduce_add_sync(~0u, before);
-        if (before < P.k && g.lane == 0) {
-            P.top_ids[g.row * P.k + before] = 0xffffffffu - static_cast<uint32_t>(key);
-            P.top_logp[g.row * P.k + before] = (key_value(static_cast<uint32_t>(key >> 32)) - m0) * P.c - logs;
+        if (edge && !(xe < limit)) take(row.edge(g.lane));
+        __syncthreads();
+        if (cluster) {
+            if (g.tid == 0) st_shared_cluster_u32(mapa_shared(smem_u32(top.counts + g.rank), 0), top.local);
+            cluster_sync();
+        } else {
+            if (g.tid == 0) top.counts[0] = top.local;
+            __syncthreads();
         }
+        if (g.rank != 0) return;
+        bool over = false;
+        unsigned int count = 0;
+        for (int r = 0; r < g.parts; ++r) {
+            const unsigned int n = top.counts[r];
+            over = over || n > static_cast<unsigned int>(share);
+            if (!over) {
+                for (unsigned int i = g.tid; i < n; i += GT) {
+                    const int id = top.id[r * share + i];
+                    if (count + i < CAND_MAX) top.key[count + i] = token_key(Elem<T>::get(row.p + id), id);
+                }
+            }
+            count += n;
+        }
+        if (!over && count < static_cast<unsigned int>(P.k)) {
+            // fewer than k tokens above -inf: the lowest ids of the others follow,
+            // all of them among the first k + count ids
+            __syncthreads();
+            if (g.warp == 0) {
+                unsigned int n = count;
+                for (int id = g.lane; n < static_cast<unsigned int>(P.k); id += 32) {
+                    const bool none = id < P.vocab && Elem<T>::get(row.p + id) == NEG_INF;
+                    const unsigned int set = __ballot_sync(~0u, none);
+                    const unsigned int at = n + __popc(set & ((1u << g.lane) - 1));
+                    if (none && at < CAND_MAX) top.key[at] = token_key(NEG_INF, id);
+                    n += __popc(set);
+                }
+                if (g.lane == 0) top.count = min(n, static_cast<unsigned int>(CAND_MAX));
+            }
+        } else if (g.tid == 0) {
+            top.count = over ? CAND_MAX + 1 : count;
+        }
+    } else {
+        exchange(a, 0.f, g, slots);
+        if (g.rank != 0) return;
+        if (g.tid == 0) top.count = CAND_MAX + 1;
+    }
+    if (g.warp == 0) {
+        a = acc_slots<GT, ENT>(slots, warps, g, P.c2);
+        const float m = a.m, m0 = m == NEG_INF ? 0.f : m, logs = m == NEG_INF ? 0.f : logf(a.s);
+        if (g.lane == 0) {
+            const float H = ENT && m != NEG_INF ? logs - LN2 * (a.t / a.s) : 0.f;
+            if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
+            if (ENT && P.entropy) P.entropy[g.row] = H;
+            if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
+            top.m0 = m0;
+            top.logs = logs;
+        }
+    }
+    __syncthreads();
+    if (top.count > CAND_MAX) top_radix<T, GT>(row.p, P.vocab, P.k, top);
+    const int count = top.count;
+    const float m0 = top.m0, logs = top.logs;
+    const auto give = [&](unsigned long long key, int rank) {
+        P.top_ids[g.row * P.k + rank] = 0xffffffffu - static_cast<uint32_t>(key);
+        P.top_logp[g.row * P.k + rank] = (key_value(static_cast<uint32_t>(key >> 32)) - m0) * P.c - logs;
+    };
+    if (count <= 32) {
+        if (g.warp == 0) {
+            unsigned long long key[1] = {g.lane < count ? top.key[g.lane] : 0ull};
+            sort_warp(key, g.lane);
+            if (g.lane < P.k) give(key[0], g.lane);
+        }
+    } else if (count <= 128) {
+        if (g.warp == 0) {
+            unsigned long long key[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) key[r] = r * 32 + g.lane < count ? top.key[r * 32 + g.lane] : 0ull;
+            sort_warp(key, g.lane);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r * 32 + g.lane < P.k) give(key[r], r * 32 + g.lane);
+        }
+    } else {
+        const int n = 1 << (32 - __clz(count - 1));
+        for (int i = count + g.tid; i < n; i += GT) top.key[i] = 0;
+        sort_block<GT>(top.key, n);
+        for (int i = g.tid; i < P.k; i += GT) give(top.key[i], i);
     }
 }
 
@@ -744,191 +907,242 @@ __device__ __forceinline__ float excess(float r)
     return r + expm1f(-r);
 }
 
-// A teacher's list, taken in by one warp of each CTA of the row.
+// A teacher's list, taken in by every CTA of the row: entry i by thread i mod GT.
+template <int GT>
 struct ListShared {
-    int id[VOCAB_MAX_K];
-    float logq[VOCAB_MAX_K], q[VOCAB_MAX_K], x[VOCAB_MAX_K];   // x: the student's logit
-    float m, s, Q;                                             // the student's statistics on the list, sum of q
+    int id[VOCAB_MAX_K];                    // -1: no token
+    float u[VOCAB_MAX_K], x[VOCAB_MAX_K];   // the teacher's exponent, the student's logit
+    float4 part[Group<GT>::W];              // per warp: maximum and sum of the student's, of the teacher's
+    float sum[Group<GT>::W];
+    unsigned int edges;                     // bits of the row's edge elements that are on the list
 };
 
-// Bans the elements of a tile that are on the list: one word of bits per
-// thread, a bit per element it holds, set by the warp that has the list.
-template <class T, int GT>
-__device__ __forceinline__ void ban_listed(const Row<T>& row, const Part<T, GT>& part, const Group<GT>& g, int tile, int k,
-                                           const ListShared& list, unsigned long long* bits, uint4 (&d)[NV])
-{
-    constexpr int E = Elem<T>::E;
-    bits[g.tid] = 0;
-    g.sync();
-    if (g.warp == 0) {
-        for (int i = g.lane; i < k; i += 32) {
-            const int at = list.id[i] + row.off, v = at / E - part.begin - tile * Group<GT>::TILE;
-            if (list.id[i] >= 0 && v >= 0 && v < Group<GT>::TILE && at / E < part.end)
-                atomicOr(bits + v % GT, 1ull << (v / GT * E + at % E));
-        }
-    }
-    g.sync();
-    const unsigned long long mine = bits[g.tid];
-    if (mine) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) Elem<T>::ban(d[j], static_cast<uint32_t>(mine >> (j * E)));
-    }
-}
+template <class T>
+using Bits = typename Elem<T>::Bits;        // a bit per element of a tile that a thread holds
 
+// PASS: the forward, forward and backward, or the backward from saved statistics.
 template <class T, int PASS, int GT>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_distill_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
     using G = Group<GT>;
-    __shared__ float4 slots[GT == 32 ? 1 : CLUSTER_MAX * G::W];
-    __shared__ unsigned long long bits[G::THREADS];
-    __shared__ ListShared lists[G::ROWS];
-    const G g(P.parts);
+    extern __shared__ unsigned long long listed_raw[];   // forward: a word of bits per thread and tile
+    __shared__ float4 slots[GT == 32 || PASS == VOCAB_BWD ? 1 : CLUSTER_MAX * G::W];
+    __shared__ ListShared<GT> lists[G::ROWS];
+    const G g;
     if (GT == 32 && g.row >= P.n) return;
-    const int parts = GT == 32 ? 1 : P.parts;
-    const bool cluster = GT != 32 && parts > 1;
+    const bool cluster = g.parts > 1;
     if (cluster) cluster_arrive();
     const Row<T> row(static_cast<const T*>(P.logits) + g.row * P.ld, P.vocab);
-    const Part<T, GT> part(row, g, parts);
-    ListShared& list = lists[g.slot];
+    const Part<T, GT> part(row, g, P.each);
+    ListShared<GT>& list = lists[g.slot];
+    // the list's loads are under way before the row's
+    const float shift = P.rest && P.t_lse ? P.t_lse[g.row] : 0.f;
+    const long long t0 = g.tid < P.k ? P.t_ids[g.row * P.k + g.tid] : -1;
+    const float u0 = g.tid < P.k ? P.t_vals[g.row * P.k + g.tid] : 0.f;
     uint4 d[NV];
     part.load(row, g, 0, d);
-    float m = 0.f, logs = 0.f, mr = 0.f, logr = 0.f;
+    const bool edge = g.has_edges() && g.lane < row.edges();
+    const int edge_id = edge ? row.edge(g.lane) : -1;
+    float xe = edge ? Elem<T>::get(row.p + edge_id) : NEG_INF;
+    const float w = PASS != VOCAB_FWD ? P.dloss[g.row] : 0.f;
+    float m = 0.f, logs = 0.f, mr = 0.f, logr = 0.f, s, sr;
     if (PASS == VOCAB_BWD) {
         const float4 st = reinterpret_cast<const float4*>(P.stats)[g.row];
         m = st.x, logs = st.y, mr = st.z, logr = st.w;
+        s = expf(logs), sr = expf(logr);
     }
-    const float w = PASS != VOCAB_FWD ? P.dloss[g.row] : 0.f;
-    if (g.warp == 0) {
-        const float shift = P.rest && P.t_lse ? P.t_lse[g.row] : 0.f;
-        float um = NEG_INF, xm = NEG_INF;
-        for (int i = g.lane; i < P.k; i += 32) {
-            const long long t = P.t_ids[g.row * P.k + i];
-            const bool there = t >= 0 && t < P.vocab;
-            const float u = there ? P.t_vals[g.row * P.k + i] * P.t_c - shift : NEG_INF;
-            const float x = there ? Elem<T>::get(row.p + t) : NEG_INF;
-            list.id[i] = there ? static_cast<int>(t) : -1;
-            list.logq[i] = u;
-            list.x[i] = x;
-            um = max_nan(um, u);
-            xm = max_nan(xm, x);
-        }
-        um = max_nan_warp(um);
-        xm = max_nan_warp(xm);
-        float logu = 0.f;
-        if (!P.rest && um != NEG_INF) {
-            float us = 0.f;
-            for (int i = g.lane; i < P.k; i += 32) us += expf(list.logq[i] - um);
-            logu = logf(sum_warp(us));
-        }
-        float Q = 0.f, xs = 0.f;
-        for (int i = g.lane; i < P.k; i += 32) {
-            const float lq = P.rest ? list.logq[i] : (list.logq[i] - (um == NEG_INF ? 0.f : um)) - logu;
-            const float q = list.id[i] >= 0 ? expf(lq) : 0.f;
-            list.logq[i] = lq;
-            list.q[i] = q;
-            Q += q;
-            if (xm != NEG_INF) xs += ex2((list.x[i] - xm) * P.c2);
-        }
-        Q = sum_warp(Q);
-        xs = sum_warp(xs);
-        if (g.lane == 0) {
-            list.m = xm;
-            list.s = xs;
-            list.Q = Q;
-        }
+    Bits<T>* listed = reinterpret_cast<Bits<T>*>(listed_raw) + g.slot * GT;
+    if (PASS != VOCAB_BWD) {
+        for (int t = 0; t < part.tiles; ++t) listed[t * GT + g.tid] = 0;
+        if (g.tid == 0) list.edges = 0;
+        G::sync();
     }
-    float pl;   // the student's probability of the list
+    for (int i = g.tid; i < P.k; i += GT) {
+        const long long t = i == g.tid ? t0 : P.t_ids[g.row * P.k + i];
+        const bool there = t >= 0 && t < P.vocab;
+        const int id = there ? static_cast<int>(t) : -1;
+        if (PASS != VOCAB_BWD && there) {
+            const int at = id - row.head, v = at / E - part.begin, tile = v / G::TILE;
+            if (at < 0 || at >= row.full * E)
+                atomicOr(&list.edges, 1u << (at < 0 ? id : row.head + at - row.full * E));
+            else if (v >= 0 && part.begin + v < part.end)
+                atomicOr(listed + tile * GT + v % GT, static_cast<Bits<T>>(1) << (v % G::TILE / GT * E + at % E));
+        }
+        list.id[i] = id;
+        list.u[i] = there ? (i == g.tid ? u0 : P.t_vals[g.row * P.k + i]) * P.t_c - shift : NEG_INF;
+        list.x[i] = there ? Elem<T>::get(row.p + id) : NEG_INF;
+    }
+    if (PASS != VOCAB_BWD) {
+        G::sync();
+        if (edge && list.edges >> g.lane & 1) xe = NEG_INF;
+    }
+    // the list's statistics, a share per warp
+    {
+        float xm = NEG_INF, um = NEG_INF, xs = 0.f, us = 0.f;
+        if (g.warp * 32 < P.k) {
+            for (int i = g.tid; i < P.k; i += GT) {
+                xm = max_nan(xm, list.x[i]);
+                um = max_nan(um, list.u[i]);
+            }
+            xm = max_nan_warp(xm);
+            um = P.rest ? 0.f : max_nan_warp(um);
+            for (int i = g.tid; i < P.k; i += GT) {
+                if (list.id[i] < 0) continue;
+                if (xm != NEG_INF) xs += ex2((list.x[i] - xm) * P.c2);
+                if (um != NEG_INF) us += expf(list.u[i] - um);
+            }
+            xs = sum_warp(xs);
+            us = sum_warp(us);
+        }
+        if (g.lane == 0) list.part[g.warp] = make_float4(xm, xs, um, us);
+    }
+    Acc r = acc_none();
     if (PASS == VOCAB_BWD) {
         // in place: the list's logits are read before any CTA of the row stores
         if (cluster) {
             cluster_wait();
             cluster_sync();
         } else {
-            g.sync();
+            G::sync();
         }
-        pl = list.m == NEG_INF ? 0.f : list.s * ex2(((list.m - m) * P.c - logs) * LOG2E);
     } else {
         Acc a = acc_none();
         for (int t = 0; t < part.tiles; ++t) {
             if (t > 0) part.load(row, g, t, d);
-            ban_listed(row, part, g, t, P.k, list, bits + g.slot * GT, d);
-            const float mt = Elem<T>::max_of(d);
-            const Acc b = acc_tile<T, false>(d, mt, P.c2);
-            a = t > 0 ? acc_merge(a, b, P.c2) : b;
+            const Bits<T> mine = listed[t * GT + g.tid];
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) Elem<T>::ban(d[j], static_cast<uint32_t>(mine >> (j * E)));
+            }
+            const Acc b = acc_tile<T, false>(d, Elem<T>::max_of(d), P.c2);
+            a = t > 0 ? acc_merge<false>(a, b, P.c2) : b;
         }
-        const Acc r = acc_row(a, P.c2, g, parts, slots);
-        const Acc l{list.m, list.s, 0.f};
-        a = acc_merge(l, r, P.c2);
-        m = a.m, mr = r.m;
-        logs = m == NEG_INF ? 0.f : logf(a.s);
-        logr = mr == NEG_INF ? 0.f : logf(r.s);
-        pl = acc_to(l, m, P.c2).s / a.s;
+        if (g.has_edges() && row.edges() > 0) a = acc_merge<false>(a, acc_one(xe), P.c2);
+        r = acc_warp<false>(a, P.c2);
+        if (GT == 32) {
+            G::sync();
+        } else {
+            exchange(r, 0.f, g, slots);
+            if (PASS == VOCAB_FWD && (g.rank != 0 || g.warp * 32 >= P.k)) {
+                if (g.rank != 0) return;
+                list.sum[g.warp] = 0.f;
+                __syncthreads();
+                return;
+            }
+            r = acc_slots<GT, false>(slots, G::W * g.parts, g, P.c2);
+        }
+        mr = r.m, sr = r.s;
     }
-    const float m0 = m == NEG_INF ? 0.f : m, mr0 = mr == NEG_INF ? 0.f : mr;
-    const float logpr = (mr - m0) * P.c + logr - logs;
-    const float Q = list.Q, qr = P.rest && mr != NEG_INF ? fmaxf(1.f - Q, 0.f) : 0.f;
+    // the list's statistics over its warps: the student's, the teacher's
+    Acc l = acc_none();
+    float um = NEG_INF, us = 0.f;
+    if (g.lane < G::W && g.lane * 32 < P.k) {
+        const float4 o = list.part[g.lane];
+        l = Acc{o.x, o.y, 0.f};
+        um = o.z, us = o.w;
+    }
+    l = acc_warp<false>(l, P.c2);
+    const float uml = max_nan_warp(um);
+    us = sum_warp(us == 0.f ? 0.f : us * expf(um - uml));
+    um = uml;
+    if (PASS != VOCAB_BWD) {
+        const Acc a = acc_merge<false>(l, r, P.c2);
+        m = a.m, s = a.s;
+        logs = m == NEG_INF ? 0.f : logf(s);
+        logr = mr == NEG_INF ? 0.f : logf(sr);
+    }
+    const float m0 = m == NEG_INF ? 0.f : m;
+    // teacher: q_k = exp(u_k - um) uq; Q = sum q; rest: an entry of its own where q_R > 0
+    const float uq = P.rest ? 1.f : 1.f / us, u_log = P.rest ? 0.f : us == 0.f ? 0.f : um + logf(us);
+    const float Q = P.rest ? us : us == 0.f ? 0.f : us * uq;
+    const float qr = P.rest && mr != NEG_INF ? fmaxf(1.f - Q, 0.f) : 0.f;
     const bool entry = qr > 0.f;
-    const float whole = entry ? 1.f : Q;
-    if (PASS != VOCAB_BWD && g.rank == 0 && g.warp == 0) {
-        float kl = 0.f;
-        for (int i = g.lane; i < P.k; i += 32) {
+    const float pl = acc_to<false>(l, m, P.c2).s / s;   // the student's probability of the list
+    const float logpr = (mr - m0) * P.c + logr - logs;
+    const float wt = w * P.temperature;
+    const bool live = w != 0.f && m != NEG_INF;
+    // loss, and the list's gradients (stored over the row's below)
+    float kl = 0.f;
+    if (g.warp * 32 < P.k) {
+        for (int i = g.tid; i < P.k; i += GT) {
             if (list.id[i] < 0) continue;
-            const float q = list.q[i], logp = (list.x[i] - m0) * P.c - logs, r = list.logq[i] - logp;
-            if (entry) kl += q > 0.f ? q * excess(r) : expf(logp);
-            else kl += q > 0.f ? q * r : 0.f * q;
+            const float logq = list.u[i] - u_log, q = P.rest ? expf(logq) : us == 0.f ? 0.f : expf(list.u[i] - um) * uq;
+            const float logp = (list.x[i] - m0) * P.c - logs, p = expf(logp);
+            if (PASS != VOCAB_BWD) {
+                if (entry) kl += q > 0.f ? q * excess(logq - logp) : p;
+                else kl += q > 0.f ? q * (logq - logp) : 0.f * q;
+            }
+            if (PASS != VOCAB_FWD) list.u[i] = wt * ((entry ? 1.f : Q) * p - q);
         }
-        kl = sum_warp(kl);
-        if (entry) kl += qr * excess(log1pf(-Q) - logpr);
-        if (g.lane == 0) {
-            P.loss[g.row] = P.temperature * P.temperature * kl;
-            if (PASS == VOCAB_FWD && P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, mr, logr);
+        if (PASS != VOCAB_BWD) {
+            kl = sum_warp(kl);
+            if (g.lane == 0) list.sum[g.warp] = kl;
         }
     }
     if constexpr (PASS != VOCAB_FWD) {
         T* out = static_cast<T*>(P.dlogits) + g.row * P.ld_d;
+        uint4* vout = reinterpret_cast<uint4*>(out + row.head);
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
-        const float wt = w * P.temperature;
-        const bool live = w != 0.f && m != NEG_INF;
         const bool near = fabsf(mr * P.c2) < NEAR;
-        const Base base(mr0, P.c2);
-        const float rate = wt * (entry ? Q - pl : Q * expf(logpr));
-        const float A = mr == NEG_INF ? 0.f : rate * ex2(-base.delta - logr * LOG2E);
-        const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A);
+        const Base base(mr, P.c2);
+        const float rate = mr == NEG_INF ? 0.f : wt * (entry ? Q - pl : Q * expf(logpr)) / sr;
+        const float A = rate * ex2(-base.delta);
+        const auto one = [&](float x) -> float {
+            if (!live || mr == NEG_INF) return 0.f;
+            return rate * ex2((x - mr) * P.c2);
+        };
         for (int t = part.tiles - 1; t >= 0; --t) {
-            if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
+            const int first = part.at(g, t), left = part.left(g, t);
+            if (live && near && same) {
+                if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
+                const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const int v = part.at(g, t, j);
-                if (v >= part.end) break;
-                float x[E];
-                Elem<T>::unpack(d[j], x);
-                if (!live) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = 0.f;
-                } else if (near) {
+                for (int j = 0; j < NV; ++j) {
+                    float x[E];
+                    Elem<T>::unpack(d[j], x);
 #pragma unroll
                     for (int e = 0; e < E; e += 2) {
                         float y0, y1;
                         split(fma2(pair(x[e], x[e + 1]), cc, nb), y0, y1);
                         split(mul2(pair(ex2(y0), ex2(y1)), A2), x[e], x[e + 1]);
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = mr == NEG_INF ? 0.f : rate * ex2(((x[e] - mr0) * P.c - logr) * LOG2E);
+                    if (left > j * GT) vout[first + j * GT] = Elem<T>::pack(x);
                 }
-                row.store(out, same, v, x);
+            } else {
+#pragma unroll 1
+                for (int j = 0; j * GT < left && j < NV; ++j) {
+                    float x[E] = {};
+                    if (live) Elem<T>::unpack(row.vec()[first + j * GT], x);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = one(x[e]);
+                    if (same) {
+                        vout[first + j * GT] = Elem<T>::pack(x);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) Elem<T>::put(out + row.head + (first + j * GT) * E + e, x[e]);
+                    }
+                }
             }
         }
-        g.sync();
-        if (g.warp == 0 && live) {
-            for (int i = g.lane; i < P.k; i += 32) {
-                const int id = list.id[i], v = (id + row.off) / E;
-                if (id < 0 || v < part.begin || v >= part.end) continue;
-                const float p = expf((list.x[i] - m0) * P.c - logs);
-                Elem<T>::put(out + id, wt * (whole * p - list.q[i]));
-            }
+        if (edge) Elem<T>::put(out + edge_id, one(xe));
+        G::sync();
+        for (int i = g.tid; live && i < P.k; i += GT) {
+            const int id = list.id[i];
+            if (id < 0) continue;
+            const int at = id - row.head, v = at / E;
+            const bool vector = at >= 0 && v < row.full;
+            if (vector ? v >= part.begin && v < part.end : g.rank == 0) Elem<T>::put(out + id, list.u[i]);
         }
+    } else {
+        G::sync();
+    }
+    if (PASS != VOCAB_BWD && g.rank == 0 && g.tid == 0) {
+        kl = 0.f;
+        for (int i = 0; i < G::W && i * 32 < P.k; ++i) kl += list.sum[i];
+        if (entry) kl += qr * excess(log1pf(-Q) - logpr);
+        P.loss[g.row] = P.temperature * P.temperature * kl;
+        if (PASS == VOCAB_FWD && P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, mr, logr);
     }
 }
 #endif
