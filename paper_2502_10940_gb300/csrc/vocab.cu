@@ -13,19 +13,34 @@ struct Plan {
     int threads, parts;
 };
 
+#ifndef VOCAB_FWD_GT
+#define VOCAB_FWD_GT 256
+#endif
+#ifndef VOCAB_STEP_GT
+#define VOCAB_STEP_GT 256
+#endif
+#ifndef VOCAB_HOLD_KB
+#define VOCAB_HOLD_KB 256
+#endif
+
 // A warp or four warps where their registers hold the row (NV vectors a
-// thread), else sixteen.  A step writes the row that it has read: it takes as
-// many CTAs as hold it in registers, up to a portable cluster's eight; the other
-// passes read tile after tile.  All take more CTAs where there are fewer rows
-// than CTAs that the device runs at once (two per SM), down to a vector per thread.
-Plan plan(const VocabParams& p, int e, int pass, int least, int sms)
+// thread).  Longer rows: a forward reads tile after tile with eight warps, so
+// that the ends of several rows overlap on an SM; a step, which writes what it
+// has read, takes sixteen warps and as many CTAs as hold the row in
+// registers, up to a portable cluster's eight; a backward a CTA per tile.  All
+// take more CTAs where there are fewer rows than the device runs CTAs at once,
+// down to a vector per thread.
+Plan plan(const VocabParams& p, int e, int pass, bool split, int least, int sms)
 {
     const int nvec = (p.vocab + e - 1) / e;
     if (least <= 32 && nvec <= 32 * NV) return {32, 1};
     if (least <= 128 && nvec <= 128 * NV) return {128, 1};
-    const int hold = pass == VOCAB_STEP ? (nvec + 512 * NV - 1) / (512 * NV) : 1;
-    const int fill = static_cast<int>(std::min<long long>(2ll * sms / p.n, nvec / 512));
-    return {512, std::min(CLUSTER_MAX, std::max({1, hold, fill}))};
+    const int threads = least > 256 ? 512 : pass == VOCAB_FWD ? VOCAB_FWD_GT : pass == VOCAB_STEP ? VOCAB_STEP_GT : 512;
+    const int hold = pass == VOCAB_STEP ? (nvec * 16 <= VOCAB_HOLD_KB * 1024 ? 1 : (nvec + 512 * NV - 1) / (512 * NV))
+                     : split            ? (nvec + 512 * NV - 1) / (512 * NV)
+                                        : 1;
+    const int fill = static_cast<int>(std::min<long long>(1024ll / threads * sms / p.n, nvec / threads));
+    return {threads, std::min(CLUSTER_MAX, std::max({1, hold, fill}))};
 }
 
 template <class K>
@@ -53,9 +68,12 @@ template <class T, bool ENT>
 cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    const Plan s = plan(p, E, VOCAB_FWD, p.k <= 64 ? 128 : 512, sms);
-    return s.threads == 128 ? launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, stream)
-                            : launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, stream);
+    const Plan s = plan(p, E, VOCAB_FWD, false, p.k <= 64 ? 128 : 512, sms);
+    switch (s.threads) {
+    case 128: return launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, stream);
+    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT>, p, E, s, true, 0, stream);
+    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, stream);
+    }
 }
 
 template <class T, int PASS, bool ENT>
@@ -63,11 +81,12 @@ cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    const Plan s = plan(p, E, PASS, 32, sms);
+    constexpr int GT = PASS == VOCAB_FWD ? VOCAB_FWD_GT : PASS == VOCAB_STEP ? VOCAB_STEP_GT : 512;
+    const Plan s = plan(p, E, PASS, !cluster, 32, sms);
     switch (s.threads) {
     case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, stream);
     case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, stream);
-    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT>, p, E, s, cluster, 0, stream);
+    default: return launch_rows(token_logprob_kernel<T, PASS, GT, ENT>, p, E, s, cluster, 0, stream);
     }
 }
 
@@ -114,11 +133,12 @@ cudaError_t distill_rows(VocabParams& p, const Plan& s, cudaStream_t stream)
 template <class T, int PASS>
 cudaError_t distill(VocabParams p, int sms, cudaStream_t stream)
 {
-    const Plan s = plan(p, Elem<T>::E, PASS, 32, sms);
+    constexpr int GT = PASS == VOCAB_FWD ? VOCAB_FWD_GT : PASS == VOCAB_STEP ? VOCAB_STEP_GT : 512;
+    const Plan s = plan(p, Elem<T>::E, PASS, false, 32, sms);
     switch (s.threads) {
     case 32: return distill_rows<T, PASS, 32>(p, s, stream);
     case 128: return distill_rows<T, PASS, 128>(p, s, stream);
-    default: return distill_rows<T, PASS, 512>(p, s, stream);
+    default: return distill_rows<T, PASS, GT>(p, s, stream);
     }
 }
 

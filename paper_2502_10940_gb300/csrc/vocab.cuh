@@ -484,11 +484,10 @@ __device__ __forceinline__ unsigned long long token_key(float x, int j)
 // The candidates of a row's top k, in the first of its CTAs.
 struct TopShared {
     unsigned long long key[CAND_MAX];
-    int id[CAND_MAX];                   // a share of it for each CTA of the row
+    unsigned long long found[CAND_MAX];   // a cluster's: a share for each CTA of the row
     unsigned int hist[256];
     unsigned int counts[CLUSTER_MAX];
     unsigned int count, digit, above, bound, local;
-    float m0, logs;
 };
 
 // Gathers at least k and at most CAND_MAX keys of a row in memory, the k
@@ -527,40 +526,6 @@ __device__ __noinline__ void top_radix(const T* p, int vocab, unsigned int k, To
         if (key >= bound) sh.key[atomicAdd(&sh.count, 1u)] = key;
     }
     __syncthreads();
-}
-
-// Sorts key[0 .. count), padded to R x 32 with zeros (below every key), falling,
-// in one warp: element r 32 + lane in register r.
-template <int R>
-__device__ __forceinline__ void sort_warp(unsigned long long (&key)[R], int lane)
-{
-#pragma unroll
-    for (int size = 2; size <= 32 * R; size *= 2) {
-#pragma unroll
-        for (int step = size / 2; step; step /= 2) {
-            if (step >= 32) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int o = r ^ step / 32;
-                    if (o > r) {
-                        const bool falling = (r * 32 & size) == 0;
-                        const unsigned long long a = key[r], b = key[o];
-                        const bool swap = falling ? a < b : a > b;
-                        key[r] = swap ? b : a;
-                        key[o] = swap ? a : b;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const unsigned long long o = __shfl_xor_sync(~0u, key[r], step);
-                    const int i = r * 32 + lane;
-                    const bool larger = ((i & size) == 0) == ((i & step) == 0);   // this lane keeps the larger
-                    key[r] = (key[r] > o) == larger ? key[r] : o;
-                }
-            }
-        }
-    }
 }
 
 // Sorts key[0 .. n), n a power of two, falling, by the whole CTA.
@@ -709,13 +674,15 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     }
 }
 
-// The forward with the k most likely tokens.  Each warp gives, with its
-// statistics, the `each`-th largest of its threads' maxima; at least k tokens
-// reach the ceil(k / each)-th largest of those, and few more than k do where the
-// largest are spread over the threads (`each` a little above k over the number of
-// warps: 105 at k = 64 of 32000 in random order, where each = k / warps gives
-// 170 and larger ones more barriers' worth of work).  These are gathered, by
-// their bits, from the registers, and sorted in one warp.
+// The forward with the k most likely tokens.  At least k tokens reach the k-th
+// largest of the threads' maxima, and few more than k do where the largest are
+// spread over the threads (74 at k = 64 of 32000 in random order, 256 threads).
+// In a cluster, whose threads are too many and too far apart for that, each warp
+// gives with its statistics the `each`-th largest of its threads' maxima, and at
+// least k tokens reach the ceil(k / each)-th largest of those.  The tokens that
+// reach the bound are gathered, by their bits, from the registers (or, of a tile
+// before the last, read again), and each takes as its place the number of
+// candidates before it.
 template <class T, int GT, bool ENT>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_top_kernel(const VocabParams P)
 {
@@ -742,36 +709,42 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     for (int t = 0; t < part.tiles; ++t) {
         if (t > 0) part.load(row, g, t, d);
         const Acc b = acc_tile<T, ENT>(d, Elem<T>::max_of(d), P.c2);
-        // (acc_tile gives acc_none for a tile of nothing but -inf)
         a = t > 0 ? acc_merge<ENT>(a, b, P.c2) : b;
     }
     if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
     const uint32_t mine = value_key(a.m);   // of this thread
     a = acc_warp<ENT>(a, P.c2);
     const int warps = G::W * g.parts;
-    // one and a half times k over the warps, one where there are as many warps
+    // a cluster: of each warp, a little more of its largest than k over the warps
     const int each = P.k <= warps ? 1 : (3 * P.k + 2 * warps - 1) / (2 * warps);
-    const bool bounded = each <= 24;
-    if (bounded) {
-        uint32_t left = mine, best = 0;
+    const bool bounded = cluster ? each <= 24 : P.k <= GT;
+    uint32_t best = 0;
+    if (cluster && bounded) {
+        uint32_t left = mine;
         for (int i = 0; i < each; ++i) {
             best = __reduce_max_sync(~0u, left);
             if (g.lane == __ffs(__ballot_sync(~0u, left == best)) - 1) left = 0;
         }
-        exchange(a, __uint_as_float(best), g, slots);
-        // the value with `before` = ceil(k / each) - 1 before it
-        const unsigned int before = (P.k + each - 1) / each - 1;
-        uint32_t bound;
-        if (!cluster) {   // at most 16 values: every warp for itself
-            const uint32_t v = g.lane < G::W ? __float_as_uint(slots[g.lane].w) : 0u;
-            unsigned int n = 0;
-#pragma unroll
-            for (int i = 0; i < G::W; ++i) {
-                const uint32_t o = __shfl_sync(~0u, v, i);
-                n += o > v || (o == v && i < g.lane);
-            }
-            bound = __shfl_sync(~0u, v, __ffs(__ballot_sync(~0u, n == before)) - 1);
+    }
+    exchange(a, __uint_as_float(best), g, slots);
+    a = acc_slots<GT, ENT>(slots, warps, g, P.c2);
+    const float m = a.m, m0 = m == NEG_INF ? 0.f : m, logs = m == NEG_INF ? 0.f : logf(a.s);
+    if (g.rank == 0 && g.tid == 0) {
+        const float H = ENT && m != NEG_INF ? logs - LN2 * (a.t / a.s) : 0.f;
+        if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
+        if (ENT && P.entropy) P.entropy[g.row] = H;
+        if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
+    }
+    unsigned int count = CAND_MAX + 1;
+    if (bounded) {
+        uint32_t bound = 0;
+        if (!cluster) {
+            // the k-th largest of the threads' maxima, from above to its upper 16 bits
+            for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
+                if (__syncthreads_count(mine >= (bound | bit)) >= P.k) bound |= bit;
         } else {
+            // the warps' value with `before` = ceil(k / each) - 1 before it
+            const unsigned int before = (P.k + each - 1) / each - 1;
             for (int i = g.warp; i < warps; i += G::W) {
                 const uint32_t v = __float_as_uint(slots[i].w);
                 unsigned int n = 0;
@@ -786,13 +759,13 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         }
         // a bound of -inf: what lies above it here; the first of the -inf tokens follow below
         const float limit = bound <= value_key(NEG_INF) ? Elem<T>::LOWEST : key_value(bound);
-        const int share = CAND_MAX / g.parts;
-        const uint32_t list = cluster ? mapa_shared(smem_u32(top.id + g.rank * share), 0) : smem_u32(top.id);
-        const auto take = [&](int id) {
-            const int at = atomicAdd(&top.local, 1u);
+        const unsigned int share = cluster ? CAND_MAX / g.parts : CAND_MAX;
+        const uint32_t list = cluster ? mapa_shared(smem_u32(top.found + g.rank * share), 0) : 0;
+        const auto take = [&](int id, float x) {
+            const unsigned int at = atomicAdd(&top.local, 1u);
             if (at < share) {
-                if (cluster) st_shared_cluster_u32(list + 4 * at, id);
-                else top.id[at] = id;
+                if (cluster) st_cluster_u64(list + 8 * at, token_key(x, id));
+                else top.key[at] = token_key(x, id);
             }
         };
         if (mine >= bound) {
@@ -802,34 +775,28 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
                 while (bits) {
                     const int b = Elem<T>::place(__ffsll(bits) - 1);
                     bits &= bits - 1;
-                    take(row.head + (part.at(g, t) + b / E * GT) * E + b % E);
+                    const int id = row.head + (part.at(g, t) + b / E * GT) * E + b % E;
+                    if (b / E * GT < part.left(g, t)) take(id, Elem<T>::get(row.p + id));
                 }
             }
         }
-        if (edge && !(xe < limit)) take(row.edge(g.lane));
+        if (edge && !(xe < limit)) take(row.edge(g.lane), xe);
         __syncthreads();
         if (cluster) {
             if (g.tid == 0) st_shared_cluster_u32(mapa_shared(smem_u32(top.counts + g.rank), 0), top.local);
             cluster_sync();
-        } else {
-            if (g.tid == 0) top.counts[0] = top.local;
-            __syncthreads();
-        }
-        if (g.rank != 0) return;
-        bool over = false;
-        unsigned int count = 0;
-        for (int r = 0; r < g.parts; ++r) {
-            const unsigned int n = top.counts[r];
-            over = over || n > static_cast<unsigned int>(share);
-            if (!over) {
-                for (unsigned int i = g.tid; i < n; i += GT) {
-                    const int id = top.id[r * share + i];
-                    if (count + i < CAND_MAX) top.key[count + i] = token_key(Elem<T>::get(row.p + id), id);
-                }
+            if (g.rank != 0) return;
+            count = 0;
+            for (int r = 0; r < g.parts; ++r) {
+                const unsigned int n = top.counts[r];
+                for (unsigned int i = g.tid; i < min(n, share); i += GT) top.key[min(count + i, CAND_MAX - 1u)] = top.found[r * share + i];
+                count = n > share ? CAND_MAX + 1 : count + n;
+                if (count > CAND_MAX) break;
             }
-            count += n;
+        } else {
+            count = top.local;
         }
-        if (!over && count < static_cast<unsigned int>(P.k)) {
+        if (count < static_cast<unsigned int>(P.k)) {
             // fewer than k tokens above -inf: the lowest ids of the others follow,
             // all of them among the first k + count ids
             __syncthreads();
@@ -844,52 +811,35 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
                 }
                 if (g.lane == 0) top.count = min(n, static_cast<unsigned int>(CAND_MAX));
             }
-        } else if (g.tid == 0) {
-            top.count = over ? CAND_MAX + 1 : count;
+            __syncthreads();
+            count = top.count;
+        } else if (cluster) {
+            __syncthreads();
         }
-    } else {
-        exchange(a, 0.f, g, slots);
-        if (g.rank != 0) return;
-        if (g.tid == 0) top.count = CAND_MAX + 1;
+    } else if (g.rank != 0) {
+        return;
     }
-    if (g.warp == 0) {
-        a = acc_slots<GT, ENT>(slots, warps, g, P.c2);
-        const float m = a.m, m0 = m == NEG_INF ? 0.f : m, logs = m == NEG_INF ? 0.f : logf(a.s);
-        if (g.lane == 0) {
-            const float H = ENT && m != NEG_INF ? logs - LN2 * (a.t / a.s) : 0.f;
-            if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
-            if (ENT && P.entropy) P.entropy[g.row] = H;
-            if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
-            top.m0 = m0;
-            top.logs = logs;
-        }
+    if (count > CAND_MAX) {
+        top_radix<T, GT>(row.p, P.vocab, P.k, top);
+        count = top.count;
     }
-    __syncthreads();
-    if (top.count > CAND_MAX) top_radix<T, GT>(row.p, P.vocab, P.k, top);
-    const int count = top.count;
-    const float m0 = top.m0, logs = top.logs;
-    const auto give = [&](unsigned long long key, int rank) {
-        P.top_ids[g.row * P.k + rank] = 0xffffffffu - static_cast<uint32_t>(key);
-        P.top_logp[g.row * P.k + rank] = (key_value(static_cast<uint32_t>(key >> 32)) - m0) * P.c - logs;
+    const auto give = [&](unsigned long long key, unsigned int place) {
+        P.top_ids[g.row * P.k + place] = 0xffffffffu - static_cast<uint32_t>(key);
+        P.top_logp[g.row * P.k + place] = (key_value(static_cast<uint32_t>(key >> 32)) - m0) * P.c - logs;
     };
-    if (count <= 32) {
-        if (g.warp == 0) {
-            unsigned long long key[1] = {g.lane < count ? top.key[g.lane] : 0ull};
-            sort_warp(key, g.lane);
-            if (g.lane < P.k) give(key[0], g.lane);
-        }
-    } else if (count <= 128) {
-        if (g.warp == 0) {
-            unsigned long long key[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) key[r] = r * 32 + g.lane < count ? top.key[r * 32 + g.lane] : 0ull;
-            sort_warp(key, g.lane);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (r * 32 + g.lane < P.k) give(key[r], r * 32 + g.lane);
+    const int n = count <= 2 ? static_cast<int>(count) : 1 << (32 - __clz(count - 1));
+    if (n <= GT) {
+        // `share` neighbouring threads count for one candidate
+        const unsigned int share = min(32, GT / n), c = g.tid / share;
+        const unsigned long long key = c < count ? top.key[c] : 0;
+        unsigned int before = 0;
+        if (c - g.lane / share < count) {   // the warp has candidates
+#pragma unroll 4
+            for (unsigned int i = g.tid % share; i < count; i += share) before += top.key[i] > key;
+            for (unsigned int i = share / 2; i; i /= 2) before += __shfl_xor_sync(~0u, before, i);
+            if (c < count && g.tid % share == 0 && before < static_cast<unsigned int>(P.k)) give(key, before);
         }
     } else {
-        const int n = 1 << (32 - __clz(count - 1));
         for (int i = count + g.tid; i < n; i += GT) top.key[i] = 0;
         sort_block<GT>(top.key, n);
         for (int i = g.tid; i < P.k; i += GT) give(top.key[i], i);
@@ -912,7 +862,7 @@ template <int GT>
 struct ListShared {
     int id[VOCAB_MAX_K];                    // -1: no token
     float u[VOCAB_MAX_K], x[VOCAB_MAX_K];   // the teacher's exponent, the student's logit
-    float4 part[Group<GT>::W];              // per warp: maximum and sum of the student's, of the teacher's
+    float2 student[Group<GT>::W], teacher[Group<GT>::W];   // maximum and sum, per warp
     float sum[Group<GT>::W];
     unsigned int edges;                     // bits of the row's edge elements that are on the list
 };
@@ -958,44 +908,52 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         if (g.tid == 0) list.edges = 0;
         G::sync();
     }
-    for (int i = g.tid; i < P.k; i += GT) {
-        const long long t = i == g.tid ? t0 : P.t_ids[g.row * P.k + i];
-        const bool there = t >= 0 && t < P.vocab;
-        const int id = there ? static_cast<int>(t) : -1;
-        if (PASS != VOCAB_BWD && there) {
-            const int at = id - row.head, v = at / E - part.begin, tile = v / G::TILE;
-            if (at < 0 || at >= row.full * E)
-                atomicOr(&list.edges, 1u << (at < 0 ? id : row.head + at - row.full * E));
-            else if (v >= 0 && part.begin + v < part.end)
-                atomicOr(listed + tile * GT + v % GT, static_cast<Bits<T>>(1) << (v % G::TILE / GT * E + at % E));
+    const bool lister = g.warp * 32 < P.k;   // the warp has entries
+    float x0 = NEG_INF;                      // the thread's first entry's, under way until after the barrier
+    if (lister) {
+        float um = NEG_INF, us = 0.f;
+        for (int i = g.tid; i < P.k; i += GT) {
+            const long long t = i == g.tid ? t0 : P.t_ids[g.row * P.k + i];
+            const bool there = t >= 0 && t < P.vocab;
+            const int id = there ? static_cast<int>(t) : -1;
+            if (there) {
+                if (i == g.tid) x0 = Elem<T>::get(row.p + id);
+                if (PASS != VOCAB_BWD) {
+                    const int at = id - row.head, v = at / E - part.begin, tile = v / G::TILE;
+                    if (at < 0 || at >= row.full * E)
+                        atomicOr(&list.edges, 1u << (at < 0 ? id : row.head + at - row.full * E));
+                    else if (v >= 0 && part.begin + v < part.end)
+                        atomicOr(listed + tile * GT + v % GT, static_cast<Bits<T>>(1) << (v % G::TILE / GT * E + at % E));
+                }
+            }
+            const float u = there ? (i == g.tid ? u0 : P.t_vals[g.row * P.k + i]) * P.t_c - shift : NEG_INF;
+            list.id[i] = id;
+            list.u[i] = u;
+            um = max_nan(um, u);
         }
-        list.id[i] = id;
-        list.u[i] = there ? (i == g.tid ? u0 : P.t_vals[g.row * P.k + i]) * P.t_c - shift : NEG_INF;
-        list.x[i] = there ? Elem<T>::get(row.p + id) : NEG_INF;
+        um = P.rest ? 0.f : max_nan_warp(um);
+        for (int i = g.tid; i < P.k; i += GT)
+            if (list.id[i] >= 0 && um != NEG_INF) us += expf(list.u[i] - um);
+        us = sum_warp(us);
+        if (g.lane == 0) list.teacher[g.warp] = make_float2(um, us);
     }
     if (PASS != VOCAB_BWD) {
         G::sync();
         if (edge && list.edges >> g.lane & 1) xe = NEG_INF;
     }
-    // the list's statistics, a share per warp
-    {
-        float xm = NEG_INF, um = NEG_INF, xs = 0.f, us = 0.f;
-        if (g.warp * 32 < P.k) {
-            for (int i = g.tid; i < P.k; i += GT) {
-                xm = max_nan(xm, list.x[i]);
-                um = max_nan(um, list.u[i]);
-            }
-            xm = max_nan_warp(xm);
-            um = P.rest ? 0.f : max_nan_warp(um);
-            for (int i = g.tid; i < P.k; i += GT) {
-                if (list.id[i] < 0) continue;
-                if (xm != NEG_INF) xs += ex2((list.x[i] - xm) * P.c2);
-                if (um != NEG_INF) us += expf(list.u[i] - um);
-            }
-            xs = sum_warp(xs);
-            us = sum_warp(us);
+    if (lister) {
+        float xm = NEG_INF, xs = 0.f;
+        for (int i = g.tid; i < P.k; i += GT) {
+            const int id = list.id[i];
+            const float x = i == g.tid ? x0 : id >= 0 ? Elem<T>::get(row.p + id) : NEG_INF;
+            list.x[i] = x;
+            xm = max_nan(xm, x);
         }
-        if (g.lane == 0) list.part[g.warp] = make_float4(xm, xs, um, us);
+        xm = max_nan_warp(xm);
+        for (int i = g.tid; i < P.k; i += GT)
+            if (list.id[i] >= 0 && xm != NEG_INF) xs += ex2((list.x[i] - xm) * P.c2);
+        xs = sum_warp(xs);
+        if (g.lane == 0) list.student[g.warp] = make_float2(xm, xs);
     }
     Acc r = acc_none();
     if (PASS == VOCAB_BWD) {
@@ -1013,7 +971,10 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
             const Bits<T> mine = listed[t * GT + g.tid];
             if (mine) {
 #pragma unroll
-                for (int j = 0; j < NV; ++j) Elem<T>::ban(d[j], static_cast<uint32_t>(mine >> (j * E)));
+                for (int j = 0; j < NV; ++j) {
+                    const uint32_t b = static_cast<uint32_t>(mine >> (j * E)) & ((1u << E) - 1);
+                    if (b) Elem<T>::ban(d[j], b);
+                }
             }
             const Acc b = acc_tile<T, false>(d, Elem<T>::max_of(d), P.c2);
             a = t > 0 ? acc_merge<false>(a, b, P.c2) : b;
@@ -1024,10 +985,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
             G::sync();
         } else {
             exchange(r, 0.f, g, slots);
-            if (PASS == VOCAB_FWD && (g.rank != 0 || g.warp * 32 >= P.k)) {
-                if (g.rank != 0) return;
-                list.sum[g.warp] = 0.f;
-                __syncthreads();
+            if (PASS == VOCAB_FWD && (g.rank != 0 || !lister)) {
+                if (g.rank == 0) __syncthreads();
                 return;
             }
             r = acc_slots<GT, false>(slots, G::W * g.parts, g, P.c2);
@@ -1038,36 +997,42 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
     Acc l = acc_none();
     float um = NEG_INF, us = 0.f;
     if (g.lane < G::W && g.lane * 32 < P.k) {
-        const float4 o = list.part[g.lane];
+        const float2 o = list.student[g.lane], q = list.teacher[g.lane];
         l = Acc{o.x, o.y, 0.f};
-        um = o.z, us = o.w;
+        um = q.x, us = q.y;
     }
     l = acc_warp<false>(l, P.c2);
-    const float uml = max_nan_warp(um);
-    us = sum_warp(us == 0.f ? 0.f : us * expf(um - uml));
-    um = uml;
+    if (P.rest) {
+        us = sum_warp(us);
+    } else {
+        const float uml = max_nan_warp(um);
+        us = sum_warp(us == 0.f ? 0.f : us * expf(um - uml));
+        um = uml;
+    }
     if (PASS != VOCAB_BWD) {
-        const Acc a = acc_merge<false>(l, r, P.c2);
-        m = a.m, s = a.s;
-        logs = m == NEG_INF ? 0.f : logf(s);
-        logr = mr == NEG_INF ? 0.f : logf(sr);
+        m = max_nan(l.m, r.m);
+        s = acc_to<false>(l, m, P.c2).s + acc_to<false>(r, m, P.c2).s;
     }
     const float m0 = m == NEG_INF ? 0.f : m;
-    // teacher: q_k = exp(u_k - um) uq; Q = sum q; rest: an entry of its own where q_R > 0
-    const float uq = P.rest ? 1.f : 1.f / us, u_log = P.rest ? 0.f : us == 0.f ? 0.f : um + logf(us);
-    const float Q = P.rest ? us : us == 0.f ? 0.f : us * uq;
+    // teacher: q_k = exp(u_k - um) / us or exp(u_k); Q = sum q; rest: an entry of its own where q_R > 0
+    const float Q = P.rest ? us : us == 0.f ? 0.f : us - us + 1.f;
     const float qr = P.rest && mr != NEG_INF ? fmaxf(1.f - Q, 0.f) : 0.f;
     const bool entry = qr > 0.f;
-    const float pl = acc_to<false>(l, m, P.c2).s / s;   // the student's probability of the list
-    const float logpr = (mr - m0) * P.c + logr - logs;
     const float wt = w * P.temperature;
     const bool live = w != 0.f && m != NEG_INF;
+    float logpr = 0.f;
     // loss, and the list's gradients (stored over the row's below)
     float kl = 0.f;
-    if (g.warp * 32 < P.k) {
+    if (lister) {
+        if (PASS != VOCAB_BWD) {
+            logs = m == NEG_INF ? 0.f : logf(s);
+            logr = mr == NEG_INF ? 0.f : logf(sr);
+        }
+        logpr = (mr - m0) * P.c + logr - logs;
+        const float u_log = P.rest ? 0.f : us == 0.f ? 0.f : um + logf(us);
         for (int i = g.tid; i < P.k; i += GT) {
             if (list.id[i] < 0) continue;
-            const float logq = list.u[i] - u_log, q = P.rest ? expf(logq) : us == 0.f ? 0.f : expf(list.u[i] - um) * uq;
+            const float logq = list.u[i] - u_log, q = us == 0.f ? 0.f : P.rest ? expf(logq) : expf(list.u[i] - um) / us;
             const float logp = (list.x[i] - m0) * P.c - logs, p = expf(logp);
             if (PASS != VOCAB_BWD) {
                 if (entry) kl += q > 0.f ? q * excess(logq - logp) : p;
@@ -1086,7 +1051,10 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15u) == 0;
         const bool near = fabsf(mr * P.c2) < NEAR;
         const Base base(mr, P.c2);
-        const float rate = mr == NEG_INF ? 0.f : wt * (entry ? Q - pl : Q * expf(logpr)) / sr;
+        // rate of exp(c (x - mr)): with the rest (Q - sum p) / sr, else Q p_R / sr
+        const float rate = mr == NEG_INF ? 0.f
+                           : entry       ? wt * (Q - acc_to<false>(l, m, P.c2).s / s) / sr
+                                         : wt * Q * ex2((mr - m) * P.c2) / s;
         const float A = rate * ex2(-base.delta);
         const auto one = [&](float x) -> float {
             if (!live || mr == NEG_INF) return 0.f;
