@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 namespace cola {
 namespace {
@@ -13,41 +14,48 @@ struct Plan {
     int threads, parts;
 };
 
-#ifndef VOCAB_FWD_GT
-#define VOCAB_FWD_GT 256
-#endif
-#ifndef VOCAB_STEP_GT
-#define VOCAB_STEP_GT 256
-#endif
-#ifndef VOCAB_HOLD_KB
-#define VOCAB_HOLD_KB 256
-#endif
+// Bytes of the rows that the device works on at once that L2 still holds when a
+// step reads them again, its stores beside them: at 39 and 61 MB a step over rows
+// of 64 and 100 KB runs at 1.00 and 0.93 of the copy bandwidth, at 122 MB (rows of
+// 200 KB on one CTA each) at 0.84, on two at 0.93.
+constexpr double STEP_L2_BYTES = 62e6;
 
 // A warp or four warps where their registers hold the row (NV vectors a
-// thread).  Longer rows: a forward reads tile after tile with eight warps, so
-// that the ends of several rows overlap on an SM; a step, which writes what it
-// has read, takes sixteen warps and as many CTAs as hold the row in
-// registers, up to a portable cluster's eight; a backward a CTA per tile.  All
-// take more CTAs where there are fewer rows than the device runs CTAs at once,
-// down to a vector per thread.
+// thread).  Longer rows take eight warps, so that the phases of four rows overlap
+// on an SM, tile after tile; sixteen where eight have too few threads for the
+// bound of the top k (`least`).  A step reads its row twice, the second time from L2:
+// as many CTAs share a row as keep the rows in flight within it, sixteen warps
+// where that would take more than a portable cluster's eight CTAs.  The
+// backward without a list (`split`) exchanges nothing: a CTA per tile.  All take more CTAs
+// where there are fewer rows than the device runs CTAs at once, down to a vector
+// per thread.  CTAs that form a cluster are a power of two: threes and sixes
+// leave SMs empty (390 us against 332 us for a step of 2048 x 262144 on six and four).
 Plan plan(const VocabParams& p, int e, int pass, bool split, int least, int sms)
 {
     const int nvec = (p.vocab + e - 1) / e;
     if (least <= 32 && nvec <= 32 * NV) return {32, 1};
     if (least <= 128 && nvec <= 128 * NV) return {128, 1};
-    const int threads = least > 256 ? 512 : pass == VOCAB_FWD ? VOCAB_FWD_GT : pass == VOCAB_STEP ? VOCAB_STEP_GT : 512;
-    const int hold = pass == VOCAB_STEP ? (nvec * 16 <= VOCAB_HOLD_KB * 1024 ? 1 : (nvec + 512 * NV - 1) / (512 * NV))
-                     : split            ? (nvec + 512 * NV - 1) / (512 * NV)
-                                        : 1;
+    int threads = least <= 256 ? 256 : 512, hold = 1;
+    if (pass == VOCAB_STEP) {
+        hold = static_cast<int>(std::ceil(4.0 * sms * 16.0 * nvec / STEP_L2_BYTES));
+        if (hold > CLUSTER_MAX) threads = 512, hold = (hold + 1) / 2;
+    } else if (pass == VOCAB_BWD) {
+        threads = 512;
+        if (split) hold = (nvec + 512 * NV - 1) / (512 * NV);
+    }
     const int fill = static_cast<int>(std::min<long long>(1024ll / threads * sms / p.n, nvec / threads));
-    return {threads, std::min(CLUSTER_MAX, std::max({1, hold, fill}))};
+    if (split) return {threads, std::min(CLUSTER_MAX, std::max(hold, fill))};
+    int parts = 1;
+    while (parts < CLUSTER_MAX && (parts < hold || 2 * parts <= fill)) parts *= 2;
+    return {threads, parts};
 }
 
 template <class K>
-cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, cudaStream_t stream)
+cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, int sms, cudaStream_t stream)
 {
     const int rows = s.threads == 32 ? 4 : 1;
     p.each = (p.vocab / e + s.parts - 1) / s.parts;
+    p.ahead = static_cast<int>(sms * 1024ll / (s.threads * rows) / s.parts * rows);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned int>((p.n + rows - 1) / rows), s.parts);
     cfg.blockDim = dim3(s.threads * rows);
@@ -68,11 +76,11 @@ template <class T, bool ENT>
 cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    const Plan s = plan(p, E, VOCAB_FWD, false, p.k <= 64 ? 128 : 512, sms);
+    const Plan s = plan(p, E, VOCAB_FWD, false, p.k <= 64 ? 128 : p.k <= 128 ? 256 : 512, sms);
     switch (s.threads) {
-    case 128: return launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, stream);
-    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT>, p, E, s, true, 0, stream);
-    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, stream);
+    case 128: return launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, sms, stream);
+    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT>, p, E, s, true, 0, sms, stream);
+    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, sms, stream);
     }
 }
 
@@ -81,12 +89,12 @@ cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    constexpr int GT = PASS == VOCAB_FWD ? VOCAB_FWD_GT : PASS == VOCAB_STEP ? VOCAB_STEP_GT : 512;
     const Plan s = plan(p, E, PASS, !cluster, 32, sms);
     switch (s.threads) {
-    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, stream);
-    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, stream);
-    default: return launch_rows(token_logprob_kernel<T, PASS, GT, ENT>, p, E, s, cluster, 0, stream);
+    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, sms, stream);
+    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, sms, stream);
+    case 256: return launch_rows(token_logprob_kernel<T, PASS, 256, ENT>, p, E, s, cluster, 0, sms, stream);
+    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT>, p, E, s, cluster, 0, sms, stream);
     }
 }
 
@@ -105,7 +113,7 @@ cudaError_t logprob_pass(VocabParams p, int pass, int sms, cudaStream_t stream)
 }
 
 template <class T, int PASS, int GT>
-cudaError_t distill_rows(VocabParams& p, const Plan& s, cudaStream_t stream)
+cudaError_t distill_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     auto kern = topk_distill_kernel<T, PASS, GT>;
@@ -127,18 +135,18 @@ cudaError_t distill_rows(VocabParams& p, const Plan& s, cudaStream_t stream)
             }
         }
     }
-    return launch_rows(kern, p, E, s, true, smem, stream);
+    return launch_rows(kern, p, E, s, true, smem, sms, stream);
 }
 
 template <class T, int PASS>
 cudaError_t distill(VocabParams p, int sms, cudaStream_t stream)
 {
-    constexpr int GT = PASS == VOCAB_FWD ? VOCAB_FWD_GT : PASS == VOCAB_STEP ? VOCAB_STEP_GT : 512;
     const Plan s = plan(p, Elem<T>::E, PASS, false, 32, sms);
     switch (s.threads) {
-    case 32: return distill_rows<T, PASS, 32>(p, s, stream);
-    case 128: return distill_rows<T, PASS, 128>(p, s, stream);
-    default: return distill_rows<T, PASS, GT>(p, s, stream);
+    case 32: return distill_rows<T, PASS, 32>(p, s, sms, stream);
+    case 128: return distill_rows<T, PASS, 128>(p, s, sms, stream);
+    case 256: return distill_rows<T, PASS, 256>(p, s, sms, stream);
+    default: return distill_rows<T, PASS, 512>(p, s, sms, stream);
     }
 }
 

@@ -30,6 +30,7 @@ struct VocabParams {
     void* dlogits;
     long long n, ld, ld_d;
     int vocab, k, rest;
+    int ahead;                // rows from one CTA to the next in its place
     int each;                 // 16-byte vectors of a row per CTA (the grid's y: CTAs of a row)
     float temperature;
     float c;                  // 1 / temperature
@@ -236,10 +237,15 @@ struct Elem<__nv_bfloat16> {
     }
     __device__ __forceinline__ static uint32_t ban_pair(uint32_t w, uint32_t bits)
     {
-        const uint32_t m = (bits & 1 ? 0x0000ffffu : 0u) | (bits & 2 ? 0xffff0000u : 0u);
+        const uint32_t m = ((bits | bits << 15) & 0x00010001u) * 0xffffu;
         return (w & ~m) | (FILL & m);
     }
 };
+
+__device__ __forceinline__ void prefetch_l2_bulk(const void* p, int bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
 
 // ------------------------------------------------------------- rows in memory
 // A row of `vocab` elements: the 16-byte vectors at 16-byte boundaries, and up
@@ -306,6 +312,10 @@ struct Part {
     // this thread's first vector of a tile; vector j lies GT j after it and is there where left > GT j
     __device__ __forceinline__ int at(const Group<GT>& g, int tile) const { return begin + tile * Group<GT>::TILE + g.tid; }
     __device__ __forceinline__ int left(const Group<GT>& g, int tile) const { return end - at(g, tile); }
+    // vectors of a tile that any thread holds
+    __device__ __forceinline__ int used(int tile) const { return (end - begin - tile * Group<GT>::TILE + GT - 1) / GT; }
+    // LAST: for the last time (streaming stores and these leave L2 to rows still to be read again)
+    template <bool LAST = false>
     __device__ __forceinline__ void load(const Row<T>& row, const Group<GT>& g, int tile, uint4 (&d)[NV]) const
     {
         const uint4* q = row.vec() + at(g, tile);
@@ -313,8 +323,14 @@ struct Part {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             d[j] = make_uint4(Elem<T>::FILL, Elem<T>::FILL, Elem<T>::FILL, Elem<T>::FILL);
-            if (n > j * GT) d[j] = q[j * GT];
+            if (n > j * GT) d[j] = LAST ? __ldcs(q + j * GT) : q[j * GT];
         }
+    }
+    // the tiles after the first on their way to L2, ahead of the loads
+    __device__ __forceinline__ void prefetch(const Row<T>& row, const Group<GT>& g) const
+    {
+        const int from = begin + Group<GT>::TILE;
+        if (g.tid == 0 && from < end) prefetch_l2_bulk(row.vec() + from, (end - from) * 16);
     }
     // the thread that holds vector v
     __device__ __forceinline__ bool owns(const Group<GT>& g, int v) const
@@ -394,7 +410,7 @@ struct Base {
 // maxima whose exponent rounds coarsely (masks of the lowest value, +inf, NaN),
 // the difference from the maximum first, as an operation of its own.
 template <class T, bool ENT, bool FAR>
-__device__ __forceinline__ Acc acc_tile_from(const uint4 (&d)[NV], float m, float c2)
+__device__ __forceinline__ Acc acc_tile_from(const uint4 (&d)[NV], int used, float m, float c2)
 {
     constexpr int E = Elem<T>::E;
     const Base base(FAR ? 0.f : m, c2);
@@ -402,6 +418,7 @@ __device__ __forceinline__ Acc acc_tile_from(const uint4 (&d)[NV], float m, floa
     Pair s2[2] = {0, 0}, t2[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+        if (j % 2 == 0 && j >= used) break;
         float x[E];
         Elem<T>::unpack(d[j], x);
 #pragma unroll
@@ -426,11 +443,11 @@ __device__ __forceinline__ Acc acc_tile_from(const uint4 (&d)[NV], float m, floa
 }
 
 template <class T, bool ENT>
-__device__ __forceinline__ Acc acc_tile(const uint4 (&d)[NV], float m, float c2)
+__device__ __forceinline__ Acc acc_tile(const uint4 (&d)[NV], int used, float m, float c2)
 {
     if (m == NEG_INF) return acc_none();
-    if (fabsf(m * c2) < NEAR) return acc_tile_from<T, ENT, false>(d, m, c2);
-    return acc_tile_from<T, ENT, true>(d, m, c2);
+    if (fabsf(m * c2) < NEAR) return acc_tile_from<T, ENT, false>(d, used, m, c2);
+    return acc_tile_from<T, ENT, true>(d, used, m, c2);
 }
 
 // Every warp's statistics to every CTA of the row; the barrier of the exchange.
@@ -484,7 +501,7 @@ __device__ __forceinline__ unsigned long long token_key(float x, int j)
 // The candidates of a row's top k, in the first of its CTAs.
 struct TopShared {
     unsigned long long key[CAND_MAX];
-    unsigned long long found[CAND_MAX];   // a cluster's: a share for each CTA of the row
+    int found[CAND_MAX];                  // ids; a share for each CTA of the row
     unsigned int hist[256];
     unsigned int counts[CLUSTER_MAX];
     unsigned int count, digit, above, bound, local;
@@ -569,10 +586,11 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
     for (int t = part.tiles - 1; t >= 0; --t) {
         const int first = part.at(g, t), left = part.left(g, t);
         if (live && near && same) {
-            if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
+            if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.template load<true>(row, g, t, d);
             const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A), B2 = pair(B, B);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
+                if (j % 2 == 0 && j >= part.used(t)) break;
                 float x[E];
                 Elem<T>::unpack(d[j], x);
 #pragma unroll
@@ -582,7 +600,7 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
                     const Pair w = pair(ex2(y0), ex2(y1));
                     split(mul2(w, ENT ? fma2(pair(fmaxf(y0, FLOOR), fmaxf(y1, FLOOR)), B2, A2) : A2), x[e], x[e + 1]);
                 }
-                if (left > j * GT) vout[first + j * GT] = Elem<T>::pack(x);
+                if (left > j * GT) __stcs(vout + first + j * GT, Elem<T>::pack(x));
             }
         } else {
 #pragma unroll 1
@@ -619,6 +637,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     const Part<T, GT> part(row, g, P.each);
     uint4 d[NV];
     part.load(row, g, 0, d);
+    if (PASS == VOCAB_STEP) part.prefetch(row, g);
     const long long target = P.targets ? P.targets[g.row] : -1;
     const bool there = target >= 0 && target < P.vocab;
     const int y = there ? static_cast<int>(target) : -1;
@@ -641,7 +660,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         Acc a = acc_none();
         for (int t = 0; t < part.tiles; ++t) {
             if (t > 0) part.load(row, g, t, d);
-            const Acc b = acc_tile<T, ENT>(d, Elem<T>::max_of(d), P.c2);
+            const Acc b = acc_tile<T, ENT>(d, part.used(t), Elem<T>::max_of(d), P.c2);
             a = t > 0 ? acc_merge<ENT>(a, b, P.c2) : b;
         }
         if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
@@ -706,20 +725,25 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     const bool edge = g.has_edges() && g.lane < row.edges();
     if (edge) xe = Elem<T>::get(row.p + row.edge(g.lane));
     Acc a = acc_none();
+    uint32_t mine = 0, second = 0;   // this thread's largest, the largest of its other tiles
+    int tile = 0;                    // and the tile that has it
     for (int t = 0; t < part.tiles; ++t) {
         if (t > 0) part.load(row, g, t, d);
-        const Acc b = acc_tile<T, ENT>(d, Elem<T>::max_of(d), P.c2);
+        const float mt = Elem<T>::max_of(d);
+        const uint32_t key = value_key(mt);
+        second = max(second, min(mine, key));
+        if (key > mine) mine = key, tile = t;
+        const Acc b = acc_tile<T, ENT>(d, part.used(t), mt, P.c2);
         a = t > 0 ? acc_merge<ENT>(a, b, P.c2) : b;
     }
     if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
-    const uint32_t mine = value_key(a.m);   // of this thread
     a = acc_warp<ENT>(a, P.c2);
     const int warps = G::W * g.parts;
     // a cluster: of each warp, a little more of its largest than k over the warps
     const int each = P.k <= warps ? 1 : (3 * P.k + 2 * warps - 1) / (2 * warps);
     const bool bounded = cluster ? each <= 24 : P.k <= GT;
     uint32_t best = 0;
-    if (cluster && bounded) {
+    if (bounded && (cluster || P.k <= G::W)) {
         uint32_t left = mine;
         for (int i = 0; i < each; ++i) {
             best = __reduce_max_sync(~0u, left);
@@ -738,10 +762,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     unsigned int count = CAND_MAX + 1;
     if (bounded) {
         uint32_t bound = 0;
-        if (!cluster) {
+        if (!cluster && P.k > G::W) {
             // the k-th largest of the threads' maxima, from above to its upper 16 bits
+            const uint32_t most = value_key(m);
             for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
-                if (__syncthreads_count(mine >= (bound | bit)) >= P.k) bound |= bit;
+                if ((bound | bit) <= most && __syncthreads_count(mine >= (bound | bit)) >= P.k) bound |= bit;
         } else {
             // the warps' value with `before` = ceil(k / each) - 1 before it
             const unsigned int before = (P.k + each - 1) / each - 1;
@@ -759,63 +784,66 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         }
         // a bound of -inf: what lies above it here; the first of the -inf tokens follow below
         const float limit = bound <= value_key(NEG_INF) ? Elem<T>::LOWEST : key_value(bound);
-        const unsigned int share = cluster ? CAND_MAX / g.parts : CAND_MAX;
+        const unsigned int share = CAND_MAX / g.parts;
         const uint32_t list = cluster ? mapa_shared(smem_u32(top.found + g.rank * share), 0) : 0;
-        const auto take = [&](int id, float x) {
+        const auto take = [&](int id) {
             const unsigned int at = atomicAdd(&top.local, 1u);
             if (at < share) {
-                if (cluster) st_cluster_u64(list + 8 * at, token_key(x, id));
-                else top.key[at] = token_key(x, id);
+                if (cluster) st_shared_cluster_u32(list + 4 * at, id);
+                else top.found[at] = id;
             }
         };
-        if (mine >= bound) {
-            for (int t = part.tiles - 1; t >= 0; --t) {
-                if (t < part.tiles - 1) part.load(row, g, t, d);
-                unsigned long long bits = Elem<T>::reach(d, limit);
-                while (bits) {
-                    const int b = Elem<T>::place(__ffsll(bits) - 1);
-                    bits &= bits - 1;
-                    const int id = row.head + (part.at(g, t) + b / E * GT) * E + b % E;
-                    if (b / E * GT < part.left(g, t)) take(id, Elem<T>::get(row.p + id));
-                }
+        const auto take_tile = [&](int t) {
+            unsigned long long bits = Elem<T>::reach(d, limit);
+            while (bits) {
+                const int b = Elem<T>::place(__ffsll(bits) - 1);
+                bits &= bits - 1;
+                if (b / E * GT < part.left(g, t)) take(row.head + (part.at(g, t) + b / E * GT) * E + b % E);
+            }
+        };
+        if (mine >= bound) {   // each thread the tile of its largest, then the rest if its second reaches too
+            if (part.tiles > 1) part.load(row, g, tile, d);
+            take_tile(tile);
+            for (int t = 0; second >= bound && t < part.tiles; ++t) {
+                if (t == tile) continue;
+                part.load(row, g, t, d);
+                take_tile(t);
             }
         }
-        if (edge && !(xe < limit)) take(row.edge(g.lane), xe);
+        if (edge && !(xe < limit)) take(row.edge(g.lane));
         __syncthreads();
         if (cluster) {
             if (g.tid == 0) st_shared_cluster_u32(mapa_shared(smem_u32(top.counts + g.rank), 0), top.local);
             cluster_sync();
             if (g.rank != 0) return;
             count = 0;
-            for (int r = 0; r < g.parts; ++r) {
-                const unsigned int n = top.counts[r];
-                for (unsigned int i = g.tid; i < min(n, share); i += GT) top.key[min(count + i, CAND_MAX - 1u)] = top.found[r * share + i];
-                count = n > share ? CAND_MAX + 1 : count + n;
-                if (count > CAND_MAX) break;
-            }
+            for (int r = 0; r < g.parts; ++r) count = top.counts[r] > share ? 2 * CAND_MAX : count + top.counts[r];
         } else {
             count = top.local;
         }
-        if (count < static_cast<unsigned int>(P.k)) {
+        if (count <= CAND_MAX) {
+            for (unsigned int c = g.tid; c < count; c += GT) {
+                unsigned int at = c;
+                for (int r = 0; cluster && r < g.parts - 1 && at >= r * share + top.counts[r]; ++r) at += share - top.counts[r];
+                const int id = top.found[at];
+                top.key[c] = token_key(Elem<T>::get(row.p + id), id);
+            }
+        }
+        if (count < static_cast<unsigned int>(P.k) && g.warp == 0) {
             // fewer than k tokens above -inf: the lowest ids of the others follow,
             // all of them among the first k + count ids
-            __syncthreads();
-            if (g.warp == 0) {
-                unsigned int n = count;
-                for (int id = g.lane; n < static_cast<unsigned int>(P.k); id += 32) {
-                    const bool none = id < P.vocab && Elem<T>::get(row.p + id) == NEG_INF;
-                    const unsigned int set = __ballot_sync(~0u, none);
-                    const unsigned int at = n + __popc(set & ((1u << g.lane) - 1));
-                    if (none && at < CAND_MAX) top.key[at] = token_key(NEG_INF, id);
-                    n += __popc(set);
-                }
-                if (g.lane == 0) top.count = min(n, static_cast<unsigned int>(CAND_MAX));
+            unsigned int n = count;
+            for (int id = g.lane; n < static_cast<unsigned int>(P.k); id += 32) {
+                const bool none = id < P.vocab && Elem<T>::get(row.p + id) == NEG_INF;
+                const unsigned int set = __ballot_sync(~0u, none);
+                const unsigned int at = n + __popc(set & ((1u << g.lane) - 1));
+                if (none && at < CAND_MAX) top.key[at] = token_key(NEG_INF, id);
+                n += __popc(set);
             }
-            __syncthreads();
-            count = top.count;
-        } else if (cluster) {
-            __syncthreads();
+            if (g.lane == 0) top.count = min(n, static_cast<unsigned int>(CAND_MAX));
         }
+        __syncthreads();
+        if (count < static_cast<unsigned int>(P.k)) count = top.count;
     } else if (g.rank != 0) {
         return;
     }
@@ -828,7 +856,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         P.top_logp[g.row * P.k + place] = (key_value(static_cast<uint32_t>(key >> 32)) - m0) * P.c - logs;
     };
     const int n = count <= 2 ? static_cast<int>(count) : 1 << (32 - __clz(count - 1));
-    if (n <= GT) {
+    // counting takes count^2 / 32 steps of all warps together, sorting 30 to 55 barriers
+    if (n <= min(GT, 256)) {
         // `share` neighbouring threads count for one candidate
         const unsigned int share = min(32, GT / n), c = g.tid / share;
         const unsigned long long key = c < count ? top.key[c] : 0;
@@ -892,6 +921,12 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
     const float u0 = g.tid < P.k ? P.t_vals[g.row * P.k + g.tid] : 0.f;
     uint4 d[NV];
     part.load(row, g, 0, d);
+    if (PASS == VOCAB_STEP) part.prefetch(row, g);
+    if (g.row + P.ahead < P.n) {   // a later row's list
+        const long long at = (g.row + P.ahead) * P.k;
+        if (g.tid * 16 < P.k) prefetch_l2(P.t_ids + at + g.tid * 16);
+        else if (g.tid >= 32 && g.tid * 32 - 1024 < P.k) prefetch_l2(P.t_vals + at + g.tid * 32 - 1024);
+    }
     const bool edge = g.has_edges() && g.lane < row.edges();
     const int edge_id = edge ? row.edge(g.lane) : -1;
     float xe = edge ? Elem<T>::get(row.p + edge_id) : NEG_INF;
@@ -941,7 +976,9 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         G::sync();
         if (edge && list.edges >> g.lane & 1) xe = NEG_INF;
     }
-    if (lister) {
+    // the student's statistics on the list, a share per warp (the gathers were issued before the barrier)
+    const auto gather = [&]() {
+        if (!lister) return;
         float xm = NEG_INF, xs = 0.f;
         for (int i = g.tid; i < P.k; i += GT) {
             const int id = list.id[i];
@@ -954,9 +991,10 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
             if (list.id[i] >= 0 && xm != NEG_INF) xs += ex2((list.x[i] - xm) * P.c2);
         xs = sum_warp(xs);
         if (g.lane == 0) list.student[g.warp] = make_float2(xm, xs);
-    }
+    };
     Acc r = acc_none();
     if (PASS == VOCAB_BWD) {
+        gather();
         // in place: the list's logits are read before any CTA of the row stores
         if (cluster) {
             cluster_wait();
@@ -976,10 +1014,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
                     if (b) Elem<T>::ban(d[j], b);
                 }
             }
-            const Acc b = acc_tile<T, false>(d, Elem<T>::max_of(d), P.c2);
+            const Acc b = acc_tile<T, false>(d, part.used(t), Elem<T>::max_of(d), P.c2);
             a = t > 0 ? acc_merge<false>(a, b, P.c2) : b;
         }
         if (g.has_edges() && row.edges() > 0) a = acc_merge<false>(a, acc_one(xe), P.c2);
+        gather();
         r = acc_warp<false>(a, P.c2);
         if (GT == 32) {
             G::sync();
@@ -1063,10 +1102,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         for (int t = part.tiles - 1; t >= 0; --t) {
             const int first = part.at(g, t), left = part.left(g, t);
             if (live && near && same) {
-                if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.load(row, g, t, d);
+                if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.template load<true>(row, g, t, d);
                 const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A);
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
+                    if (j % 2 == 0 && j >= part.used(t)) break;
                     float x[E];
                     Elem<T>::unpack(d[j], x);
 #pragma unroll
@@ -1075,7 +1115,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
                         split(fma2(pair(x[e], x[e + 1]), cc, nb), y0, y1);
                         split(mul2(pair(ex2(y0), ex2(y1)), A2), x[e], x[e + 1]);
                     }
-                    if (left > j * GT) vout[first + j * GT] = Elem<T>::pack(x);
+                    if (left > j * GT) __stcs(vout + first + j * GT, Elem<T>::pack(x));
                 }
             } else {
 #pragma unroll 1
