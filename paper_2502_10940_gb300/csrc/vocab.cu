@@ -77,6 +77,12 @@ cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     const Plan s = plan(p, E, VOCAB_FWD, false, p.k <= 64 ? 128 : p.k <= 128 ? 256 : 512, sms);
+    // one CTA: the k-th largest of its warps' maxima, or (counted by the CTA) of its threads';
+    // a cluster: of each warp a little more of the largest than k over the warps
+    const int warps = s.threads / 32 * s.parts;
+    p.top_each = p.k <= warps ? 1 : s.parts == 1 ? (p.k <= s.threads ? 1 : 0) : (3 * p.k + 2 * warps - 1) / (2 * warps);
+    if (p.top_each > 24) p.top_each = 0;
+    p.top_before = p.top_each ? (p.k + p.top_each - 1) / p.top_each - 1 : 0;
     switch (s.threads) {
     case 128: return launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, sms, stream);
     case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT>, p, E, s, true, 0, sms, stream);

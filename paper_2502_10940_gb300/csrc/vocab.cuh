@@ -42,6 +42,7 @@ struct VocabParams {
     float* entropy;
     long long* top_ids;
     float* top_logp;
+    int top_each, top_before; // of each warp's largest, the one it gives; how many of those lie before the bound (each 0: no bound)
     const float* dlogp;
     const float* dentropy;
     // distillation
@@ -70,6 +71,13 @@ __device__ __forceinline__ float ex2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -682,7 +690,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         if (PASS == VOCAB_FWD && P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
     }
     if constexpr (PASS != VOCAB_FWD) {
-        const float inv_s = 1.f / s;
+        const float inv_s = rcp(s);
         if (!ENT || up_h == 0.f) emit_logprob<T, PASS, GT, false>(P, row, part, g, m, inv_s, logs, H, up_g, 0.f, y, xe, d);
         else emit_logprob<T, PASS, GT, true>(P, row, part, g, m, inv_s, logs, H, up_g, up_h, y, xe, d);
         if (owner && m != NEG_INF && (up_g != 0.f || up_h != 0.f)) {   // over its own store of that vector
@@ -739,13 +747,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
     a = acc_warp<ENT>(a, P.c2);
     const int warps = G::W * g.parts;
-    // a cluster: of each warp, a little more of its largest than k over the warps
-    const int each = P.k <= warps ? 1 : (3 * P.k + 2 * warps - 1) / (2 * warps);
-    const bool bounded = cluster ? each <= 24 : P.k <= GT;
+    const bool bounded = P.top_each > 0;
     uint32_t best = 0;
     if (bounded && (cluster || P.k <= G::W)) {
         uint32_t left = mine;
-        for (int i = 0; i < each; ++i) {
+        for (int i = 0; i < P.top_each; ++i) {
             best = __reduce_max_sync(~0u, left);
             if (g.lane == __ffs(__ballot_sync(~0u, left == best)) - 1) left = 0;
         }
@@ -768,23 +774,28 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
             for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
                 if ((bound | bit) <= most && __syncthreads_count(mine >= (bound | bit)) >= P.k) bound |= bit;
         } else {
-            // the warps' value with `before` = ceil(k / each) - 1 before it
-            const unsigned int before = (P.k + each - 1) / each - 1;
-            for (int i = g.warp; i < warps; i += G::W) {
-                const uint32_t v = __float_as_uint(slots[i].w);
-                unsigned int n = 0;
-                for (int q = g.lane; q < warps; q += 32) {
-                    const uint32_t o = __float_as_uint(slots[q].w);
-                    n += o > v || (o == v && q < i);
+            // the warps' value with top_before before it: each warp counts for one of each CTA
+            uint32_t all[CLUSTER_MAX * G::W / 32];
+#pragma unroll
+            for (int q = 0; q < CLUSTER_MAX * G::W / 32; ++q)
+                all[q] = g.lane + 32 * q < warps ? __float_as_uint(slots[g.lane + 32 * q].w) : 0u;
+#pragma unroll
+            for (int r = 0; r < CLUSTER_MAX; ++r) {
+                if (r < g.parts) {
+                    const int i = r * G::W + g.warp;
+                    const uint32_t v = __float_as_uint(slots[i].w);
+                    unsigned int n = 0;
+#pragma unroll
+                    for (int q = 0; q < CLUSTER_MAX * G::W / 32; ++q) n += all[q] > v || (all[q] == v && g.lane + 32 * q < i);
+                    if (__reduce_add_sync(~0u, n) == static_cast<unsigned int>(P.top_before) && g.lane == 0) top.bound = v;
                 }
-                if (__reduce_add_sync(~0u, n) == before && g.lane == 0) top.bound = v;
             }
             __syncthreads();
             bound = top.bound;
         }
         // a bound of -inf: what lies above it here; the first of the -inf tokens follow below
         const float limit = bound <= value_key(NEG_INF) ? Elem<T>::LOWEST : key_value(bound);
-        const unsigned int share = CAND_MAX / g.parts;
+        const unsigned int share = CAND_MAX >> (31 - __clz(g.parts));   // clusters are powers of two
         const uint32_t list = cluster ? mapa_shared(smem_u32(top.found + g.rank * share), 0) : 0;
         const auto take = [&](int id) {
             const unsigned int at = atomicAdd(&top.local, 1u);
@@ -859,14 +870,15 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     // counting takes count^2 / 32 steps of all warps together, sorting 30 to 55 barriers
     if (n <= min(GT, 256)) {
         // `share` neighbouring threads count for one candidate
-        const unsigned int share = min(32, GT / n), c = g.tid / share;
+        const int log_share = min(5, __clz(n) - __clz(GT));
+        const unsigned int share = 1u << log_share, c = g.tid >> log_share;
         const unsigned long long key = c < count ? top.key[c] : 0;
         unsigned int before = 0;
-        if (c - g.lane / share < count) {   // the warp has candidates
+        if (g.warp * 32u >> log_share < count) {   // the warp has candidates
 #pragma unroll 4
-            for (unsigned int i = g.tid % share; i < count; i += share) before += top.key[i] > key;
+            for (unsigned int i = g.tid & (share - 1); i < count; i += share) before += top.key[i] > key;
             for (unsigned int i = share / 2; i; i /= 2) before += __shfl_xor_sync(~0u, before, i);
-            if (c < count && g.tid % share == 0 && before < static_cast<unsigned int>(P.k)) give(key, before);
+            if (c < count && (g.tid & (share - 1)) == 0 && before < static_cast<unsigned int>(P.k)) give(key, before);
         }
     } else {
         for (int i = count + g.tid; i < n; i += GT) top.key[i] = 0;
@@ -922,10 +934,10 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
     uint4 d[NV];
     part.load(row, g, 0, d);
     if (PASS == VOCAB_STEP) part.prefetch(row, g);
-    if (g.row + P.ahead < P.n) {   // a later row's list
+    if (g.warp == 0 && g.row + P.ahead < P.n) {   // a later row's list
         const long long at = (g.row + P.ahead) * P.k;
-        if (g.tid * 16 < P.k) prefetch_l2(P.t_ids + at + g.tid * 16);
-        else if (g.tid >= 32 && g.tid * 32 - 1024 < P.k) prefetch_l2(P.t_vals + at + g.tid * 32 - 1024);
+        if (g.lane * 16 < P.k) prefetch_l2(P.t_ids + at + g.lane * 16);
+        if (g.lane * 32 < P.k) prefetch_l2(P.t_vals + at + g.lane * 32);
     }
     const bool edge = g.has_edges() && g.lane < row.edges();
     const int edge_id = edge ? row.edge(g.lane) : -1;
@@ -1092,8 +1104,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         const Base base(mr, P.c2);
         // rate of exp(c (x - mr)): with the rest (Q - sum p) / sr, else Q p_R / sr
         const float rate = mr == NEG_INF ? 0.f
-                           : entry       ? wt * (Q - acc_to<false>(l, m, P.c2).s / s) / sr
-                                         : wt * Q * ex2((mr - m) * P.c2) / s;
+                           : entry       ? wt * (Q - acc_to<false>(l, m, P.c2).s * rcp(s)) * rcp(sr)
+                                         : wt * Q * ex2((mr - m) * P.c2) * rcp(s);
         const float A = rate * ex2(-base.delta);
         const auto one = [&](float x) -> float {
             if (!live || mr == NEG_INF) return 0.f;
