@@ -340,6 +340,15 @@ struct Part {
         const int from = begin + Group<GT>::TILE;
         if (g.tid == 0 && from < end) prefetch_l2_bulk(row.vec() + from, (end - from) * 16);
     }
+    // a tile again into a thread's registers; what lies past its vectors stays what it was
+    __device__ __forceinline__ void reload(const Row<T>& row, const Group<GT>& g, int tile, uint4 (&d)[NV]) const
+    {
+        const uint4* q = row.vec() + at(g, tile);
+        const int n = left(g, tile);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (n > j * GT) d[j] = q[j * GT];
+    }
     // the thread that holds vector v
     __device__ __forceinline__ bool owns(const Group<GT>& g, int v) const
     {
@@ -771,8 +780,13 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         if (!cluster && P.k > G::W) {
             // the k-th largest of the threads' maxima, from above to its upper 16 bits
             const uint32_t most = value_key(m);
-            for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1)
-                if ((bound | bit) <= most && __syncthreads_count(mine >= (bound | bit)) >= P.k) bound |= bit;
+            // (its upper bits, where few more than k reach them)
+            for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1) {
+                if ((bound | bit) > most) continue;
+                const int n = __syncthreads_count(mine >= (bound | bit));
+                if (n >= P.k) bound |= bit;
+                if (n >= P.k && n <= P.k + (P.k >> 3) + 2) break;
+            }
         } else {
             // the warps' value with top_before before it: each warp counts for one of each CTA
             uint32_t all[CLUSTER_MAX * G::W / 32];
@@ -813,11 +827,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
             }
         };
         if (mine >= bound) {   // each thread the tile of its largest, then the rest if its second reaches too
-            if (part.tiles > 1) part.load(row, g, tile, d);
+            if (part.tiles > 1) part.reload(row, g, tile, d);
             take_tile(tile);
             for (int t = 0; second >= bound && t < part.tiles; ++t) {
                 if (t == tile) continue;
-                part.load(row, g, t, d);
+                part.reload(row, g, t, d);
                 take_tile(t);
             }
         }
