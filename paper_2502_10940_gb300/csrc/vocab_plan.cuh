@@ -1,0 +1,78 @@
+// vocab_plan.cuh -- how the rows of a vocabulary call are shared by threads
+// and CTAs, and their launch.
+#pragma once
+#include <algorithm>
+#include <cmath>
+
+#include "vocab_rows.cuh"
+
+namespace cola {
+
+// How a row is shared: `threads` of a CTA (32: a warp, four rows a CTA) and `parts` CTAs.
+struct Plan {
+    int threads, parts;
+};
+
+// Bytes of the rows that the device works on at once that L2 still holds when a
+// step reads them again, its stores beside them: at 39 and 61 MB a step over rows
+// of 64 and 100 KB runs at 1.00 and 0.93 of the copy bandwidth, at 122 MB (rows of
+// 200 KB on one CTA each) at 0.84, on two at 0.93.
+constexpr double STEP_L2_BYTES = 62e6;
+
+// A warp or four warps where their registers hold the row (NV vectors a
+// thread).  Longer rows take eight warps, so that the phases of four rows overlap
+// on an SM, tile after tile; sixteen where eight have too few threads for the
+// bound of the top k (`least`), and four where the top k of many rows of up to 4096
+// vectors, half of its work the same for every warp, has enough of 128 (116 us against
+// 129 us for the top 64 of 8192 x 32000; 130 against 105 for 2048 x 128000).  A step reads its row twice, the second time from L2:
+// as many CTAs share a row as keep the rows in flight within it, sixteen warps
+// where that would take more than a portable cluster's eight CTAs.  The
+// backward without a list (`split`) exchanges nothing: a CTA per tile.  All take more CTAs
+// where there are fewer rows than the device runs CTAs at once, down to a vector
+// per thread.  CTAs that form a cluster are a power of two: threes and sixes
+// leave SMs empty (390 us against 332 us for a step of 2048 x 262144 on six and four).
+inline Plan plan(const VocabParams& p, int e, int pass, bool split, int least, int sms)
+{
+    const int nvec = (p.vocab + e - 1) / e;
+    if (least <= 32 && nvec <= 32 * NV) return {32, 1};
+    if (least <= 128 && nvec <= 128 * NV) return {128, 1};
+    int threads = least <= 256 ? 256 : 512, hold = 1;
+    if (pass == VOCAB_FWD) {
+        if (least == 128 && nvec <= 4096 && p.n >= 4ll * sms) return {128, 1};
+    } else if (pass == VOCAB_STEP) {
+        hold = static_cast<int>(std::ceil(4.0 * sms * 16.0 * nvec / STEP_L2_BYTES));
+        if (hold > CLUSTER_MAX) threads = 512, hold = (hold + 1) / 2;
+    } else if (pass == VOCAB_BWD) {
+        threads = 512;
+        if (split) hold = (nvec + 512 * NV - 1) / (512 * NV);
+    }
+    const int fill = static_cast<int>(std::min<long long>(1024ll / threads * sms / p.n, nvec / threads));
+    if (split) return {threads, std::min(CLUSTER_MAX, std::max(hold, fill))};
+    int parts = 1;
+    while (parts < CLUSTER_MAX && (parts < hold || 2 * parts <= fill)) parts *= 2;
+    return {threads, parts};
+}
+
+template <class K>
+inline cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, int sms, cudaStream_t stream)
+{
+    const int rows = s.threads == 32 ? 4 : 1;
+    p.each = (p.vocab / e + s.parts - 1) / s.parts;
+    p.ahead = static_cast<int>(sms * 1024ll / (s.threads * rows) / s.parts * rows);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned int>((p.n + rows - 1) / rows), s.parts);
+    cfg.blockDim = dim3(s.threads * rows);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    if (cluster && s.parts > 1) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.y = s.parts;
+        attr[0].val.clusterDim.x = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+    return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+}  // namespace cola

@@ -253,3 +253,59 @@ def test_optional_outputs_and_trace():
     assert [r[0] for r in tr.records()] == ["token_logprob"]
     p = torch.softmax(X.double(), 1)
     assert (ent.double() + (p * p.log()).sum(1)).abs().max().item() <= 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(8200, 1), (9001, 20), (20011, 64), (33000, 128), (40009, 7)])
+def test_many_long_rows(V, k, dtype):
+    """Rows enough for the kernel that ranks one row while it reads the next,
+    every awkward order and mask among them."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V + k)
+    n = 2500
+    low = torch.finfo(H.TORCH[dtype]).min
+    x = torch.randn((n, V), generator=g, device="cuda") * 3
+    j = torch.arange(V, device="cuda", dtype=torch.float32)
+    special = [torch.zeros(V, device="cuda"), -j / 64, j / 64, torch.where(j % 4096 < 8, 5 + j / 1e4, -1.0),
+               torch.where(j < V // 2, 1.0, 2.0), torch.round(x[0]), torch.full((V,), -torch.inf, device="cuda"),
+               torch.where(j == V - 1, 3.0, -torch.inf), torch.where(j % 997 == 5, x[1], -torch.inf),
+               torch.full((V,), low, device="cuda"), torch.where(j < 3, x[2], low), torch.where(j < V - 2, -torch.inf, low),
+               torch.where(j % 2 == 0, 1.5, x[3].clamp(max=1.0)), torch.where(j % 50 == 0, 4.0, 0.0)]
+    for i, row in enumerate(special):
+        x[100 + 37 * i] = row
+    x = x.to(H.TORCH[dtype])
+    bad = [7, 1999, 2480]
+    x[bad[0], V // 2] = torch.nan
+    x[bad[1], :] = torch.nan
+    x[bad[2], 11] = torch.inf
+    t = torch.randint(0, V, (n,), generator=g, device="cuda")
+    d = cola.vocab_desc(n, V, dtype=dtype, temperature=0.75, k=k)
+    f = lambda *s: torch.full(s, -7.0, device="cuda")   # noqa: E731
+    logp, ent, top, stats = f(n), f(n), f(n, k), f(n, 4)
+    ids = torch.full((n, k), -7, dtype=torch.int64, device="cuda")
+    cola.cola_token_logprob_fwd(d, x, t, logp, ent, ids, top, stats)
+    z = x.double()
+    order = torch.where(torch.isnan(z), torch.inf, z)   # the one row with both holds its NaN alone
+    best = torch.sort(order, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(ids, best)
+    m = z.amax(1, keepdim=True)
+    m = torch.where(m == -torch.inf, 0.0, m)
+    w = (z - m) / 0.75
+    s = w.exp().sum(1, keepdim=True)
+    logs = torch.where(s == 0, 0.0, s.log())
+    lp = w - logs
+    p = lp.exp()
+    H_ref = -torch.where(p == 0, 0.0, p * lp).sum(1)
+
+    def near(a, b, tol):
+        b = torch.where(b.float().isinf(), b.float().double(), b)
+        assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.isinf(a), torch.isinf(b))
+        ok = torch.isfinite(b)
+        assert bool(((a[ok].double() - b[ok]).abs() <= 1e-5 + tol * b[ok].abs()).all())
+
+    near(logp, lp.gather(1, t[:, None])[:, 0], 1e-6)
+    near(top, lp.gather(1, best), 1e-6)
+    near(ent, torch.where(s[:, 0] == 0, 0.0, H_ref), 1e-5)
+    again = torch.empty_like(top)
+    cola.cola_token_logprob_fwd(d, x, t, logp, None, ids, again, None)
+    assert torch.equal(again.nan_to_num(5.0), top.nan_to_num(5.0)) and torch.equal(ids, best)
