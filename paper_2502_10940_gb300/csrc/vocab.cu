@@ -10,17 +10,20 @@ template <class T, bool ENT>
 cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    const Plan s = plan(p, E, VOCAB_FWD, false, p.k <= 64 ? 128 : p.k <= 128 ? 256 : 512, sms);
-    // one CTA: the k-th largest of its warps' maxima, or (counted by the CTA) of its threads';
-    // a cluster: of each warp a little more of the largest than k over the warps
+    const Plan s = plan(p, E, VOCAB_FWD, false, p.k, sms);
+    // a cluster's bound: of each warp, a little more of its largest than k over the warps
+    // (one CTA, with more than k warps too: the k-th largest of the warps' maxima)
     const int warps = s.threads / 32 * s.parts;
-    p.top_each = p.k <= warps ? 1 : s.parts == 1 ? (p.k <= s.threads ? 1 : 0) : (3 * p.k + 2 * warps - 1) / (2 * warps);
-    if (p.top_each > 24) p.top_each = 0;
-    p.top_before = p.top_each ? (p.k + p.top_each - 1) / p.top_each - 1 : 0;
+    p.top_each = p.k <= warps || s.parts == 1 ? 1 : (3 * p.k + 2 * warps - 1) / (2 * warps);
+    p.top_before = (p.k + p.top_each - 1) / p.top_each - 1;
     switch (s.threads) {
-    case 128: return launch_rows(token_logprob_top_kernel<T, 128, ENT>, p, E, s, true, 0, sms, stream);
-    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT>, p, E, s, true, 0, sms, stream);
-    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT>, p, E, s, true, 0, sms, stream);
+    case 32: return launch_rows(token_logprob_top_warp_kernel<T, ENT>, p, E, s, false, 0, sms, stream);
+    case 128:
+        // (more than 64 only of rows that 128 threads hold)
+        return p.k > 64 ? launch_rows(token_logprob_top_kernel<T, 128, ENT, true>, p, E, s, false, 0, sms, stream)
+                        : launch_rows(token_logprob_top_kernel<T, 128, ENT, false>, p, E, s, false, 0, sms, stream);
+    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT, false>, p, E, s, true, 0, sms, stream);
+    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT, false>, p, E, s, true, 0, sms, stream);
     }
 }
 
@@ -29,7 +32,7 @@ cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    const Plan s = plan(p, E, PASS, !cluster, 32, sms);
+    const Plan s = plan(p, E, PASS, !cluster, 0, sms);
     switch (s.threads) {
     case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, sms, stream);
     case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, sms, stream);

@@ -37,7 +37,7 @@ struct VocabParams {
     float* entropy;
     long long* top_ids;
     float* top_logp;
-    int top_each, top_before; // of each warp's largest, the one it gives; how many of those lie before the bound (each 0: no bound)
+    int top_each, top_before; // of each warp's largest maxima, the one it gives; how many of those lie before the bound
     const float* dlogp;
     const float* dentropy;
     // distillation

@@ -21,32 +21,39 @@ constexpr double STEP_L2_BYTES = 62e6;
 
 // A warp or four warps where their registers hold the row (NV vectors a
 // thread).  Longer rows take eight warps, so that the phases of four rows overlap
-// on an SM, tile after tile; sixteen where eight have too few threads for the
-// bound of the top k (`least`), and four where the top k of many rows of up to 4096
-// vectors, half of its work the same for every warp, has enough of 128 (116 us against
-// 129 us for the top 64 of 8192 x 32000; 130 against 105 for 2048 x 128000).  A step reads its row twice, the second time from L2:
-// as many CTAs share a row as keep the rows in flight within it, sixteen warps
-// where that would take more than a portable cluster's eight CTAs.  The
-// backward without a list (`split`) exchanges nothing: a CTA per tile.  All take more CTAs
-// where there are fewer rows than the device runs CTAs at once, down to a vector
-// per thread.  CTAs that form a cluster are a power of two: threes and sixes
-// leave SMs empty (390 us against 332 us for a step of 2048 x 262144 on six and four).
-inline Plan plan(const VocabParams& p, int e, int pass, bool split, int least, int sms)
+// on an SM, tile after tile.
+//   - A forward with the `top` k (0: without) takes sixteen where eight have too
+//     few threads for its bound, and four where many rows of up to 4096 vectors
+//     have enough of 128: much of its work is the same for every warp (116 us
+//     against 129 us for the top 64 of 8192 x 32000, but 130 us against 105 us for
+//     2048 x 128000).
+//   - A step reads its row twice, the second time from L2: as many CTAs share a row
+//     as keep the rows in flight within it, of sixteen warps where that would
+//     take more than a portable cluster's eight CTAs.
+//   - A backward takes sixteen warps, and without a list (`split`: its CTAs exchange
+//     nothing) a CTA per tile.
+//   - All take more CTAs a row where there are few rows, to two CTAs of eight warps
+//     per SM (one per SM, or as many as it can hold, took 0.3 to 1.5 us more),
+//     down to a vector per thread.
+// CTAs that form a cluster are a power of two: threes and sixes leave SMs empty
+// (390 us on six, 332 us on four for a step of 2048 x 262144).
+inline Plan plan(const VocabParams& p, int e, int pass, bool split, int top, int sms)
 {
     const int nvec = (p.vocab + e - 1) / e;
-    if (least <= 32 && nvec <= 32 * NV) return {32, 1};
-    if (least <= 128 && nvec <= 128 * NV) return {128, 1};
-    int threads = least <= 256 ? 256 : 512, hold = 1;
+    if (nvec <= 32 * NV) return {32, 1};
+    if (nvec <= 128 * NV) return {128, 1};
+    int threads = 256, hold = 1;
     if (pass == VOCAB_FWD) {
-        if (least == 128 && nvec <= 4096 && p.n >= 4ll * sms) return {128, 1};
+        if (top > 0 && top <= 64 && nvec <= 4096 && p.n >= 4ll * sms) return {128, 1};
+        if (top > 128) threads = 512;
     } else if (pass == VOCAB_STEP) {
         hold = static_cast<int>(std::ceil(4.0 * sms * 16.0 * nvec / STEP_L2_BYTES));
         if (hold > CLUSTER_MAX) threads = 512, hold = (hold + 1) / 2;
-    } else if (pass == VOCAB_BWD) {
+    } else {
         threads = 512;
         if (split) hold = (nvec + 512 * NV - 1) / (512 * NV);
     }
-    const int fill = static_cast<int>(std::min<long long>(1024ll / threads * sms / p.n, nvec / threads));
+    const int fill = static_cast<int>(std::min<long long>(512ll * sms / threads / p.n, nvec / threads));
     if (split) return {threads, std::min(CLUSTER_MAX, std::max(hold, fill))};
     int parts = 1;
     while (parts < CLUSTER_MAX && (parts < hold || 2 * parts <= fill)) parts *= 2;

@@ -109,17 +109,19 @@ struct Elem<float> {
                                    max_nan(__uint_as_float(d[j].z), __uint_as_float(d[j].w))));
         return m;
     }
-    // a bit for each element that reaches `limit` (or is NaN), and the place of a bit's element in its tile
-    static constexpr float LOWEST = -3.402823466e38f;
-    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], float limit)
+    // a bit for each element of the first `used` vectors that is not below `limit` (a NaN is not),
+    // NANS: that is a NaN; and the place of a bit's element in its tile
+    template <bool NANS = false>
+    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], int used, float limit)
     {
         unsigned int bits = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (j % 2 == 0 && j >= used) break;
             float x[4];
             unpack(d[j], x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) bits |= x[e] < limit ? 0u : 1u << (j * 4 + e);
+            for (int e = 0; e < 4; ++e) bits |= (NANS ? x[e] != x[e] : !(x[e] < limit)) ? 1u << (j * 4 + e) : 0u;
         }
         return bits;
     }
@@ -160,20 +162,24 @@ struct Elem<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    // as above; a word's two elements compared at once, the bits of words 0..15 and 16..31 in
-    // halves: low elements, then high ones
-    static constexpr float LOWEST = -3.38953139e38f;
-    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], float limit)
+    // as above; the limit's upper half (a key between two values of this type stands for the one above),
+    // a word's two elements compared at once, the bits of words 0..15 and 16..31 in halves:
+    // low elements, then high ones
+    template <bool NANS = false>
+    __device__ __forceinline__ static unsigned long long reach(const uint4 (&d)[NV], int used, float limit)
     {
-        const __nv_bfloat162 l = __float2bfloat162_rn(limit);   // exact: an element's value
+        const uint32_t half = __float_as_uint(limit) >> 16, both = half << 16 | half;
+        const __nv_bfloat162 l = *reinterpret_cast<const __nv_bfloat162*>(&both);
         uint32_t bits[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (j % 2 == 0 && j >= used) break;
             const uint32_t w[4] = {d[j].x, d[j].y, d[j].z, d[j].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t below = __hlt2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), l);
-                bits[j / 4] |= ~below & (0x00010001u << (j % 4 * 4 + i));
+                const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+                const uint32_t there = NANS ? __hneu2_mask(x, x) : ~__hlt2_mask(x, l);
+                bits[j / 4] |= there & (0x00010001u << (j % 4 * 4 + i));
             }
         }
         return static_cast<unsigned long long>(bits[1]) << 32 | bits[0];

@@ -31,6 +31,22 @@ __device__ __forceinline__ int key_id(uint32_t key) { return static_cast<int>(0x
 __device__ __forceinline__ float key_logit(unsigned long long key) { return key_value(static_cast<uint32_t>(key >> 32)); }
 __device__ __forceinline__ float key_logit(uint32_t key) { return key_value(key & 0x80000000u ? key & 0xffff0000u : key | 0xffffu); }
 
+constexpr uint32_t KEY_NEG_INF = 0x007fffffu, KEY_POS_INF = 0xff800000u;   // of the infinities; above the latter, NaNs
+
+// The lowest value key above `key` that a value of type T may have; the bits of a key that tell values apart.
+template <class T>
+__device__ __forceinline__ uint32_t next_key(uint32_t key) { return sizeof(T) == 2 ? (key & 0xffff0000u) + 0x10000u : key + 1; }
+template <class T>
+__device__ __forceinline__ bool same_key(uint32_t a, uint32_t b) { return sizeof(T) == 2 ? a >> 16 == b >> 16 : a == b; }
+
+// Bits of the elements of a tile whose value key is at least `from`.
+template <class T>
+__device__ __forceinline__ unsigned long long reach(const uint4 (&d)[NV], int used, uint32_t from)
+{
+    if (from > KEY_POS_INF) return Elem<T>::template reach<true>(d, used, 0.f);
+    return Elem<T>::template reach<false>(d, used, from <= KEY_NEG_INF ? NEG_INF : key_value(from));
+}
+
 // How many of `count` keys (zeros after them, to a multiple of 16 bytes) are
 // above `key`, the 16-byte words first, first + step, ... counted.
 __device__ __forceinline__ unsigned int count_above(const unsigned long long* keys, unsigned int count, unsigned long long key,
@@ -63,7 +79,10 @@ struct TopShared {
     unsigned int hist[256];
     unsigned int counts[CLUSTER_MAX];
     unsigned int count, digit, above, bound, local;
+    unsigned int part[2][16];           // counts of the warps, in turn
 };
+
+constexpr unsigned int RANK_MAX = 320;   // candidates that are counted, not sorted
 
 // Gathers at least k and at most CAND_MAX keys of a row in memory, the k
 // largest among them, by a radix search from the top digit that stops as soon
@@ -122,7 +141,9 @@ __device__ __noinline__ void sort_block(unsigned long long* key, int n)
     __syncthreads();
 }
 
-// The forward with the k most likely tokens.  At least k tokens reach the k-th
+// The forward with the k most likely tokens.  FEW: k is more than half of the
+// threads, whose registers hold the row; the tokens themselves are counted, by
+// their bits, for the bound.  Else at least k tokens reach the k-th
 // largest of the threads' maxima, and few more than k do where the largest are
 // spread over the threads (74 at k = 64 of 32000 in random order, 256 threads).
 // In a cluster, whose threads are too many and too far apart for that, each warp
@@ -131,7 +152,7 @@ __device__ __noinline__ void sort_block(unsigned long long* key, int n)
 // reach the bound are gathered, by their bits, from the registers (or, of a tile
 // before the last, read again), and each takes as its place the number of
 // candidates before it.
-template <class T, int GT, bool ENT>
+template <class T, int GT, bool ENT, bool FEW>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_top_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
@@ -170,9 +191,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     if (g.has_edges() && row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
     a = acc_warp<ENT>(a, P.c2);
     const int warps = G::W * g.parts;
-    const bool bounded = P.top_each > 0;
     uint32_t best = 0;
-    if (bounded && (cluster || P.k <= G::W)) {
+    if (cluster || P.k <= G::W) {
         uint32_t left = mine;
         for (int i = 0; i < P.top_each; ++i) {
             best = __reduce_max_sync(~0u, left);
@@ -188,119 +208,140 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         if (ENT && P.entropy) P.entropy[g.row] = H;
         if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
     }
-    unsigned int count = CAND_MAX + 1;
+    unsigned int count = 0;
     bool narrow = false;
     uint32_t* key32 = reinterpret_cast<uint32_t*>(top.key);
-    if (bounded) {
-        uint32_t bound = 0;
-        if (!cluster && P.k > G::W) {
-            // the k-th largest of the threads' maxima, from above to its upper 16 bits
-            const uint32_t most = value_key(m);
-            // (its upper bits, where few more than k reach them)
-            for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1) {
-                if ((bound | bit) > most) continue;
-                const int n = __syncthreads_count(mine >= (bound | bit));
-                if (n >= P.k) bound |= bit;
-                if (n >= P.k && n <= P.k + (P.k >> 3) + 2) break;
-            }
-        } else {
-            // the warps' value with top_before before it: each warp counts for one of each CTA
-            uint32_t all[(CLUSTER_MAX * G::W + 31) / 32];
-#pragma unroll
-            for (int q = 0; q < (CLUSTER_MAX * G::W + 31) / 32; ++q)
-                all[q] = g.lane + 32 * q < warps ? __float_as_uint(slots[g.lane + 32 * q].w) : 0u;
-#pragma unroll
-            for (int r = 0; r < CLUSTER_MAX; ++r) {
-                if (r < g.parts) {
-                    const int i = r * G::W + g.warp;
-                    const uint32_t v = __float_as_uint(slots[i].w);
-                    unsigned int n = 0;
-#pragma unroll
-                    for (int q = 0; q < (CLUSTER_MAX * G::W + 31) / 32; ++q) n += all[q] > v || (all[q] == v && g.lane + 32 * q < i);
-                    if (__reduce_add_sync(~0u, n) == static_cast<unsigned int>(P.top_before) && g.lane == 0) top.bound = v;
-                }
-            }
-            __syncthreads();
-            bound = top.bound;
-        }
-        // a bound of -inf: what lies above it here; the first of the -inf tokens follow below
-        const float limit = bound <= value_key(NEG_INF) ? Elem<T>::LOWEST : key_value(bound);
-        const unsigned int share = CAND_MAX >> (31 - __clz(g.parts));   // clusters are powers of two
-        const uint32_t list = cluster ? mapa_shared(smem_u32(top.found + g.rank * share), 0) : 0;
-        const auto take = [&](int id) {
-            const unsigned int at = atomicAdd(&top.local, 1u);
-            if (at < share) {
-                if (cluster) st_shared_cluster_u32(list + 4 * at, id);
-                else top.found[at] = id;
-            }
-        };
-        const auto take_tile = [&](int t) {
-            unsigned long long bits = Elem<T>::reach(d, limit);
-            while (bits) {
-                const int b = Elem<T>::place(__ffsll(bits) - 1);
-                bits &= bits - 1;
-                if (b / E * GT < part.left(g, t)) take(row.head + (part.at(g, t) + b / E * GT) * E + b % E);
-            }
-        };
-        if (mine >= bound) {   // each thread the tile of its largest, that of its second, rarely all others
-            if (part.tiles > 1) part.reload(row, g, tile, d);
-            take_tile(tile);
-            if (second >= bound) {
-                part.reload(row, g, tile2, d);
-                take_tile(tile2);
-                for (int t = 0; third >= bound && t < part.tiles; ++t) {
-                    if (t == tile || t == tile2) continue;
-                    part.reload(row, g, t, d);
-                    take_tile(t);
-                }
-            }
-        }
-        if (edge && !(xe < limit)) take(row.edge(g.lane));
+    uint32_t bound = 0;
+    const uint32_t most = value_key(m);
+    int turn = 0;
+    const auto reached = [&](uint32_t from) -> int {
+        if constexpr (!FEW) return __syncthreads_count(mine >= from);
+        const int n = __reduce_add_sync(~0u, __popcll(reach<T>(d, part.used(0), from)) + (edge && value_key(xe) >= from));
+        if (g.lane == 0) top.part[turn][g.warp] = n;
         __syncthreads();
-        if (cluster) {
-            if (g.tid == 0) st_shared_cluster_u32(mapa_shared(smem_u32(top.counts + g.rank), 0), top.local);
-            cluster_sync();
-            if (g.rank != 0) return;
-            count = 0;
-            for (int r = 0; r < g.parts; ++r) count = top.counts[r] > share ? 2 * CAND_MAX : count + top.counts[r];
-        } else {
-            count = top.local;
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < G::W; ++w) all += top.part[turn][w];
+        turn ^= 1;
+        return all;
+    };
+    if (!cluster && P.k > G::W) {
+        // the k-th largest of the threads' maxima, or of the tokens: its upper 16
+        // bits from above, as far as more than a few above k reach them
+        for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1) {
+            if ((bound | bit) > most) continue;
+            const int n = reached(bound | bit);
+            if (n >= P.k) bound |= bit;
+            if (n >= P.k && n <= P.k + (P.k >> 3) + 2) break;
         }
-        const auto put = [&](unsigned int at, float x, int id) {
-            if (narrow) key32[at] = narrow_key(x, id);
-            else top.key[at] = token_key(x, id);
-        };
-        narrow = sizeof(T) == 2 && P.vocab <= 65536 && count <= 128;
-        if (count <= CAND_MAX) {
-            for (unsigned int c = g.tid; c < count; c += GT) {
-                unsigned int at = c;
-                for (int r = 0; cluster && r < g.parts - 1 && at >= r * share + top.counts[r]; ++r) at += share - top.counts[r];
-                const int id = top.found[at];
-                put(c, Elem<T>::get(row.p + id), id);
+    } else {
+        // the warps' value with top_before before it: each warp counts for one of each CTA
+        uint32_t all[(CLUSTER_MAX * G::W + 31) / 32];
+#pragma unroll
+        for (int q = 0; q < (CLUSTER_MAX * G::W + 31) / 32; ++q)
+            all[q] = g.lane + 32 * q < warps ? __float_as_uint(slots[g.lane + 32 * q].w) : 0u;
+#pragma unroll
+        for (int r = 0; r < CLUSTER_MAX; ++r) {
+            if (r < g.parts) {
+                const int i = r * G::W + g.warp;
+                const uint32_t v = __float_as_uint(slots[i].w);
+                unsigned int n = 0;
+#pragma unroll
+                for (int q = 0; q < (CLUSTER_MAX * G::W + 31) / 32; ++q) n += all[q] > v || (all[q] == v && g.lane + 32 * q < i);
+                if (__reduce_add_sync(~0u, n) == static_cast<unsigned int>(P.top_before) && g.lane == 0) top.bound = v;
             }
-        }
-        if (count < static_cast<unsigned int>(P.k) && g.warp == 0) {
-            // fewer than k tokens above -inf: the lowest ids of the others follow,
-            // all of them among the first k + count ids
-            unsigned int n = count;
-            for (int id = g.lane; n < static_cast<unsigned int>(P.k); id += 32) {
-                const bool none = id < P.vocab && Elem<T>::get(row.p + id) == NEG_INF;
-                const unsigned int set = __ballot_sync(~0u, none);
-                const unsigned int at = n + __popc(set & ((1u << g.lane) - 1));
-                if (none && at < static_cast<unsigned int>(P.k)) put(at, NEG_INF, id);
-                n += __popc(set);
-            }
-        }
-        count = max(count, static_cast<unsigned int>(P.k));
-        // zeros after the last key
-        if (count <= CAND_MAX - 4 && g.tid < 4) {
-            if (narrow) key32[count + g.tid] = 0;
-            else top.key[count + g.tid] = 0;
         }
         __syncthreads();
-    } else if (g.rank != 0) {
-        return;
+        bound = top.bound;
     }
+    const unsigned int share = CAND_MAX >> (31 - __clz(g.parts));   // clusters are powers of two
+    const uint32_t list = cluster ? mapa_shared(smem_u32(top.found + g.rank * share), 0) : 0;
+    const auto take = [&](int id) {
+        const unsigned int at = atomicAdd(&top.local, 1u);
+        if (at < share) {
+            if (cluster) st_shared_cluster_u32(list + 4 * at, id);
+            else top.found[at] = id;
+        }
+    };
+    // a bound of -inf: what lies above it, then the first of the -inf tokens
+    bool above = bound <= KEY_NEG_INF;
+    bound = max(bound, KEY_NEG_INF);
+    for (;;) {
+        const uint32_t from = above ? next_key<T>(bound) : bound;
+        if (mine >= from && from >= KEY_NEG_INF) {   // (0: nothing lies above a NaN)
+            // each thread the tile of its largest, that of its second, rarely all others
+            int next = 0;
+            for (int i = 0, t = tile;; ++i) {
+                if (part.tiles > 1) part.reload(row, g, t, d);
+                unsigned long long bits = reach<T>(d, NV, from);
+                while (bits) {
+                    const int b = Elem<T>::place(__ffsll(bits) - 1);
+                    bits &= bits - 1;
+                    if (b / E * GT < part.left(g, t)) take(row.head + (part.at(g, t) + b / E * GT) * E + b % E);
+                }
+                if (i == 0) {
+                    if (second < from) break;
+                    t = tile2;
+                } else {
+                    if (third < from) break;
+                    while (next == tile || next == tile2) ++next;
+                    if (next >= part.tiles) break;
+                    t = next++;
+                }
+            }
+        }
+        if (edge && value_key(xe) >= from && from >= KEY_NEG_INF) take(row.edge(g.lane));
+        __syncthreads();
+        if (cluster || above || top.local <= CAND_MAX) break;
+        // many tie: the whole bound, what lies above it, and the lowest ids at it
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+            if (!(bound & bit) && (bound | bit) <= most && reached(bound | bit) >= P.k) bound |= bit;
+        __syncthreads();
+        if (g.tid == 0) top.local = 0;
+        __syncthreads();
+        above = true;
+    }
+    if (cluster) {
+        if (g.tid == 0) st_shared_cluster_u32(mapa_shared(smem_u32(top.counts + g.rank), 0), top.local);
+        cluster_sync();
+        if (g.rank != 0) return;
+        count = 0;
+        for (int r = 0; r < g.parts; ++r) count = top.counts[r] > share ? 2 * CAND_MAX : count + top.counts[r];
+    } else {
+        count = top.local;
+    }
+    const auto put = [&](unsigned int at, float x, int id) {
+        if (narrow) key32[at] = narrow_key(x, id);
+        else top.key[at] = token_key(x, id);
+    };
+    narrow = sizeof(T) == 2 && P.vocab <= 65536 && max(count, static_cast<unsigned int>(P.k)) <= RANK_MAX;
+    if (count <= CAND_MAX) {
+        for (unsigned int c = g.tid; c < count; c += GT) {
+            unsigned int at = c;
+            for (int r = 0; cluster && r < g.parts - 1 && at >= r * share + top.counts[r]; ++r) at += share - top.counts[r];
+            const int id = top.found[at];
+            put(c, Elem<T>::get(row.p + id), id);
+        }
+    }
+    if (count < static_cast<unsigned int>(P.k) && g.warp == 0) {
+        // fewer than k tokens lie above the bound: the lowest ids of those at it follow
+        unsigned int n = count;
+        for (int id = g.lane; n < static_cast<unsigned int>(P.k) && id - g.lane < P.vocab; id += 32) {
+            const float x = id < P.vocab ? Elem<T>::get(row.p + id) : 0.f;
+            const bool at_bound = id < P.vocab && same_key<T>(value_key(x), bound);
+            const unsigned int set = __ballot_sync(~0u, at_bound);
+            const unsigned int at = n + __popc(set & ((1u << g.lane) - 1));
+            if (at_bound && at < static_cast<unsigned int>(P.k)) put(at, x, id);
+            n += __popc(set);
+        }
+    }
+    count = max(count, static_cast<unsigned int>(P.k));
+    // zeros after the last key
+    if (count <= CAND_MAX - 4 && g.tid < 4) {
+        if (narrow) key32[count + g.tid] = 0;
+        else top.key[count + g.tid] = 0;
+    }
+    __syncthreads();
     if (count > CAND_MAX) {
         top_radix<T, GT>(row.p, P.vocab, P.k, top);
         count = top.count;
@@ -310,25 +351,187 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         P.top_logp[g.row * P.k + place] = (key_logit(key) - m0) * P.c - logs;
     };
     const int n = count <= 2 ? static_cast<int>(count) : 1 << (32 - __clz(count - 1));
-    // counting takes count^2 / 32 steps of all warps together, sorting 30 to 55 barriers
-    if (n <= min(GT, 256)) {
+    // counting takes count^2 / 32 steps of all warps together, sorting 45 to 55 barriers
+    if (count <= RANK_MAX) {
         // `share` neighbouring threads count for one candidate
-        const int log_share = min(5, __clz(n) - __clz(GT));
-        const unsigned int share = 1u << log_share, c = g.tid >> log_share, first = g.tid & (share - 1);
-        if (g.warp * 32u >> log_share < count) {   // the warp has candidates
-            const auto rank = [&](const auto* keys) {
+        const int log_share = n <= GT ? min(5, __clz(n) - __clz(GT)) : 0;
+        const unsigned int share = 1u << log_share, first = g.tid & (share - 1);
+        const auto rank = [&](const auto* keys) {
+            for (unsigned int c0 = g.warp * 32u >> log_share; c0 < count; c0 += GT) {   // the warp has candidates
+                const unsigned int c = c0 + (g.lane >> log_share);
                 const auto key = keys[min(c, count - 1)];
                 unsigned int before = count_above(keys, count, key, first, share);
                 for (unsigned int i = share / 2; i; i /= 2) before += __shfl_xor_sync(~0u, before, i);
                 if (c < count && first == 0 && before < static_cast<unsigned int>(P.k)) give(key, before);
-            };
-            if (narrow) rank(key32);
-            else rank(top.key);
-        }
+            }
+        };
+        if (narrow) rank(key32);
+        else rank(top.key);
     } else {
         for (int i = count + g.tid; i < n; i += GT) top.key[i] = 0;
         sort_block<GT>(top.key, n);
         for (int i = g.tid; i < P.k; i += GT) give(top.key[i], i);
+    }
+}
+
+// Sorts 32 R keys falling in one warp: key r 32 + lane in register r.
+template <class K, int R>
+__device__ __forceinline__ void sort_warp(K (&key)[R], int lane)
+{
+#pragma unroll
+    for (int size = 2; size <= 32 * R; size *= 2) {
+#pragma unroll
+        for (int step = size / 2; step; step /= 2) {
+            if (step >= 32) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int o = r ^ step / 32;
+                    if (o > r) {
+                        const bool falling = (r * 32 & size) == 0;
+                        const K a = key[r], b = key[o];
+                        key[r] = falling ? max(a, b) : min(a, b);
+                        key[o] = falling ? min(a, b) : max(a, b);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const K o = __shfl_xor_sync(~0u, key[r], step);
+                    const int i = r * 32 + lane;
+                    const bool larger = ((i & size) == 0) == ((i & step) == 0);   // this lane keeps the larger
+                    key[r] = larger ? max(key[r], o) : min(key[r], o);
+                }
+            }
+        }
+    }
+}
+
+template <class T>
+struct WarpKey {
+    using K = unsigned long long;
+    __device__ static K make(float x, int j) { return token_key(x, j); }
+};
+template <>
+struct WarpKey<__nv_bfloat16> {
+    using K = uint32_t;   // rows of a warp have fewer than 2^16 tokens
+    __device__ static K make(float x, int j) { return narrow_key(x, j); }
+};
+
+// The same for rows that one warp holds: the bound is the k-th largest of the
+// lanes' maxima where these are enough (k <= 16), else of the tokens themselves,
+// counted by their bits; candidates are gathered and sorted within the warp.
+template <class T, bool ENT>
+__global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const VocabParams P)
+{
+    constexpr int E = Elem<T>::E, CAND = VOCAB_MAX_K;
+    using G = Group<32>;
+    using K = typename WarpKey<T>::K;
+    __shared__ K keys[G::ROWS][CAND];
+    const G g;
+    if (g.row >= P.n) return;
+    const int lane = g.lane;
+    const Row<T> row(static_cast<const T*>(P.logits) + g.row * P.ld, P.vocab);
+    const Part<T, 32> part(row, g, P.each);
+    uint4 d[NV];
+    part.load(row, g, 0, d);
+    const bool edge = lane < row.edges();
+    const float xe = edge ? Elem<T>::get(row.p + row.edge(lane)) : NEG_INF;
+    const long long y = P.targets ? P.targets[g.row] : -1;
+    const bool there = y >= 0 && y < P.vocab;
+    const float xy = there ? Elem<T>::get(row.p + y) : 0.f;
+    const int used = part.used(0);
+    const float mt = Elem<T>::max_of(d);
+    Acc a = acc_tile<T, ENT>(d, used, mt, P.c2);
+    if (row.edges() > 0) a = acc_merge<ENT>(a, acc_one(xe), P.c2);
+    a = acc_warp<ENT>(a, P.c2);
+    const float m = a.m, m0 = m == NEG_INF ? 0.f : m, logs = m == NEG_INF ? 0.f : logf(a.s);
+    if (lane == 0) {
+        const float H = ENT && m != NEG_INF ? logs - LN2 * (a.t / a.s) : 0.f;
+        if (P.logp) P.logp[g.row] = there ? (xy - m0) * P.c - logs : 0.f;
+        if (ENT && P.entropy) P.entropy[g.row] = H;
+        if (P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, H, 0.f);
+    }
+    const uint32_t most = value_key(m);
+    const auto reached = [&](uint32_t from) -> int {
+        return __reduce_add_sync(~0u, __popcll(reach<T>(d, used, from)) + (edge && value_key(xe) >= from));
+    };
+    const auto gather = [&](uint32_t from) -> int {
+        unsigned long long bits = reach<T>(d, used, from);
+        bool also = edge && value_key(xe) >= from;
+        int count = 0;
+        while (__any_sync(~0u, bits != 0 || also)) {
+            int id = -1;
+            if (bits) {
+                const int b = Elem<T>::place(__ffsll(bits) - 1);
+                bits &= bits - 1;
+                if (b / E * 32 < part.left(g, 0)) id = row.head + (part.at(g, 0) + b / E * 32) * E + b % E;
+            } else if (also) {
+                also = false;
+                id = row.edge(lane);
+            }
+            const unsigned int set = __ballot_sync(~0u, id >= 0);
+            const int at = count + __popc(set & ((1u << lane) - 1));
+            if (id >= 0 && at < CAND) keys[g.slot][at] = WarpKey<T>::make(Elem<T>::get(row.p + id), id);
+            count += __popc(set);
+        }
+        return count;
+    };
+    uint32_t bound = 0;
+    if (P.k <= 16) {
+        uint32_t best[1] = {max(value_key(mt), value_key(xe))};
+        sort_warp(best, lane);
+        bound = __shfl_sync(~0u, best[0], P.k - 1);
+    } else {
+        for (uint32_t bit = 0x80000000u; bit > 0x8000u; bit >>= 1) {
+            if ((bound | bit) > most) continue;
+            const int n = reached(bound | bit);
+            if (n >= P.k) bound |= bit;
+            if (n >= P.k && n <= P.k + (P.k >> 3) + 2) break;
+        }
+    }
+    // a bound of -inf: what lies above it, then the first of the -inf tokens
+    int count = gather(bound <= KEY_NEG_INF ? next_key<T>(KEY_NEG_INF) : bound);
+    bound = max(bound, KEY_NEG_INF);
+    if (count > CAND) {
+        // many tie: the k-th largest itself, fewer than k above it, and the lowest ids at it
+        bound = 0;
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+            if ((bound | bit) <= most && reached(bound | bit) >= P.k) bound |= bit;
+        count = bound == 0xffffffffu ? 0 : gather(next_key<T>(bound));   // (nothing lies above a NaN)
+    }
+    for (int j0 = 0; count < P.k && j0 < P.vocab; j0 += 32) {
+        const int j = j0 + lane;
+        const float x = j < P.vocab ? Elem<T>::get(row.p + j) : 0.f;
+        const bool at_bound = j < P.vocab && same_key<T>(value_key(x), bound);
+        const unsigned int set = __ballot_sync(~0u, at_bound);
+        const int at = count + __popc(set & ((1u << lane) - 1));
+        if (at_bound && at < P.k) keys[g.slot][at] = WarpKey<T>::make(x, j);
+        count = min(count + __popc(set), P.k);
+    }
+    __syncwarp();
+    const auto sorted = [&](auto& key) {
+        constexpr int R = sizeof(key) / sizeof(key[0]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) key[i] = i * 32 + lane < count ? keys[g.slot][i * 32 + lane] : K(0);
+        sort_warp(key, lane);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int place = i * 32 + lane;
+            if (place < P.k) {
+                P.top_ids[g.row * P.k + place] = key_id(key[i]);
+                P.top_logp[g.row * P.k + place] = (key_logit(key[i]) - m0) * P.c - logs;
+            }
+        }
+    };
+    if (count <= 32) {
+        K key[1];
+        sorted(key);
+    } else if (count <= 128) {
+        K key[4];
+        sorted(key);
+    } else {
+        K key[8];
+        sorted(key);
     }
 }
 
