@@ -10,7 +10,7 @@ template <class T, bool ENT>
 cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    const Plan s = plan(p, E, VOCAB_FWD, false, p.k, sms);
+    const Plan s = plan(p, E, VOCAB_FWD, false, p.k, 0, sms);
     // a cluster's bound: of each warp, a little more of its largest than k over the warps
     // (one CTA, with more than k warps too: the k-th largest of the warps' maxima)
     const int warps = s.threads / 32 * s.parts;
@@ -32,7 +32,7 @@ cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
     const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    const Plan s = plan(p, E, PASS, !cluster, 0, sms);
+    const Plan s = plan(p, E, PASS, !cluster, 0, 0, sms);
     switch (s.threads) {
     case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, sms, stream);
     case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, sms, stream);

@@ -37,7 +37,7 @@ cudaError_t distill_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t st
 template <class T, int PASS>
 cudaError_t distill(VocabParams p, int sms, cudaStream_t stream)
 {
-    const Plan s = plan(p, Elem<T>::E, PASS, false, 0, sms);
+    const Plan s = plan(p, Elem<T>::E, PASS, false, 0, p.k, sms);
     switch (s.threads) {
     case 32: return distill_rows<T, PASS, 32>(p, s, sms, stream);
     case 128: return distill_rows<T, PASS, 128>(p, s, sms, stream);

@@ -5,6 +5,14 @@
 namespace cola {
 
 // ------------------------------------------------- token log probabilities
+// Bound by HBM: a row is read once (a step's second read hits L2), a gradient
+// written once.  Per element the forward takes 3.5 instructions (half a packed
+// maximum, an unpacking, half a packed fused product and sum each, an exponential)
+// and the gradient as many; an SM has about 11 for each bf16 logit that HBM gives
+// it.  bf16 logits, 32000 a row: forward of 8192 rows 77 us (6.8 TB/s), step of
+// 32768 rows 598 us (7.0 TB/s); fp32 backward with entropy of 4096 x 65537, rows
+// unaligned, 319 us (6.7 TB/s).
+//
 // The gradient of one CTA's share of a row.  H: with the entropy's term,
 //   c p (-g - h (logp + H)) = 2^y (A + B y),   y = c2 x - base.b.
 template <class T, int PASS, int GT, bool ENT>
