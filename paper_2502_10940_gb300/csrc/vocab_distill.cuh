@@ -11,7 +11,7 @@ namespace cola {
 __device__ __forceinline__ float excess(float r)
 {
     if (fabsf(r) < 0.3f)
-        return r * r * (0.5f - r * (1.f / 6 - r * (1.f / 24 - r * (1.f / 120 - r * (1.f / 720 - r / 5040)))));
+        return __fmul_rn(r * r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(r, -1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f));
     return r + expm1f(-r);
 }
 
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
                         atomicOr(listed + tile * GT + v % GT, static_cast<Bits<T>>(1) << (v % G::TILE / GT * E + at % E));
                 }
             }
-            const float u = there ? (i == g.tid ? u0 : P.t_vals[g.row * P.k + i]) * P.t_c - shift : NEG_INF;
+            const float u = there ? fmaf(i == g.tid ? u0 : P.t_vals[g.row * P.k + i], P.t_c, -shift) : NEG_INF;
             list.id[i] = id;
             list.u[i] = u;
             um = max_nan(um, u);
@@ -204,15 +204,16 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
             logs = m == NEG_INF ? 0.f : logf(s);
             logr = mr == NEG_INF ? 0.f : logf(sr);
         }
-        logpr = (mr - m0) * P.c + logr - logs;
+        logpr = __fadd_rn(fmaf(mr - m0, P.c, logr), -logs);
         const float u_top = P.rest || us == 0.f ? 0.f : um, log_us = P.rest || us == 0.f ? 0.f : logf(us);
         for (int i = g.tid; i < P.k; i += GT) {
             if (list.id[i] < 0) continue;
             const float logq = (list.u[i] - u_top) - log_us, q = us == 0.f ? 0.f : expf(logq);
-            const float logp = (list.x[i] - m0) * P.c - logs, p = expf(logp);
+            // (roundings written out: the same loss from every pass)
+            const float logp = fmaf(list.x[i] - m0, P.c, -logs), p = expf(logp);
             if (PASS != VOCAB_BWD) {
-                if (entry) kl += q > 0.f ? q * excess(logq - logp) : p;
-                else kl += q > 0.f ? q * (logq - logp) : 0.f * q;
+                const float r = __fadd_rn(logq, -logp);
+                kl = __fadd_rn(kl, entry ? (q > 0.f ? __fmul_rn(q, excess(r)) : p) : q > 0.f ? __fmul_rn(q, r) : 0.f * q);
             }
             if (PASS != VOCAB_FWD) list.u[i] = wt * ((entry ? 1.f : Q) * p - q);
         }
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
     if (PASS != VOCAB_BWD && g.rank == 0 && g.tid == 0) {
         kl = 0.f;
         for (int i = 0; i < G::W && i * 32 < P.k; ++i) kl += list.sum[i];
-        if (entry) kl += qr * excess(log1pf(-Q) - logpr);
+        if (entry) kl = __fadd_rn(kl, __fmul_rn(qr, excess(__fadd_rn(log1pf(-Q), -logpr))));
         P.loss[g.row] = P.temperature * P.temperature * kl;
         if (PASS == VOCAB_FWD && P.stats) reinterpret_cast<float4*>(P.stats)[g.row] = make_float4(m, logs, mr, logr);
     }

@@ -195,3 +195,56 @@ def test_trace():
     assert [r[0] for r in tr.records()] == ["topk_distill"]
     ref = -torch.log_softmax(X.double(), 1)[:, 0]
     assert (loss.double() - ref).abs().max().item() <= 2e-5
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_vocabulary(dtype, rest):
+    rng = np.random.default_rng(13)
+    V = 1 << 20
+    x = H.logits(rng, 1, V, dtype)
+    ids, vals, lse = H.teacher(rng, x, 256, 1.0)
+    compare(x, ids, vals, lse if rest else None, dtype, 1.0, 1.0, rest, [0.5])
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,k", [(2600, 700, 200), (2600, 700, 9), (1500, 5003, 64), (1300, 20011, 40), (40, 600, 200)])
+def test_many_rows(n, V, k, dtype, rest):
+    """More rows than CTAs run at once, by the definition on the GPU in 64 bits."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + V + k)
+    T = 1.5
+    x = (torch.randn((n, V), generator=g, device="cuda") * 2).to(H.TORCH[dtype])
+    t = x.float() * 0.9 + torch.randn((n, V), generator=g, device="cuda")
+    top = torch.topk(t, k, dim=1)
+    ids, vals = top.indices.contiguous(), top.values.contiguous()
+    lse = torch.logsumexp(t / T, 1) if rest else None
+    w = torch.randn(n, generator=g, device="cuda")
+    d = cola.vocab_desc(n, V, dtype=dtype, temperature=T, k=k, rest=rest, teacher_temperature=T)
+    loss, loss2, stats, dx, dx2 = (torch.full(s, float("nan"), device="cuda") for s in ((n,), (n,), (n, 4), (n, V), (n, V)))
+    dx, dx2 = dx.to(x.dtype), dx2.to(x.dtype)
+    cola.cola_topk_distill_fwd(d, x, ids, vals, lse, loss, stats)
+    cola.cola_topk_distill_bwd(d, x, ids, vals, lse, stats, w, dx)
+    cola.cola_topk_distill_step(d, x, ids, vals, lse, w, loss2, dx2)
+    assert torch.equal(loss, loss2)
+    lp = torch.log_softmax(x.double() / T, 1)
+    u = vals.double() / T
+    q = (u - lse.double()[:, None]).exp() if rest else torch.softmax(u, 1)
+    logq = u - lse.double()[:, None] if rest else torch.log_softmax(u, 1)
+    out = torch.ones_like(lp).scatter_(1, ids, 0.0)
+    kl = (q * (logq - lp.gather(1, ids))).sum(1)
+    want = torch.zeros_like(lp).scatter_(1, ids, q)
+    lpr = torch.logsumexp(torch.where(out > 0, lp, -torch.inf), 1)
+    r = (lp - lpr[:, None]).exp() * out
+    if rest:
+        qr = (1 - q.sum(1)).clamp(min=0.0)
+        kl = kl + torch.where(qr > 0, qr * (qr.clamp(min=1e-300).log() - lpr), 0.0)
+        want = want + qr[:, None] * r
+    ref = w.double()[:, None] * T * (want.sum(1, keepdim=True) * lp.exp() - want)
+    ref_loss = T * T * kl
+    assert bool(((loss.double() - ref_loss).abs() <= T * T * 2e-5 + 1e-5 * ref_loss.abs()).all())
+    # as in check_distill_grad
+    tol = w.double().abs()[:, None] * T * (4e-6 * r + 2e-5 * (1 - out)) + (2e-5 + (2.0 ** -8 if dtype == "bf16" else 0.0)) * ref.abs() + 1e-37
+    for got in (dx, dx2):
+        assert bool(((got.double() - ref).abs() <= tol).all())

@@ -309,3 +309,29 @@ def test_many_long_rows(V, k, dtype):
     again = torch.empty_like(top)
     cola.cola_token_logprob_fwd(d, x, t, logp, None, ids, again, None)
     assert torch.equal(again.nan_to_num(5.0), top.nan_to_num(5.0)) and torch.equal(ids, best)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_vocabulary(dtype):
+    rng = np.random.default_rng(12)
+    V = 1 << 20
+    x = H.logits(rng, 2, V, dtype)
+    compare(x, [3, V - 1], dtype, 1.0, 256, [1.0, -0.5], [0.25, 0.5])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(250, 250), (640, 17), (1000, 200), (2290, 149), (3333, 256)])
+def test_many_short_rows_with_long_lists(V, k, dtype):
+    """k near or beyond the threads that hold a row, ties and masks among them."""
+    rng = np.random.default_rng(V + k)
+    x = H.logits(rng, 300, V, dtype)
+    x[7] = 0.0
+    x[8, k:] = -np.inf
+    x[9, 3:] = -np.inf
+    x[10] = np.round(x[10])
+    x[11] = np.arange(V) / 64.0
+    x[12, V // 2] = np.nan
+    x[13, : k + 1] = np.nan
+    x[14] = np.where(np.arange(V) % 3 == 0, 1.0, -np.inf)
+    x = H.rounded(x, dtype)
+    compare(x, rng.integers(0, V, 300), dtype, 1.5, k, None, None)
