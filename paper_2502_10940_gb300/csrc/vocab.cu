@@ -1,54 +1,37 @@
-// Launchers of the token log probabilities (vocab_logprob.cuh, vocab_top.cuh).
+// Launchers of the token log probabilities (vocab_logprob.cuh).
 #include "vocab_logprob.cuh"
 #include "vocab_plan.cuh"
-#include "vocab_top.cuh"
 
 namespace cola {
 namespace {
 
-template <class T, bool ENT>
-cudaError_t logprob_top(VocabParams& p, int sms, cudaStream_t stream)
+template <class T, int PASS, bool ENT, bool APART>
+cudaError_t logprob_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    const Plan s = plan(p, E, VOCAB_FWD, false, p.k, 0, sms);
-    // a cluster's bound: of each warp, a little more of its largest than k over the warps
-    // (one CTA, with more than k warps too: the k-th largest of the warps' maxima)
-    const int warps = s.threads / 32 * s.parts;
-    p.top_each = p.k <= warps || s.parts == 1 ? 1 : (3 * p.k + 2 * warps - 1) / (2 * warps);
-    p.top_before = (p.k + p.top_each - 1) / p.top_each - 1;
+    const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
     switch (s.threads) {
-    case 32: return launch_rows(token_logprob_top_warp_kernel<T, ENT>, p, E, s, false, 0, sms, stream);
-    case 128:
-        // (more than 64 only of rows that 128 threads hold)
-        return p.k > 64 ? launch_rows(token_logprob_top_kernel<T, 128, ENT, true>, p, E, s, false, 0, sms, stream)
-                        : launch_rows(token_logprob_top_kernel<T, 128, ENT, false>, p, E, s, false, 0, sms, stream);
-    case 256: return launch_rows(token_logprob_top_kernel<T, 256, ENT, false>, p, E, s, true, 0, sms, stream);
-    default: return launch_rows(token_logprob_top_kernel<T, 512, ENT, false>, p, E, s, true, 0, sms, stream);
+    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT, false>, p, E, s, cluster, 0, sms, stream);
+    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT, APART>, p, E, s, cluster, 0, sms, stream);
+    case 256: return launch_rows(token_logprob_kernel<T, PASS, 256, ENT, APART>, p, E, s, cluster, 0, sms, stream);
+    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT, APART>, p, E, s, cluster, 0, sms, stream);
     }
 }
 
 template <class T, int PASS, bool ENT>
 cudaError_t logprob(VocabParams& p, int sms, cudaStream_t stream)
 {
-    constexpr int E = Elem<T>::E;
-    const bool cluster = PASS != VOCAB_BWD;   // the backward's CTAs have nothing to exchange
-    const Plan s = plan(p, E, PASS, !cluster, 0, 0, sms);
-    switch (s.threads) {
-    case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT>, p, E, s, cluster, 0, sms, stream);
-    case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT>, p, E, s, cluster, 0, sms, stream);
-    case 256: return launch_rows(token_logprob_kernel<T, PASS, 256, ENT>, p, E, s, cluster, 0, sms, stream);
-    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT>, p, E, s, cluster, 0, sms, stream);
-    }
+    const Plan s = plan(p, Elem<T>::E, PASS, PASS == VOCAB_BWD, 0, 0, sms);
+    if constexpr (PASS != VOCAB_FWD)
+        if (lies_apart(p, Elem<T>::E)) return logprob_rows<T, PASS, ENT, true>(p, s, sms, stream);
+    return logprob_rows<T, PASS, ENT, false>(p, s, sms, stream);
 }
 
 template <class T>
 cudaError_t logprob_pass(VocabParams p, int pass, int sms, cudaStream_t stream)
 {
-    if (pass == VOCAB_FWD) {
-        const bool ent = p.entropy || p.stats;
-        if (p.k > 0) return ent ? logprob_top<T, true>(p, sms, stream) : logprob_top<T, false>(p, sms, stream);
-        return ent ? logprob<T, VOCAB_FWD, true>(p, sms, stream) : logprob<T, VOCAB_FWD, false>(p, sms, stream);
-    }
+    if (pass == VOCAB_FWD)
+        return p.entropy || p.stats ? logprob<T, VOCAB_FWD, true>(p, sms, stream) : logprob<T, VOCAB_FWD, false>(p, sms, stream);
     if (pass == VOCAB_STEP)
         return p.entropy || p.dentropy ? logprob<T, VOCAB_STEP, true>(p, sms, stream)
                                        : logprob<T, VOCAB_STEP, false>(p, sms, stream);
@@ -59,6 +42,7 @@ cudaError_t logprob_pass(VocabParams p, int pass, int sms, cudaStream_t stream)
 
 cudaError_t launch_token_logprob(const VocabParams& p, int dtype, int pass, int sms, cudaStream_t stream)
 {
+    if (pass == VOCAB_FWD && p.k > 0) return launch_token_logprob_top(p, dtype, sms, stream);
     return dtype == 0 ? logprob_pass<__nv_bfloat16>(p, pass, sms, stream) : logprob_pass<float>(p, pass, sms, stream);
 }
 

@@ -50,6 +50,8 @@ struct VocabParams {
 };
 
 cudaError_t launch_token_logprob(const VocabParams& p, int dtype, int pass, int sms, cudaStream_t stream);
+// the forward with p.k > 0 alternatives
+cudaError_t launch_token_logprob_top(const VocabParams& p, int dtype, int sms, cudaStream_t stream);
 cudaError_t launch_topk_distill(const VocabParams& p, int dtype, int pass, int sms, cudaStream_t stream);
 
 }  // namespace cola

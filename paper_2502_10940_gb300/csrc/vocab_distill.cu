@@ -8,11 +8,11 @@
 namespace cola {
 namespace {
 
-template <class T, int PASS, int GT>
+template <class T, int PASS, int GT, bool APART>
 cudaError_t distill_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E;
-    auto kern = topk_distill_kernel<T, PASS, GT>;
+    auto kern = topk_distill_kernel<T, PASS, GT, APART>;
     size_t smem = 0;
     if (PASS != VOCAB_BWD) {   // a word of bits per thread and tile
         const int each = (p.vocab / E + s.parts - 1) / s.parts;
@@ -34,16 +34,24 @@ cudaError_t distill_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t st
     return launch_rows(kern, p, E, s, true, smem, sms, stream);
 }
 
+template <class T, int PASS, bool APART>
+cudaError_t distill_plan(VocabParams& p, const Plan& s, int sms, cudaStream_t stream)
+{
+    switch (s.threads) {
+    case 32: return distill_rows<T, PASS, 32, false>(p, s, sms, stream);
+    case 128: return distill_rows<T, PASS, 128, APART>(p, s, sms, stream);
+    case 256: return distill_rows<T, PASS, 256, APART>(p, s, sms, stream);
+    default: return distill_rows<T, PASS, 512, APART>(p, s, sms, stream);
+    }
+}
+
 template <class T, int PASS>
 cudaError_t distill(VocabParams p, int sms, cudaStream_t stream)
 {
     const Plan s = plan(p, Elem<T>::E, PASS, false, 0, p.k, sms);
-    switch (s.threads) {
-    case 32: return distill_rows<T, PASS, 32>(p, s, sms, stream);
-    case 128: return distill_rows<T, PASS, 128>(p, s, sms, stream);
-    case 256: return distill_rows<T, PASS, 256>(p, s, sms, stream);
-    default: return distill_rows<T, PASS, 512>(p, s, sms, stream);
-    }
+    if constexpr (PASS != VOCAB_FWD)
+        if (lies_apart(p, Elem<T>::E)) return distill_plan<T, PASS, true>(p, s, sms, stream);
+    return distill_plan<T, PASS, false>(p, s, sms, stream);
 }
 
 template <class T>

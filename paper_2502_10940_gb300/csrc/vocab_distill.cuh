@@ -36,7 +36,7 @@ using Bits = typename Elem<T>::Bits;        // a bit per element of a tile that 
 // on the list's way: ids, then the student's logits at them, both under way
 // while the row is read.  A step of 16384 x 32000 with lists of 64 takes 340 us,
 // 6.2 TB/s, of 18,000 instructions a row where the cross entropy's 13,000 leave HBM the bound.
-template <class T, int PASS, int GT>
+template <class T, int PASS, int GT, bool APART>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_distill_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
@@ -237,11 +237,11 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
             if (!live || mr == NEG_INF) return 0.f;
             return rate * ex2((x - mr) * P.c2);
         };
-        for (int t = part.tiles - 1; t >= 0; --t) {
-            const int first = part.at(g, t), left = part.left(g, t);
-            if (live && near && same) {
+        if (!APART && live && near && same) {
+            const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A);
+            for (int t = part.tiles - 1; t >= 0; --t) {
+                const int first = part.at(g, t), left = part.left(g, t);
                 if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.template load<true>(row, g, t, d);
-                const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A);
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     if (j % 2 == 0 && j >= part.used(t)) break;
@@ -255,20 +255,12 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
                     }
                     if (left > j * GT) __stcs(vout + first + j * GT, Elem<T>::pack(x));
                 }
-            } else {
-#pragma unroll 1
-                for (int j = 0; j * GT < left && j < NV; ++j) {
-                    float x[E] = {};
-                    if (live) Elem<T>::unpack(row.vec()[first + j * GT], x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = one(x[e]);
-                    if (same) {
-                        vout[first + j * GT] = Elem<T>::pack(x);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < E; ++e) Elem<T>::put(out + row.head + (first + j * GT) * E + e, x[e]);
-                    }
-                }
+            }
+        } else {
+            for (int t = 0; t < part.tiles; ++t) {
+                const int first = part.at(g, t);
+                emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV), mr, P.c2,
+                                  rate, 0.f, live && mr != NEG_INF);
             }
         }
         if (edge) Elem<T>::put(out + edge_id, one(xe));

@@ -15,7 +15,7 @@ namespace cola {
 //
 // The gradient of one CTA's share of a row.  H: with the entropy's term,
 //   c p (-g - h (logp + H)) = 2^y (A + B y),   y = c2 x - base.b.
-template <class T, int PASS, int GT, bool ENT>
+template <class T, int PASS, int GT, bool ENT, bool APART>
 __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>& row, const Part<T, GT>& part, const Group<GT>& g,
                                              float m, float inv_s, float logs, float H, float up_g, float up_h, int y, float xe,
                                              uint4 (&d)[NV])
@@ -33,11 +33,11 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
         const float l = (x - m) * P.c2, p = inv_s * ex2(l);
         return -P.c * p * (up_g + (ENT ? up_h * (LN2 * fmaxf(l, FLOOR) - logs + H) : 0.f));
     };
-    for (int t = part.tiles - 1; t >= 0; --t) {
-        const int first = part.at(g, t), left = part.left(g, t);
-        if (live && near && same) {
+    if (!APART && live && near && same) {
+        const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A), B2 = pair(B, B);
+        for (int t = part.tiles - 1; t >= 0; --t) {
+            const int first = part.at(g, t), left = part.left(g, t);
             if (t < part.tiles - 1 || (PASS == VOCAB_BWD && t > 0)) part.template load<true>(row, g, t, d);
-            const Pair cc = pair(P.c2, P.c2), nb = pair(-base.b, -base.b), A2 = pair(A, A), B2 = pair(B, B);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (j % 2 == 0 && j >= part.used(t)) break;
@@ -52,20 +52,12 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
                 }
                 if (left > j * GT) __stcs(vout + first + j * GT, Elem<T>::pack(x));
             }
-        } else {
-#pragma unroll 1
-            for (int j = 0; j * GT < left && j < NV; ++j) {
-                float x[E] = {};
-                if (live) Elem<T>::unpack(row.vec()[first + j * GT], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = one(x[e]);
-                if (same) {
-                    vout[first + j * GT] = Elem<T>::pack(x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) Elem<T>::put(out + row.head + (first + j * GT) * E + e, x[e]);
-                }
-            }
+        }
+    } else {
+        for (int t = 0; t < part.tiles; ++t) {
+            const int first = part.at(g, t);
+            emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV), m, P.c2,
+                              -P.c * inv_s * (up_g + (ENT ? up_h * (H - logs) : 0.f)), ENT ? -P.c * inv_s * up_h * LN2 : 0.f, live);
         }
     }
     if (g.has_edges() && g.lane < row.edges()) {
@@ -74,7 +66,7 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
     }
 }
 
-template <class T, int PASS, int GT, bool ENT>
+template <class T, int PASS, int GT, bool ENT, bool APART>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E;
@@ -133,8 +125,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
     }
     if constexpr (PASS != VOCAB_FWD) {
         const float inv_s = rcp(s);
-        if (!ENT || up_h == 0.f) emit_logprob<T, PASS, GT, false>(P, row, part, g, m, inv_s, logs, H, up_g, 0.f, y, xe, d);
-        else emit_logprob<T, PASS, GT, true>(P, row, part, g, m, inv_s, logs, H, up_g, up_h, y, xe, d);
+        if (!ENT || up_h == 0.f) emit_logprob<T, PASS, GT, false, APART>(P, row, part, g, m, inv_s, logs, H, up_g, 0.f, y, xe, d);
+        else emit_logprob<T, PASS, GT, true, APART>(P, row, part, g, m, inv_s, logs, H, up_g, up_h, y, xe, d);
         if (owner && m != NEG_INF && (up_g != 0.f || up_h != 0.f)) {   // over its own store of that vector
             const float l = (xy - m) * P.c2, p = inv_s * ex2(l);
             const float r = P.c * (up_g - p * (up_g + up_h * (LN2 * fmaxf(l, FLOOR) - logs + H)));

@@ -62,6 +62,13 @@ inline Plan plan(const VocabParams& p, int e, int pass, bool split, int top, int
     return {threads, parts};
 }
 
+// Whether any row of the gradient lies otherwise on 16-byte boundaries than its logits.
+inline bool lies_apart(const VocabParams& p, int e)
+{
+    return p.dlogits && (((reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) & 15u) != 0 ||
+                         (p.n > 1 && (p.ld - p.ld_d) % e != 0));
+}
+
 template <class K>
 inline cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, int sms, cudaStream_t stream)
 {

@@ -235,6 +235,42 @@ struct Row {
     __device__ __forceinline__ const uint4* vec() const { return reinterpret_cast<const uint4*>(p + head); }
 };
 
+// Stores a warp's consecutive vectors (those that are `mine`, from lane 0 on) where
+// they do not begin on a 16-byte boundary: each lane the 16-byte block that begins
+// within its vector and ends in the next lane's; the ends element by element.
+template <class T>
+__device__ __forceinline__ void store_apart(T* dst, const uint4& p, bool mine)
+{
+    constexpr int E = Elem<T>::E;
+    const int lane = threadIdx.x & 31;
+    const unsigned int cut = 16 - static_cast<unsigned int>(reinterpret_cast<uintptr_t>(dst) & 15u);   // bytes before the block
+    const uint32_t c[8] = {p.x, p.y, p.z, p.w, __shfl_down_sync(~0u, p.x, 1), __shfl_down_sync(~0u, p.y, 1),
+                           __shfl_down_sync(~0u, p.z, 1), __shfl_down_sync(~0u, p.w, 1)};
+    const bool next = __shfl_down_sync(~0u, mine, 1) && lane < 31;
+    uint32_t a[7], b[5];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) a[i] = cut & 8 ? c[i + 2 < 8 ? i + 2 : 7] : c[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) b[i] = cut & 4 ? a[i + 1] : a[i];
+    const unsigned int bits = (cut & 3) * 8;
+    if (cut == 16) {   // (some rows may lie alike)
+        if (mine) __stcs(reinterpret_cast<uint4*>(dst), p);
+        return;
+    }
+    if (mine && next)
+        __stcs(reinterpret_cast<uint4*>(reinterpret_cast<char*>(dst) + cut),
+               make_uint4(__funnelshift_r(b[0], b[1], bits), __funnelshift_r(b[1], b[2], bits), __funnelshift_r(b[2], b[3], bits),
+                          __funnelshift_r(b[3], b[4], bits)));
+    if (mine && (lane == 0 || !next)) {
+        const int first = static_cast<int>(cut / sizeof(T));
+        float x[E];
+        Elem<T>::unpack(p, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < first ? lane == 0 : !next) Elem<T>::put(dst + e, x[e]);
+    }
+}
+
 // The GT threads that work on one row in one CTA: a warp (four rows a CTA) or
 // the whole CTA; the row's CTAs lie along the grid's y, and form a cluster
 // where they exchange anything.
@@ -453,6 +489,38 @@ __device__ __forceinline__ Acc acc_slots(const float4* slots, int count, const G
         a = acc_merge<ENT>(a, Acc{o.x, o.y, o.z}, c2);
     }
     return acc_warp<ENT>(a, c2);
+}
+
+// A tile's gradient 2^y (A + B y), y = c2 (x - m), read from memory again (zeros
+// where not `live`): for rows without gradient and maxima far from 0, and, APART,
+// for results that lie otherwise on 16-byte boundaries than the logits.
+template <class T, int GT, bool APART>
+__device__ __forceinline__ void emit_again(const uint4* src, T* dst, int left, int used, float m, float c2, float A, float B,
+                                           bool live)
+{
+    constexpr int E = Elem<T>::E;
+    const bool same = (reinterpret_cast<uintptr_t>(dst) & 15u) == 0;
+#pragma unroll(APART ? 4 : 1)
+    for (int j = 0; j < used; ++j) {
+        const bool mine = left > j * GT;
+        float x[E] = {};
+        if (live && mine) Elem<T>::unpack(src[j * GT], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float y = (x[e] - m) * c2;
+            x[e] = live ? ex2(y) * fmaf(fmaxf(y, FLOOR), B, A) : 0.f;
+        }
+        if constexpr (APART) {
+            store_apart(dst + j * GT * E, Elem<T>::pack(x), mine);
+        } else if (mine) {
+            if (same) {
+                __stcs(reinterpret_cast<uint4*>(dst) + j * GT, Elem<T>::pack(x));
+            } else {   // (a warp's rows alone)
+#pragma unroll
+                for (int e = 0; e < E; ++e) Elem<T>::put(dst + j * GT * E + e, x[e]);
+            }
+        }
+    }
 }
 
 }  // namespace cola
