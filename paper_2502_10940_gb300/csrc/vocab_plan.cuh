@@ -28,7 +28,9 @@ constexpr double STEP_L2_BYTES = 62e6;
 //     few threads for its bound, and four where many rows of up to 4096 vectors
 //     have enough of 128: much of its work is the same for every warp (116 us
 //     against 129 us for the top 64 of 8192 x 32000, but 130 us against 105 us for
-//     2048 x 128000).
+//     2048 x 128000).  A cluster's bound is looser than one CTA's, and long lists
+//     ranked by one of its CTAs: up to 4096 vectors one CTA takes the top 65 and
+//     more (8 to 12 us against 9 to 22 us for 44 x 13613, 18 against 14 for 1 x 128000).
 //   - A step reads its row twice, the second time from L2: as many CTAs share a row
 //     as keep the rows in flight within it, of sixteen warps where that would
 //     take more than a portable cluster's eight CTAs.
@@ -48,6 +50,7 @@ inline Plan plan(const VocabParams& p, int e, int pass, bool split, int top, int
     if (pass == VOCAB_FWD) {
         if (top > 0 && top <= 64 && nvec <= 4096 && p.n >= 4ll * sms) return {128, 1};
         if (top > 128) threads = 512;
+        if (top > 64 && nvec <= 4096) return {threads, 1};
     } else if (pass == VOCAB_STEP) {
         hold = static_cast<int>(std::ceil(4.0 * sms * 16.0 * nvec / STEP_L2_BYTES));
         if (hold > CLUSTER_MAX) threads = 512, hold = (hold + 1) / 2;

@@ -82,7 +82,7 @@ struct TopShared {
     unsigned int part[2][16];           // counts of the warps, in turn
 };
 
-constexpr unsigned int RANK_MAX = 320;   // candidates that are counted, not sorted
+constexpr unsigned int RANK_MAX = 512;   // candidates that are counted, not sorted
 
 // Gathers at least k and at most CAND_MAX keys of a row in memory, the k
 // largest among them, by a radix search from the top digit that stops as soon
@@ -427,6 +427,7 @@ __global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const Vo
     using G = Group<32>;
     using K = typename WarpKey<T>::K;
     __shared__ K keys[G::ROWS][CAND];
+    __shared__ int ids[G::ROWS][CAND];
     const G g;
     if (g.row >= P.n) return;
     const int lane = g.lane;
@@ -471,7 +472,7 @@ __global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const Vo
             }
             const unsigned int set = __ballot_sync(~0u, id >= 0);
             const int at = count + __popc(set & ((1u << lane) - 1));
-            if (id >= 0 && at < CAND) keys[g.slot][at] = WarpKey<T>::make(Elem<T>::get(row.p + id), id);
+            if (id >= 0 && at < CAND) ids[g.slot][at] = id;
             count += __popc(set);
         }
         return count;
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const Vo
             if ((bound | bit) > most) continue;
             const int n = reached(bound | bit);
             if (n >= P.k) bound |= bit;
-            if (n >= P.k && n <= P.k + (P.k >> 3) + 2) break;
+            if (n >= P.k && n <= min(P.k + (P.k >> 3) + 2, CAND)) break;
         }
     }
     // a bound of -inf: what lies above it, then the first of the -inf tokens
@@ -499,6 +500,8 @@ __global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const Vo
             if ((bound | bit) <= most && reached(bound | bit) >= P.k) bound |= bit;
         count = bound == 0xffffffffu ? 0 : gather(next_key<T>(bound));   // (nothing lies above a NaN)
     }
+    __syncwarp();
+    for (int i = lane; i < count; i += 32) keys[g.slot][i] = WarpKey<T>::make(Elem<T>::get(row.p + ids[g.slot][i]), ids[g.slot][i]);
     for (int j0 = 0; count < P.k && j0 < P.vocab; j0 += 32) {
         const int j = j0 + lane;
         const float x = j < P.vocab ? Elem<T>::get(row.p + j) : 0.f;
