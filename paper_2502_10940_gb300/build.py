@@ -14,10 +14,10 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcola.so")
 
-SOURCES = ["cola_abi.cu", "gemm_fwd.cu", "gemm_bwd.cu", "gemm_wgrad.cu", "gemm_glu.cu", "fused_layer.cu", "gemm_cluster.cu", "thin.cu", "vocab.cu", "vocab_top.cu",
-           "vocab_distill.cu", "cola_noalloc.cu"]
-HEADERS = ["ptx.cuh", "gemm.cuh", "gemm_launch.cuh", "host_plan.cuh", "fused_layer.cuh", "splitk_cluster.cuh", "thin.cuh", "vocab.cuh", "vocab_rows.cuh", "vocab_logprob.cuh", "vocab_top.cuh",
-           "vocab_distill.cuh", "vocab_plan.cuh"]
+SOURCES = ["cola_abi.cu", "gemm_fwd.cu", "gemm_bwd.cu", "gemm_wgrad.cu", "gemm_glu.cu", "fused_layer.cu", "gemm_cluster.cu",
+           "thin.cu", "vocab.cu", "vocab_top.cu", "vocab_distill.cu", "cola_noalloc.cu"]
+HEADERS = ["ptx.cuh", "gemm.cuh", "gemm_launch.cuh", "host_plan.cuh", "fused_layer.cuh", "splitk_cluster.cuh", "thin.cuh",
+           "vocab.cuh", "vocab_rows.cuh", "vocab_logprob.cuh", "vocab_top.cuh", "vocab_distill.cuh", "vocab_plan.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -11,7 +11,8 @@ namespace cola {
 __device__ __forceinline__ float excess(float r)
 {
     if (fabsf(r) < 0.3f)
-        return __fmul_rn(r * r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(r, -1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f));
+        return __fmul_rn(r * r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(-r, fmaf(r, -1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24),
+                                              1.f / 6), 0.5f));
     return r + expm1f(-r);
 }
 
@@ -34,8 +35,10 @@ using Bits = typename Elem<T>::Bits;        // a bit per element of a tile that 
 // row's maximum and sum, so that the rest's probability is its own sum, down to
 // any size, and not 1 - sum p.  The first half of the time of a short row goes by
 // on the list's way: ids, then the student's logits at them, both under way
-// while the row is read.  A step of 16384 x 32000 with lists of 64 takes 340 us,
-// 6.2 TB/s, of 18,000 instructions a row where the cross entropy's 13,000 leave HBM the bound.
+// while the row is read.  A step of 16384 x 32000 with lists of 64 takes 331 us,
+// 6.3 TB/s, of 17,500 instructions a row where the cross entropy's 13,200 leave
+// HBM the bound; a forward of 4096 x 200000 with lists of 128, 246 us (6.7 TB/s);
+// a backward of 8192 x 65536 with lists of 32, 314 us (6.8 TB/s).
 template <class T, int PASS, int GT, bool APART>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_distill_kernel(const VocabParams P)
 {
@@ -259,8 +262,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) topk_dist
         } else {
             for (int t = 0; t < part.tiles; ++t) {
                 const int first = part.at(g, t);
-                emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV), mr, P.c2,
-                                  rate, 0.f, live && mr != NEG_INF);
+                emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV),
+                                         mr, P.c2, rate, 0.f, live && mr != NEG_INF);
             }
         }
         if (edge) Elem<T>::put(out + edge_id, one(xe));

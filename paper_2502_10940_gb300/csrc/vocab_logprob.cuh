@@ -11,7 +11,7 @@ namespace cola {
 // and the gradient as many; an SM has about 11 for each bf16 logit that HBM gives
 // it.  bf16 logits, 32000 a row: forward of 8192 rows 77 us (6.8 TB/s), step of
 // 32768 rows 598 us (7.0 TB/s); fp32 backward with entropy of 4096 x 65537, rows
-// unaligned, 319 us (6.7 TB/s).
+// unaligned, 315 us (6.8 TB/s).
 //
 // The gradient of one CTA's share of a row.  H: with the entropy's term,
 //   c p (-g - h (logp + H)) = 2^y (A + B y),   y = c2 x - base.b.
@@ -56,8 +56,9 @@ __device__ __forceinline__ void emit_logprob(const VocabParams& P, const Row<T>&
     } else {
         for (int t = 0; t < part.tiles; ++t) {
             const int first = part.at(g, t);
-            emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV), m, P.c2,
-                              -P.c * inv_s * (up_g + (ENT ? up_h * (H - logs) : 0.f)), ENT ? -P.c * inv_s * up_h * LN2 : 0.f, live);
+            emit_again<T, GT, APART>(row.vec() + first, out + row.head + first * E, part.left(g, t), min(part.used(t), NV), m,
+                                     P.c2, -P.c * inv_s * (up_g + (ENT ? up_h * (H - logs) : 0.f)),
+                                     ENT ? -P.c * inv_s * up_h * LN2 : 0.f, live);
         }
     }
     if (g.has_edges() && g.lane < row.edges()) {
@@ -127,6 +128,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_log
         const float inv_s = rcp(s);
         if (!ENT || up_h == 0.f) emit_logprob<T, PASS, GT, false, APART>(P, row, part, g, m, inv_s, logs, H, up_g, 0.f, y, xe, d);
         else emit_logprob<T, PASS, GT, true, APART>(P, row, part, g, m, inv_s, logs, H, up_g, up_h, y, xe, d);
+        if (APART) __syncwarp();   // (the neighbouring lane may have stored that element)
         if (owner && m != NEG_INF && (up_g != 0.f || up_h != 0.f)) {   // over its own store of that vector
             const float l = (xy - m) * P.c2, p = inv_s * ex2(l);
             const float r = P.c * (up_g - p * (up_g + up_h * (LN2 * fmaxf(l, FLOOR) - logs + H)));

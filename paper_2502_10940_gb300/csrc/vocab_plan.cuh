@@ -22,8 +22,8 @@ constexpr double STEP_L2_BYTES = 62e6;
 // A warp or four warps where their registers hold the row (NV vectors a
 // thread); four too for a teacher's `list` beyond a warp's lanes, where the device
 // runs all rows at once (7.2 us against 11.3 us for 86 rows of 552 and lists of 220,
-// but 162 us against 86 us for 24727 of 672 and 138).  Longer rows take eight warps, so that the phases of four rows overlap
-// on an SM, tile after tile.
+// but 162 us against 86 us for 24727 of 672 and 138).  Longer rows take eight warps,
+// so that the phases of four rows overlap on an SM, tile after tile.
 //   - A forward with the `top` k (0: without) takes sixteen where eight have too
 //     few threads for its bound, and four where many rows of up to 4096 vectors
 //     have enough of 128: much of its work is the same for every warp (116 us
@@ -73,7 +73,8 @@ inline bool lies_apart(const VocabParams& p, int e)
 }
 
 template <class K>
-inline cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, int sms, cudaStream_t stream)
+inline cudaError_t launch_rows(K kern, VocabParams& p, int e, const Plan& s, bool cluster, size_t smem, int sms,
+                               cudaStream_t stream)
 {
     const int rows = s.threads == 32 ? 4 : 1;
     p.each = (p.vocab / e + s.parts - 1) / s.parts;

