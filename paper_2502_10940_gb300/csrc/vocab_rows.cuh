@@ -100,6 +100,21 @@ struct Elem<float> {
     {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    __device__ __forceinline__ static float largest(const uint4& u)
+    {
+        return max_nan(max_nan(__uint_as_float(u.x), __uint_as_float(u.y)), max_nan(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
+    // bits whose upper half alone tells x apart from 0 where it is below
+    __device__ __forceinline__ static uint32_t above_half(float x)
+    {
+        const uint32_t b = __float_as_uint(x);
+        return b > 0x80000000u && b < 0x80010000u ? 0x80010000u : b;
+    }
+    // upper halves of the maxima of two parts of two vectors (here: of each vector)
+    __device__ __forceinline__ static uint32_t halves(const uint4& a, const uint4& b)
+    {
+        return __byte_perm(above_half(largest(a)), above_half(largest(b)), 0x7632);
+    }
     __device__ __forceinline__ static float max_of(const uint4 (&d)[NV])
     {
         float m = NEG_INF;
@@ -189,6 +204,15 @@ struct Elem<__nv_bfloat16> {
     {
         const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
         return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    __device__ __forceinline__ static float largest(const uint4& u)
+    {
+        const uint32_t m = max_pair(max_pair(u.x, u.y), max_pair(u.z, u.w));
+        return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+    __device__ __forceinline__ static uint32_t halves(const uint4& a, const uint4& b)   // (of their even and odd elements)
+    {
+        return max_pair(max_pair(max_pair(a.x, a.y), max_pair(a.z, a.w)), max_pair(max_pair(b.x, b.y), max_pair(b.z, b.w)));
     }
     __device__ __forceinline__ static float max_of(const uint4 (&d)[NV])
     {

@@ -335,3 +335,20 @@ def test_many_short_rows_with_long_lists(V, k, dtype):
     x[14] = np.where(np.arange(V) % 3 == 0, 1.0, -np.inf)
     x = H.rounded(x, dtype)
     compare(x, rng.integers(0, V, 300), dtype, 1.5, k, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(600, 20), (1500, 40), (2003, 100), (5003, 20), (5003, 100), (7001, 256), (20011, 100), (33001, 5)])
+def test_order_around_zero(V, k, dtype):
+    """Subnormal logits of both signs, beside zeros of both."""
+    rng = np.random.default_rng(V + k)
+    unit = 2.0 ** (-133 if dtype == "bf16" else -149)                # the least above 0
+    few = np.zeros(V)
+    few[rng.permutation(V)[: k // 2]] = 1.0
+    rows = [rng.integers(-100, 100, V), -rng.integers(1, 120, V), rng.integers(-120, 3, V), few - rng.integers(1, 90, V) * (few == 0),
+            2 * few - 3]
+    if dtype == "f32":
+        rows += [-rng.integers(1, 0x10000, V), rng.integers(-0x30000, 0x100, V), -rng.integers(0x7000, 0x18000, V)]
+    x = np.stack(rows).astype(np.float64) * unit
+    x[0, ::5] = -0.0
+    compare(x, np.arange(len(rows)), dtype, 1.0, k, None, None)
