@@ -89,7 +89,8 @@ __device__ __forceinline__ uint32_t search_bound(const uint4* halves, int k, int
         const uint32_t from = __float_as_uint(key_value(bound | bit)) >> 16, both = from << 16 | from;
         __nv_bfloat162 reach = __floats2bfloat162_rn(0.f, 0.f);   // (counts to 16: exact)
         each([&](uint32_t w) {
-            reach = __hadd2(reach, __hgeu2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&both)));
+            reach = __hadd2(reach, __hgeu2(*reinterpret_cast<const __nv_bfloat162*>(&w),
+                                           *reinterpret_cast<const __nv_bfloat162*>(&both)));
         });
         n = __reduce_add_sync(~0u, static_cast<int>(__low2float(reach) + __high2float(reach)));
         if (n >= k) bound |= bit;
@@ -224,7 +225,7 @@ __device__ __forceinline__ unsigned int above_in(const K* keys, K key)
 // its run and the number before it in each of the others.
 // One pass of HBM, which the bound, the gather and the ranking follow in each row:
 // what overlaps them is the other rows of the SM.  4096 x 32000 fp32, k = 1: 84 us,
-// 6.2 TB/s; 8192 x 32000 bf16, k = 64: 116 us, 4.6 TB/s, where each row takes 12,000
+// 6.2 TB/s; 8192 x 32000 bf16, k = 64: 116 us, 4.6 TB/s, where each row takes 11,600
 // instructions; 32768 x 5000 bf16: 149 us at k = 20, 247 us at k = 100.
 template <class T, int GT, bool ENT, bool FEW>
 __global__ void __launch_bounds__(Group<GT>::THREADS, Group<GT>::CTAS) token_logprob_top_kernel(const VocabParams P)
