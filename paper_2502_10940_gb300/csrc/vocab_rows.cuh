@@ -301,7 +301,7 @@ __device__ __forceinline__ void store_apart(T* dst, const uint4& p, bool mine)
 template <int GT>
 struct Group {
     static constexpr int ROWS = GT == 32 ? 4 : 1, THREADS = GT * ROWS, W = GT / 32, TILE = GT * NV;
-    static constexpr int CTAS = GT == 32 ? 6 : 1024 / THREADS;   // an SM's, for the registers a thread may have
+    static constexpr int CTAS = 1024 / THREADS;   // an SM's, for the registers a thread may have
     long long row;
     int rank, parts, tid, lane, warp, slot;
 

@@ -505,7 +505,7 @@ struct WarpKey<__nv_bfloat16> {
 // bound it, so as many warps as 64 registers allow (65 us against 76 us for the top 5
 // of 65536 x 2000 bf16; the top 40: 104 us).
 template <class T, bool ENT>
-__global__ void __launch_bounds__(128, 8) token_logprob_top_warp_kernel(const VocabParams P)
+__global__ void __launch_bounds__(Group<32>::THREADS, Group<32>::CTAS) token_logprob_top_warp_kernel(const VocabParams P)
 {
     constexpr int E = Elem<T>::E, CAND = VOCAB_MAX_K;
     using G = Group<32>;
