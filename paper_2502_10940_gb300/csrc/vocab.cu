@@ -13,8 +13,11 @@ cudaError_t logprob_rows(VocabParams& p, const Plan& s, int sms, cudaStream_t st
     switch (s.threads) {
     case 32: return launch_rows(token_logprob_kernel<T, PASS, 32, ENT, false>, p, E, s, cluster, 0, sms, stream);
     case 128: return launch_rows(token_logprob_kernel<T, PASS, 128, ENT, APART>, p, E, s, cluster, 0, sms, stream);
-    case 256: return launch_rows(token_logprob_kernel<T, PASS, 256, ENT, APART>, p, E, s, cluster, 0, sms, stream);
-    default: return launch_rows(token_logprob_kernel<T, PASS, 512, ENT, APART>, p, E, s, cluster, 0, sms, stream);
+    default:
+        if constexpr (PASS == VOCAB_STEP)
+            if (s.threads == 512)
+                return launch_rows(token_logprob_kernel<T, PASS, 512, ENT, APART>, p, E, s, cluster, 0, sms, stream);
+        return launch_rows(token_logprob_kernel<T, PASS, 256, ENT, APART>, p, E, s, cluster, 0, sms, stream);
     }
 }
 

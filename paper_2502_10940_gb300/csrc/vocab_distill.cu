@@ -40,8 +40,10 @@ cudaError_t distill_plan(VocabParams& p, const Plan& s, int sms, cudaStream_t st
     switch (s.threads) {
     case 32: return distill_rows<T, PASS, 32, false>(p, s, sms, stream);
     case 128: return distill_rows<T, PASS, 128, APART>(p, s, sms, stream);
-    case 256: return distill_rows<T, PASS, 256, APART>(p, s, sms, stream);
-    default: return distill_rows<T, PASS, 512, APART>(p, s, sms, stream);
+    default:
+        if constexpr (PASS == VOCAB_STEP)
+            if (s.threads == 512) return distill_rows<T, PASS, 512, APART>(p, s, sms, stream);
+        return distill_rows<T, PASS, 256, APART>(p, s, sms, stream);
     }
 }
 

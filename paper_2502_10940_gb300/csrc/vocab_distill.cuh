@@ -38,7 +38,7 @@ using Bits = typename Elem<T>::Bits;        // a bit per element of a tile that 
 // while the row is read.  A step of 16384 x 32000 with lists of 64 takes 331 us,
 // 6.3 TB/s, of 17,500 instructions a row where the cross entropy's 13,200 leave
 // HBM the bound; a forward of 4096 x 200000 with lists of 128, 246 us (6.7 TB/s);
-// a backward of 8192 x 65536 with lists of 32, 314 us (6.8 TB/s).
+// a backward of 8192 x 65536 with lists of 32, 308 us (7.0 TB/s).
 // (A warp's row and its gradient need more registers than eight CTAs' 64: 160 us on six
 // against 164 us for a step of 65536 x 2000 with lists of 64; the forward 135 us on eight, 153 us on six.)
 template <class T, int PASS, int GT, bool APART>

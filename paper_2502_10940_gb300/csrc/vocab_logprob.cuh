@@ -11,7 +11,7 @@ namespace cola {
 // and the gradient as many; an SM has about 11 for each bf16 logit that HBM gives
 // it.  bf16 logits, 32000 a row: forward of 8192 rows 77 us (6.8 TB/s), step of
 // 32768 rows 598 us (7.0 TB/s); fp32 backward with entropy of 4096 x 65537, rows
-// unaligned, 315 us (6.8 TB/s).
+// unaligned, 312 us (6.9 TB/s).
 //
 // The gradient of one CTA's share of a row.  H: with the entropy's term,
 //   c p (-g - h (logp + H)) = 2^y (A + B y),   y = c2 x - base.b.
