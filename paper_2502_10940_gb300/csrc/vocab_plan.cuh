@@ -22,8 +22,11 @@ constexpr double STEP_L2_BYTES = 62e6;
 // A warp or four warps where their registers hold the row (NV vectors a
 // thread); four too for a teacher's `list` beyond a warp's lanes, where the device
 // runs all rows at once (7.2 us against 11.3 us for 86 rows of 552 and lists of 220,
-// but 162 us against 86 us for 24727 of 672 and 138).  Longer rows take eight warps,
-// so that the phases of four rows overlap on an SM, tile after tile.
+// but 162 us against 86 us for 24727 of 672 and 138), and of many rows up to 4096
+// vectors (2560 in a step, whose rows in flight L2 holds), tile after tile, so that the
+// phases of eight rows overlap on an SM: 193 us against 229 us for a step of 32768 x
+// 10000 bf16, 97 us against 122 us for a forward of 16384 x 20000; but 506 us against 463 us
+// for a step of 32768 x 25000.  Longer rows, and few, take eight warps.
 //   - A forward with the `top` k (0: without) takes sixteen where eight have too
 //     few threads for its bound, and four where many rows of up to 4096 vectors
 //     have enough of 128: much of its work is the same for every warp (116 us
@@ -48,6 +51,7 @@ inline Plan plan(const VocabParams& p, int e, int pass, bool split, int top, int
     const int nvec = (p.vocab + e - 1) / e;
     if (nvec <= 32 * NV && (list <= 32 || p.n > 8ll * sms)) return {32, 1};
     if (nvec <= 128 * NV) return {128, 1};
+    if (top == 0 && p.n >= 4ll * sms && nvec <= (pass == VOCAB_STEP ? 2560 : 4096)) return {128, 1};
     int threads = 256, hold = 1;
     if (pass == VOCAB_FWD) {
         if (top > 0 && top <= 64 && nvec <= 4096 && p.n >= 4ll * sms) return {128, 1};
