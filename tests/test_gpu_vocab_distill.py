@@ -248,3 +248,20 @@ def test_many_rows(n, V, k, dtype, rest):
     tol = w.double().abs()[:, None] * T * (4e-6 * r + 2e-5 * (1 - out)) + (2e-5 + (2.0 ** -8 if dtype == "bf16" else 0.0)) * ref.abs() + 1e-37
     for got in (dx, dx2):
         assert bool(((got.double() - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["dense", "odd", "shifted"])
+@pytest.mark.parametrize("V,k,rest", [(5003, 200, True), (9001, 40, True), (19003, 90, False)])
+def test_many_rows_of_middle_length(V, k, rest, layout, dtype):
+    """Rows of several tiles of one CTA of four warps, masks among them."""
+    rng = np.random.default_rng(V + k)
+    n = 640
+    x = H.logits(rng, n, V, dtype)
+    ids, vals, lse = H.teacher(rng, x, k, 1.5)
+    x[3, V // 2:] = -np.inf
+    x[4] = -np.inf
+    x[5, : V // 2] = float(torch.finfo(H.TORCH[dtype]).min)
+    w = rng.standard_normal(n)
+    w[9] = 0.0
+    compare(x, ids, vals, lse if rest else None, dtype, 1.5, 1.5, rest, w, layout)

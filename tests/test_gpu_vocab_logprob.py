@@ -352,3 +352,21 @@ def test_order_around_zero(V, k, dtype):
     x = np.stack(rows).astype(np.float64) * unit
     x[0, ::5] = -0.0
     compare(x, np.arange(len(rows)), dtype, 1.0, k, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["dense", "odd", "shifted"])
+@pytest.mark.parametrize("V", [5003, 9001, 19003])
+def test_many_rows_of_middle_length(V, layout, dtype):
+    """Rows of several tiles of one CTA of four warps, masks among them, with gradients."""
+    rng = np.random.default_rng(V)
+    n = 640
+    x = H.logits(rng, n, V, dtype)
+    x[3, V // 2:] = -np.inf
+    x[4] = -np.inf
+    x[5, : V // 2] = float(torch.finfo(H.TORCH[dtype]).min)
+    t = rng.integers(0, V, n)
+    t[3], t[8] = 7, -1
+    g, h = rng.standard_normal(n), rng.standard_normal(n)
+    g[9] = h[9] = 0.0
+    compare(x, t, dtype, 1.5, 0, g, h, layout)
