@@ -86,6 +86,7 @@ __device__ __forceinline__ uint32_t search_bound(const uint4* halves, int k, int
     const int agree = __clz(least ^ most);
     uint32_t bound = agree >= 16 ? least : least & ~(0xffffffffu >> agree);
     for (uint32_t bit = agree >= 16 ? 0 : 0x80000000u >> agree; bit > 0x8000u; bit >>= 1) {
+        if ((bound | bit) > most) continue;   // (beyond +inf lie NaNs' patterns, which every maximum would reach)
         const uint32_t from = __float_as_uint(key_value(bound | bit)) >> 16, both = from << 16 | from;
         __nv_bfloat162 reach = __floats2bfloat162_rn(0.f, 0.f);   // (counts to 16: exact)
         each([&](uint32_t w) {

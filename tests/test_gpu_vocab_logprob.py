@@ -370,3 +370,28 @@ def test_many_rows_of_middle_length(V, layout, dtype):
     g, h = rng.standard_normal(n), rng.standard_normal(n)
     g[9] = h[9] = 0.0
     compare(x, t, dtype, 1.5, 0, g, h, layout)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(700, 100), (2003, 20), (2003, 200), (3500, 256), (5003, 64), (5003, 100), (8000, 256),
+                                 (20011, 30), (33001, 200)])
+def test_top_with_many_infinities(V, k, dtype):
+    """More +inf than the list has entries, scattered, alone and beside NaNs:
+    the bound stays where the infinities reach it."""
+    rng = np.random.default_rng(V + k)
+    count = [k, k + k // 8 + 2, k + k // 8 + 3, 2 * k, V // 2, V - 1, V]
+    x = rng.standard_normal((2 * len(count) + 1, V))
+    for i, c in enumerate(count):
+        x[i, rng.permutation(V)[:c]] = np.inf
+        x[len(count) + i] = x[i]
+        x[len(count) + i, rng.permutation(V)[:3]] = np.nan
+    x[-1, rng.permutation(V)[: 2 * k]] = np.nan
+    x = H.rounded(x, dtype)
+    compare(x, np.arange(len(x)), dtype, 1.0, k, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,k", [(5003, 100), (3500, 256), (6007, 65), (5003, 30)])
+def test_many_rows_of_a_few_thousand_tokens(V, k, dtype):
+    """The same awkward rows where four warps hold a row."""
+    test_many_long_rows(V, k, dtype)
