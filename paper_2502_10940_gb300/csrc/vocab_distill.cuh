@@ -7,7 +7,9 @@ namespace cola {
 // ------------------------------------------------------------- distillation
 // r + exp(-r) - 1 >= 0.  Where q and p both sum to 1, KL(q || p) is the sum of
 // q excess(log q / p): a sum of nonnegative terms, exact to a few ulp where
-// that of q log(q / p) cancels.
+// that of q log(q / p) cancels.  (From r = -1 down nothing does, while q may be too
+// small a number to hold its digits and exp(-r) too large a one: there an entry's
+// term is p + q (r - 1).)
 __device__ __forceinline__ float excess(float r)
 {
     if (fabsf(r) < 0.3f)
@@ -219,7 +221,8 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, GT == 32 && PASS != VOCAB_
             const float logp = fmaf(list.x[i] - m0, P.c, -logs), p = expf(logp);
             if (PASS != VOCAB_BWD) {
                 const float r = __fadd_rn(logq, -logp);
-                kl = __fadd_rn(kl, entry ? (q > 0.f ? __fmul_rn(q, excess(r)) : p) : q > 0.f ? __fmul_rn(q, r) : 0.f * q);
+                const float whole = q > 0.f ? (r > -1.f ? __fmul_rn(q, excess(r)) : fmaf(q, __fadd_rn(r, -1.f), p)) : p;
+                kl = __fadd_rn(kl, entry ? whole : q > 0.f ? __fmul_rn(q, r) : 0.f * q);
             }
             if (PASS != VOCAB_FWD) list.u[i] = wt * ((entry ? 1.f : Q) * p - q);
         }

@@ -265,3 +265,21 @@ def test_many_rows_of_middle_length(V, k, rest, layout, dtype):
     w = rng.standard_normal(n)
     w[9] = 0.0
     compare(x, ids, vals, lse if rest else None, dtype, 1.5, 1.5, rest, w, layout)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [300, 3001, 40007])
+def test_listed_tokens_that_only_the_student_finds_likely(V, dtype):
+    """Teacher's probabilities down to the least above 0 and beyond, the rest
+    counted: such an entry costs the student's probability and no more."""
+    rng = np.random.default_rng(V)
+    unlikely = np.array([-80.0, -85.0, -87.5, -90.0, -100.0, -102.5, -103.5, -110.0])
+    n, k = len(unlikely) + 1, 3
+    x = H.rounded(rng.standard_normal((n, V)), dtype)
+    ids = np.tile(np.array([V // 3, V - 1, 0]), (n, 1))
+    x[:, ids[0, 0]] = 14.0                                           # nearly all of the student's probability
+    x[:, ids[0, 1]] = np.linspace(4.0, 12.0, n)
+    vals = np.tile(np.array([0.0, -30.0, -1.0], np.float32), (n, 1))
+    vals[:-1, 0] = unlikely
+    vals[-1] = -100.0                                                # a padded list
+    compare(H.rounded(x, dtype), ids, vals, np.zeros(n, np.float32), dtype, 1.0, 1.0, True, np.ones(n))
