@@ -273,9 +273,9 @@ cola_status_t cola_recompute_up(const cola_desc_t* desc, int32_t count, const vo
  *
  * Conventions, next to the ones at the top of this file:
  *   - logits and dlogits: device pointers aligned to their element, rows of
- *     any pitch >= vocab (rows on 16-byte boundaries, and dlogits with the
- *     logits' offset from them, run fastest); token ids int64; other values
- *     fp32; stats 16-byte aligned.  No workspace.
+ *     any pitch >= vocab within the limits below (rows on 16-byte boundaries,
+ *     and dlogits with the logits' offset from them, run fastest); token ids
+ *     int64; other values fp32; stats 16-byte aligned.  No workspace.
  *   - dlogits may be the logits themselves (same pointer and pitch).
  *   - Token ids outside [0, vocab) are legal and name no token: such a target
  *     is ignored (logp 0, no gradient), such a list entry absent.
@@ -284,7 +284,7 @@ cola_status_t cola_recompute_up(const cola_desc_t* desc, int32_t count, const vo
  *     results NaN.  A row whose upstream gradients are 0 has gradient 0,
  *     whatever it holds.
  *   - Limits: vocab <= 2^20, k <= 256 and <= vocab, 1e-4 <= temperatures <= 1e4,
- *     n < 2^28. */
+ *     n < 2^28, pitches <= 2^31 - 256. */
 typedef enum {
     COLA_DTYPE_BF16 = 0,
     COLA_DTYPE_F32 = 1

@@ -1610,7 +1610,7 @@ cola_status_t vocab_params(const cola_vocab_desc_t* d, const void* logits, void*
     p->ld_d = d->ld_grad ? d->ld_grad : d->vocab;
     if (p->ld < d->vocab || p->ld_d < d->vocab || d->k > d->vocab) return COLA_ERR_INVALID;
     const int64_t lim = (int64_t(1) << 31) - 256;
-    if (d->vocab > VOCAB_MAX || d->k > VOCAB_MAX_K || d->n > lim / 8 || p->ld > lim || p->ld_d > lim)
+    if (d->vocab > VOCAB_MAX || d->k > VOCAB_MAX_K || d->n >= VOCAB_MAX_ROWS || p->ld > lim || p->ld_d > lim)
         return COLA_ERR_UNSUPPORTED;
     const size_t e = d->dtype == COLA_DTYPE_BF16 ? 2 : 4;
     if (!aligned_to(logits, e) || (grad && !aligned_to(dlogits, e))) return COLA_ERR_ALIGN;

@@ -17,6 +17,7 @@
 namespace cola {
 
 constexpr int VOCAB_MAX = 1 << 20;      // tokens of a vocabulary
+constexpr long long VOCAB_MAX_ROWS = 1ll << 28;   // rows stay below it: a CTA of the grid each
 constexpr int VOCAB_MAX_K = 256;        // alternatives, entries of a teacher's list
 enum { VOCAB_FWD = 0, VOCAB_STEP = 1, VOCAB_BWD = 2 };
 

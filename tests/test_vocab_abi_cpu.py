@@ -103,3 +103,20 @@ def test_lists_go_with_k(L):   # noqa: F811
 def test_binding_raises(L):   # noqa: F811
     with pytest.raises(L.ColaError, match="cola_token_logprob_fwd"):
         L.cola_token_logprob_fwd(_desc(L, vocab=0), FAKE, FAKE, FAKE, None, None, None, None, stream=0)
+
+
+# the last values that pass (what comes next is that the logits are misaligned) and the first that do not
+@pytest.mark.parametrize("name", sorted(CALLS))
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=(1 << 28) - 1), 2), (dict(n=1 << 28), 3),
+    (dict(ld=(1 << 31) - 256), 2), (dict(ld=(1 << 31) - 255), 3),
+    (dict(ld_grad=(1 << 31) - 256), 2), (dict(ld_grad=(1 << 31) - 255), 3),
+    (dict(vocab=1 << 20), 2), (dict(vocab=(1 << 20) + 1), 3),
+    (dict(vocab=1000, k=256), 2), (dict(vocab=1000, k=257), 3),
+    (dict(temperature=1e-4), 2), (dict(temperature=1e4), 2), (dict(temperature=1.001e4), 1),
+    (dict(teacher_temperature=1e-4), 2), (dict(teacher_temperature=1e4), 2), (dict(teacher_temperature=1.001e4), 1),
+])
+def test_edges_of_the_limits(L, name, kw, code):   # noqa: F811
+    k, args = CALLS[name]
+    d = _desc(L, **{"k": k, **kw})
+    assert _call(L, name, d, [FAKE + 1] + args[1:]) == code
