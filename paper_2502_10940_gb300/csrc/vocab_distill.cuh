@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, GT == 32 && PASS != VOCAB_
         for (int i = g.tid; i < P.k; i += GT) {
             if (list.id[i] < 0) continue;
             const float logq = (list.u[i] - u_top) - log_us, q = us == 0.f ? 0.f : expf(logq);
-            // (roundings written out: the same loss from every pass)
+            // (roundings written out: the same loss from passes that share a row alike)
             const float logp = fmaf(list.x[i] - m0, P.c, -logs), p = expf(logp);
             if (PASS != VOCAB_BWD) {
                 const float r = __fadd_rn(logq, -logp);

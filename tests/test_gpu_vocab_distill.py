@@ -283,3 +283,41 @@ def test_listed_tokens_that_only_the_student_finds_likely(V, dtype):
     vals[:-1, 0] = unlikely
     vals[-1] = -100.0                                                # a padded list
     compare(H.rounded(x, dtype), ids, vals, np.zeros(n, np.float32), dtype, 1.0, 1.0, True, np.ones(n))
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,n,V,k", [("bf16", 1300, 32000, 64), ("bf16", 700, 21000, 200), ("f32", 700, 11000, 200),
+                                         ("bf16", 300, 200000, 40)])
+def test_losses_of_passes_that_share_rows_differently(dtype, n, V, k, rest):
+    """Rows that the forward and the step give to other numbers of threads or
+    CTAs: sums in another order, so losses within the tolerance of one another and
+    of the definition (where rows are shared alike they are the same bits:
+    test_many_rows)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + V + k)
+    T = 1.5
+    x = (torch.randn((n, V), generator=g, device="cuda") * 2).to(H.TORCH[dtype])
+    t = x.float() * 0.9 + torch.randn((n, V), generator=g, device="cuda")
+    top = torch.topk(t, k, dim=1)
+    ids, vals = top.indices.contiguous(), top.values.contiguous()
+    lse = torch.logsumexp(t / T, 1) if rest else None
+    w = torch.randn(n, generator=g, device="cuda")
+    d = cola.vocab_desc(n, V, dtype=dtype, temperature=T, k=k, rest=rest, teacher_temperature=T)
+    loss, loss2, dx = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x)
+    cola.cola_topk_distill_fwd(d, x, ids, vals, lse, loss, None)
+    cola.cola_topk_distill_step(d, x, ids, vals, lse, w, loss2, dx)
+    u = vals.double() / T
+    logq = u - lse.double()[:, None] if rest else torch.log_softmax(u, 1)
+    q = logq.exp()
+    for i in range(0, n, 100):
+        s = slice(i, min(n, i + 100))
+        lp = torch.log_softmax(x[s].double() / T, 1)
+        ref = (q[s] * (logq[s] - lp.gather(1, ids[s]))).sum(1)
+        if rest:
+            qr = (1 - q[s].sum(1)).clamp(min=0.0)
+            ref += qr * (qr.clamp(min=1e-300).log() - torch.logsumexp(lp.scatter(1, ids[s], -torch.inf), 1))
+        ref *= T * T
+        tol = T * T * 2e-5 + 1e-5 * ref.abs()   # H.loss_tol
+        for a in (loss[s].double(), loss2[s].double()):
+            assert bool(((a - ref).abs() <= tol).all())
+        assert bool(((loss[s].double() - loss2[s].double()).abs() <= tol).all())
