@@ -14,7 +14,6 @@ constexpr int NV = 8;                   // 16-byte vectors a thread holds at onc
 constexpr int CLUSTER_MAX = 8;
 constexpr int CAND_MAX = 1024;          // candidates for the top k kept on chip
 constexpr float NEG_INF = -__builtin_huge_valf();
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float FLOOR = -1e4f;          // an exponent of 2 whose power is 0
 constexpr float NEAR = 1e6f;            // maxima, in powers of 2, whose rounding stays far below 1
@@ -380,16 +379,6 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void st_cluster_f4(uint32_t addr, float4 v)
 {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
-}
-__device__ __forceinline__ void st_cluster_u64(uint32_t addr, unsigned long long v)
-{
-    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
-}
-__device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v)
-{
-    uint32_t r;
-    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(r) : "r"(addr), "r"(v) : "memory");
-    return r;
 }
 
 // -------------------------------------------------------- softmax statistics
