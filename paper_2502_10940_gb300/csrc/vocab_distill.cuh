@@ -221,8 +221,12 @@ __global__ void __launch_bounds__(Group<GT>::THREADS, GT == 32 && PASS != VOCAB_
             const float logp = fmaf(list.x[i] - m0, P.c, -logs), p = expf(logp);
             if (PASS != VOCAB_BWD) {
                 const float r = __fadd_rn(logq, -logp);
-                const float whole = q > 0.f ? (r > -1.f ? __fmul_rn(q, excess(r)) : fmaf(q, __fadd_rn(r, -1.f), p)) : p;
-                kl = __fadd_rn(kl, entry ? whole : q > 0.f ? __fmul_rn(q, r) : 0.f * q);
+                float term;
+                if (!entry) term = q > 0.f ? __fmul_rn(q, r) : 0.f * q;
+                else if (!(q > 0.f)) term = p;
+                else if (r > -1.f) term = __fmul_rn(q, excess(r));
+                else term = fmaf(q, __fadd_rn(r, -1.f), p);
+                kl = __fadd_rn(kl, term);
             }
             if (PASS != VOCAB_FWD) list.u[i] = wt * ((entry ? 1.f : Q) * p - q);
         }
