@@ -296,7 +296,7 @@ typedef struct {
     int64_t ld;                 /* row pitch of the logits in elements (0: vocab) */
     int64_t ld_grad;            /* row pitch of dlogits (0: vocab) */
     float temperature;          /* T */
-    float teacher_temperature;  /* distillation: what t_vals are divided by */
+    float teacher_temperature;  /* distillation: what t_vals are divided by (every call checks its limits) */
     int32_t dtype;              /* cola_dtype_t of logits and dlogits */
     int32_t k;                  /* alternatives per row (0: none); entries of a teacher's list */
     int32_t rest;               /* distillation: 1 counts the tokens outside the list as one more entry */

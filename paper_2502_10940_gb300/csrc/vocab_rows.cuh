@@ -296,7 +296,10 @@ __device__ __forceinline__ void store_apart(T* dst, const uint4& p, bool mine)
 
 // The GT threads that work on one row in one CTA: a warp (four rows a CTA) or
 // the whole CTA; the row's CTAs lie along the grid's y, and form a cluster
-// where they exchange anything.
+// where they exchange anything.  A warp's rows gain from eight CTAs an SM although
+// some of their forms then spill a few registers (65536 rows: bf16 entropy backward of
+// 1000 logits 53 us against 58 us on six, fp32 entropy step of 504 54 against 57 us; of
+// 1000 it loses, 84 against 81 us).
 template <int GT>
 struct Group {
     static constexpr int ROWS = GT == 32 ? 4 : 1, THREADS = GT * ROWS, W = GT / 32, TILE = GT * NV;
