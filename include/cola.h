@@ -358,6 +358,98 @@ cola_status_t cola_topk_distill_step(const cola_vocab_desc_t* desc, const void* 
                                      const float* t_vals, const float* t_lse, const float* dloss, float* loss,
                                      void* dlogits, void* stream);
 
+/* ---- constraints on the logits ----
+ * What a server imposes on a row of logits before a token is taken from it
+ * (cola_token_logprob_fwd with its alternatives), and the gradient of a loss of
+ * the constrained logits at the model's own.  The paper has no counterpart.
+ *
+ * For a logit x of a token that occurs c times in its row's history behind the
+ * prompt, in this order, in fp32, rounded once:
+ *   x := x > 0 ? x / repetition : x repetition   where the history, prompt
+ *                                                included, has the token
+ *   x := x - frequency c - presence [c > 0]
+ *   x := x + the sum of the token's entries among the row's biases, in their order
+ *   x := -inf                                    where the row's mask has a 0
+ *                                                bit for the token
+ * Other logits are copied bit for bit.  The history's and the biases' ids outside
+ * [0, vocab) name no token.  A mask may leave a row nothing (all -inf).
+ * Penalties are the caller's to choose; repetition > 0 is meant (1: none).
+ *
+ * Conventions as for the other vocabulary operators: desc gives n, vocab, the
+ * pitch ld of the logits and ld_grad of out, dout and dlogits, and their type;
+ * its temperatures, k and rest are checked but not used.  Integers are int64. */
+typedef struct {
+    const int64_t* history;      /* [n x history_width] (ld_history) token ids, prompt first; NULL: none */
+    const int64_t* history_len;  /* [n] ids of each row (held to 0 .. history_width); NULL: all */
+    const int64_t* prompt_len;   /* [n] of those, how many are the prompt; NULL: 0 */
+    const float* repetition;     /* [n]; NULL: 1 */
+    const float* frequency;      /* [n]; NULL: 0 */
+    const float* presence;       /* [n]; NULL: 0 */
+    const int64_t* bias_ids;     /* [n x n_bias]; NULL: none */
+    const float* bias;           /* [n x n_bias] */
+    const uint32_t* masks;       /* [n_masks x ceil(vocab / 32)] (ld_masks): bit j % 32 of word j / 32
+                                    allows token j; NULL: none */
+    const int64_t* mask_of;      /* [n] the mask of each row, none where outside [0, n_masks);
+                                    NULL: row i has mask i */
+    int64_t history_width;       /* ids a row of the history has room for, < 2^28 */
+    int64_t ld_history;          /* row pitch of the history (0: history_width) */
+    int64_t n_masks;
+    int64_t ld_masks;            /* row pitch of the masks in words (0: ceil(vocab / 32)) */
+    int32_t n_bias;              /* entries of each row's biases, at most 1024 */
+    int32_t reserved;            /* must be 0 */
+} cola_constraints_t;
+
+/* out [n x vocab] (ld_grad) = the constrained logits; out may be the logits
+ * (same pointer and pitch): then only what changes is written. */
+cola_status_t cola_constrain_logits_fwd(const cola_vocab_desc_t* desc, const cola_constraints_t* constraints,
+                                        const void* logits, void* out, void* stream);
+
+/* dlogits_j = dout_j times 1 / repetition (logits_j > 0) or repetition where the
+ * history has token j, dout_j elsewhere, 0 where masked (rounded once).  logits:
+ * the forward's own input, not its result; NULL only where no repetition is
+ * given.  dlogits may be dout or the logits (same pointer and pitch). */
+cola_status_t cola_constrain_logits_bwd(const cola_vocab_desc_t* desc, const cola_constraints_t* constraints,
+                                        const void* logits, const void* dout, void* dlogits, void* stream);
+
+/* ---- token embedding ----
+ * The other end of the vocabulary: the input X of the first layer from token
+ * ids, X_t = scale E[ids_t], and the table's gradient from dX.  (The paper
+ * leaves the embedding full-rank.)
+ *
+ * Conventions as for the layer: E, X, dX and dE 16-byte aligned, row pitches a
+ * multiple of 8 elements, whatever the width d; each bf16 or fp32.  ids: int64;
+ * those outside [0, vocab) name no token: their rows of X are 0, their rows of dX
+ * are not used.  Limits: vocab and d <= 2^20, n < 2^28. */
+typedef struct {
+    int64_t n;          /* tokens */
+    int64_t vocab;      /* rows of the table */
+    int64_t d;          /* width of a row */
+    int64_t ld_e;       /* row pitch of E in elements (0: d) */
+    int64_t ld_x;       /* row pitch of X and dX (0: d) */
+    int64_t ld_de;      /* row pitch of dE (0: d) */
+    float scale;        /* finite */
+    int32_t dtype_e;    /* cola_dtype_t of E */
+    int32_t dtype_x;    /* of X and dX */
+    int32_t dtype_de;   /* of dE */
+    int32_t accumulate; /* 0: dE is overwritten, rows that no token names with 0;
+                           1: dE (fp32) is added into, rows that no token names are left alone */
+    int32_t reserved;   /* must be 0 */
+} cola_embed_desc_t;
+
+/* X [n x d] (ld_x) = scale E[ids], rounded once.  E [vocab x d] (ld_e). */
+cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const int64_t* ids, void* X, void* stream);
+
+/* Bytes of workspace cola_embed_bwd needs on the current device (ws as for the
+ * layer's calls; the same workspace may serve both, one call at a time). */
+cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* bytes);
+
+/* dE_v = scale sum of dX_t over the tokens t with ids_t = v, [vocab x d] (ld_de).
+ * The tokens are sorted by id, and each row's sum is taken in fp32 in an order
+ * that depends on the ids, n, d and the device alone: two calls give the same
+ * bits.  A tied table accumulates this onto the output embedding's gradient. */
+cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, const void* dX, void* dE, void* ws,
+                             size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, read and clear the workspace status word.
  * Returns COLA_OK, or COLA_ERR_DEVICE_TIMEOUT if a kernel that used this
  * workspace gave up on a wait since the last check (*code_out, if not NULL,
@@ -495,7 +587,12 @@ typedef enum {
     COLA_KERNEL_REPACK = 10,     /* A copied to an aligned pitch in the workspace, ahead of a large
                                     GEMM that reads it            (M=rows, N=d_in, K=0) */
     COLA_KERNEL_TOKEN_LOGPROB = 11, /* cola_token_logprob_*                 (M=n, N=vocab, K=k) */
-    COLA_KERNEL_TOPK_DISTILL = 12   /* cola_topk_distill_*                  (M=n, N=vocab, K=k) */
+    COLA_KERNEL_TOPK_DISTILL = 12,  /* cola_topk_distill_*                  (M=n, N=vocab, K=k) */
+    COLA_KERNEL_CONSTRAIN = 13,     /* cola_constrain_logits_*              (M=n, N=vocab, K=history width) */
+    COLA_KERNEL_EMBED = 14,         /* cola_embed_fwd                       (M=n, N=d, K=vocab) */
+    COLA_KERNEL_EMBED_SORT = 15,    /* cola_embed_bwd: tokens by id         (M=n, N=d, K=vocab) */
+    COLA_KERNEL_EMBED_SUM = 16,     /* cola_embed_bwd: sums within chunks of the sorted tokens (`splits` of them) */
+    COLA_KERNEL_EMBED_JOIN = 17     /* cola_embed_bwd: sums that cross chunks */
 } cola_kernel_t;
 
 typedef struct {

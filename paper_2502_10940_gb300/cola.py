@@ -31,10 +31,13 @@ SYMBOLS = ("cola_workspace_size", "cola_workspace_init", "cola_fwd", "cola_bwd",
            "cola_set_cluster_splitk",
            "cola_token_logprob_fwd", "cola_token_logprob_bwd", "cola_token_logprob_step",
            "cola_topk_distill_fwd", "cola_topk_distill_bwd", "cola_topk_distill_step",
+           "cola_constrain_logits_fwd", "cola_constrain_logits_bwd",
+           "cola_embed_fwd", "cola_embed_workspace_size", "cola_embed_bwd",
            "cola_status_string")
 STATIC_SCRATCH_BYTES = 64 * 1024 * 1024
 KERNELS = {0: "fwd_zh", 1: "fwd_y", 2: "bwd_dz", 3: "wgrad", 4: "reduce", 5: "bwd_dx", 6: "sigma", 7: "fwd_glu", 8: "fwd_fused",
-           9: "bwd_fused", 10: "repack", 11: "token_logprob", 12: "topk_distill"}
+           9: "bwd_fused", 10: "repack", 11: "token_logprob", 12: "topk_distill",
+           13: "constrain", 14: "embed", 15: "embed_sort", 16: "embed_sum", 17: "embed_join"}
 
 
 class ColaError(RuntimeError):
@@ -54,6 +57,19 @@ class cola_vocab_desc_t(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("vocab", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
                 ("temperature", ctypes.c_float), ("teacher_temperature", ctypes.c_float), ("dtype", ctypes.c_int32),
                 ("k", ctypes.c_int32), ("rest", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class cola_constraints_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("history", "history_len", "prompt_len", "repetition", "frequency",
+                                                     "presence", "bias_ids", "bias", "masks", "mask_of")] + [
+        (name, ctypes.c_int64) for name in ("history_width", "ld_history", "n_masks", "ld_masks")] + [
+        ("n_bias", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class cola_embed_desc_t(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("n", "vocab", "d", "ld_e", "ld_x", "ld_de")] + [
+        ("scale", ctypes.c_float)] + [
+        (name, ctypes.c_int32) for name in ("dtype_e", "dtype_x", "dtype_de", "accumulate", "reserved")]
 
 
 class cola_trace_slot_t(ctypes.Structure):
@@ -129,6 +145,18 @@ def lib():
             f = getattr(l, name)
             f.argtypes = [V] + [_vp] * (count + 1)
             f.restype = st
+        C = ctypes.POINTER(cola_constraints_t)
+        l.cola_constrain_logits_fwd.argtypes = [V, C] + [_vp] * 3
+        l.cola_constrain_logits_fwd.restype = st
+        l.cola_constrain_logits_bwd.argtypes = [V, C] + [_vp] * 4
+        l.cola_constrain_logits_bwd.restype = st
+        M = ctypes.POINTER(cola_embed_desc_t)
+        l.cola_embed_fwd.argtypes = [M] + [_vp] * 4
+        l.cola_embed_fwd.restype = st
+        l.cola_embed_workspace_size.argtypes = [M, ctypes.POINTER(ctypes.c_size_t)]
+        l.cola_embed_workspace_size.restype = st
+        l.cola_embed_bwd.argtypes = [M] + [_vp] * 4 + [ctypes.c_size_t, _vp]
+        l.cola_embed_bwd.restype = st
         l.cola_status_string.argtypes = [ctypes.c_int]
         l.cola_status_string.restype = ctypes.c_char_p
         _lib = l
@@ -290,6 +318,81 @@ def cola_topk_distill_step(d, logits, t_ids, t_vals, t_lse, dloss, loss, dlogits
                                         _ptr(dloss), _ptr(loss), _ptr(dlogits), _stream(stream)), "cola_topk_distill_step")
 
 
+def _of(name, t, dtype, dim):
+    if t is not None and (t.dtype != dtype or t.dim() != dim or t.stride(-1) != 1):
+        raise ValueError(f"{name}: {dim} dimension(s) of {dtype} with unit stride along the last, got {t.dtype} of strides {t.stride()}")
+    return t
+
+
+def constraints(history=None, history_len=None, prompt_len=None, *, repetition=None, frequency=None, presence=None, bias_ids=None,
+                bias=None, masks=None, mask_of=None):
+    """What cola_constrain_logits_* imposes on n rows of logits (include/cola.h):
+    history [n x width] int64 token ids, the first history_len [n] of a row used,
+    its first prompt_len [n] the prompt; repetition, frequency, presence [n] fp32;
+    bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x ceil(vocab / 32)]
+    int32 words of bits, mask_of [n] int64 the mask of each row.  Keeps the tensors."""
+    kept = dict(history=_of("history", history, torch.int64, 2), history_len=_of("history_len", history_len, torch.int64, 1),
+                prompt_len=_of("prompt_len", prompt_len, torch.int64, 1), repetition=_of("repetition", repetition, torch.float32, 1),
+                frequency=_of("frequency", frequency, torch.float32, 1), presence=_of("presence", presence, torch.float32, 1),
+                bias_ids=_of("bias_ids", bias_ids, torch.int64, 2), bias=_of("bias", bias, torch.float32, 2),
+                masks=_of("masks", masks, torch.int32, 2), mask_of=_of("mask_of", mask_of, torch.int64, 1))
+    if (bias_ids is None) != (bias is None) or (bias is not None and not (bias_ids.is_contiguous() and bias.is_contiguous()
+                                                                           and bias.shape == bias_ids.shape)):
+        raise ValueError("bias_ids and bias: both or neither, contiguous, of one shape")
+    c = cola_constraints_t()
+    for name, t in kept.items():
+        setattr(c, name, _ptr(t))
+    if history is not None:
+        c.history_width, c.ld_history = history.shape[1], history.stride(0)
+    if masks is not None:
+        c.n_masks, c.ld_masks = masks.shape[0], masks.stride(0)
+    c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
+    c.tensors = kept
+    return c
+
+
+def cola_constrain_logits_fwd(d, c, logits, out, stream=None):
+    """Penalties for tokens that occurred, biases and masks on rows of logits
+    (d: vocab_desc, c: constraints); out may be the logits."""
+    _check(lib().cola_constrain_logits_fwd(ctypes.byref(d), ctypes.byref(c), _ptr(logits), _ptr(out), _stream(stream)),
+           "cola_constrain_logits_fwd")
+
+
+def cola_constrain_logits_bwd(d, c, logits, dout, dlogits, stream=None):
+    """The gradient at the logits from the one at the constrained logits."""
+    _check(lib().cola_constrain_logits_bwd(ctypes.byref(d), ctypes.byref(c), _ptr(logits), _ptr(dout), _ptr(dlogits),
+                                           _stream(stream)), "cola_constrain_logits_bwd")
+
+
+def embed_desc(n, vocab, d, ld_e=0, ld_x=0, ld_de=0, scale=1.0, dtype_e="bf16", dtype_x="bf16", dtype_de="bf16", accumulate=False):
+    """n tokens of a table E [vocab x d] at pitch ld_e; X and dX at pitch ld_x, dE
+    at pitch ld_de (0: d), each "bf16", "f32" or the torch type; accumulate: dE
+    (fp32) is added into."""
+    m = cola_embed_desc_t()
+    m.n, m.vocab, m.d, m.ld_e, m.ld_x, m.ld_de = int(n), int(vocab), int(d), int(ld_e), int(ld_x), int(ld_de)
+    m.scale = float(scale)
+    m.dtype_e, m.dtype_x, m.dtype_de = (DTYPE.get(t, -1) if not isinstance(t, int) else t for t in (dtype_e, dtype_x, dtype_de))
+    m.accumulate, m.reserved = int(bool(accumulate)), 0
+    return m
+
+
+def cola_embed_fwd(d, E, ids, X, stream=None):
+    """X = scale E[ids]; rows of ids outside the vocabulary are 0."""
+    _check(lib().cola_embed_fwd(ctypes.byref(d), _ptr(E), _ptr(ids), _ptr(X), _stream(stream)), "cola_embed_fwd")
+
+
+def cola_embed_workspace_size(d: cola_embed_desc_t) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().cola_embed_workspace_size(ctypes.byref(d), ctypes.byref(out)), "cola_embed_workspace_size")
+    return int(out.value)
+
+
+def cola_embed_bwd(d, ids, dX, dE, ws, stream=None):
+    """The table's gradient: for each row the scaled sum of dX over its tokens."""
+    _check(lib().cola_embed_bwd(ctypes.byref(d), _ptr(ids), _ptr(dX), _ptr(dE), _ptr(ws), _nbytes(ws), _stream(stream)),
+           "cola_embed_bwd")
+
+
 def cola_selftest_wait_timeout(ws, stream=None):
     _check(lib().cola_selftest_wait_timeout(_ptr(ws), _nbytes(ws), _stream(stream)), "cola_selftest_wait_timeout")
 
@@ -416,7 +519,15 @@ def ld_of(t) -> int:
 
 def workspace(d: cola_desc_t, nproj: int = 1, device="cuda"):
     """A zero-initialised workspace tensor for `d` (allocated by torch)."""
-    nbytes = cola_workspace_size(d, nproj)
+    return _workspace(cola_workspace_size(d, nproj), device)
+
+
+def embed_workspace(d: cola_embed_desc_t, device="cuda"):
+    """The same for cola_embed_bwd."""
+    return _workspace(cola_embed_workspace_size(d), device)
+
+
+def _workspace(nbytes, device):
     ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
     off = (-ws.data_ptr()) % 256
     ws = ws[off:off + nbytes]

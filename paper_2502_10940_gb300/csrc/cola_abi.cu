@@ -12,6 +12,8 @@
 #include <mutex>
 
 #include "cola.h"
+#include "constrain.cuh"
+#include "embed.cuh"
 #include "fused_layer.cuh"
 #include "gemm_launch.cuh"
 #include "host_plan.cuh"
@@ -1748,6 +1750,218 @@ cola_status_t cola_topk_distill_step(const cola_vocab_desc_t* desc, const void* 
     p.dloss = dloss;
     p.loss = loss;
     return run_vocab(desc, p, true, VOCAB_STEP, stream);
+}
+
+// ------------------------------------------------------- constraints on logits
+}  // extern "C"
+
+namespace cola {
+namespace {
+
+// The checks that the constraints' forward and backward share, and what their
+// kernel takes from the two descriptors.  `src` is copied into `dst`.
+cola_status_t constrain_params(const cola_vocab_desc_t* d, const cola_constraints_t* c, const void* logits, const void* src,
+                               void* dst, ConstrainParams* p)
+{
+    if (!d || !c || !src || !dst) return COLA_ERR_INVALID;
+    VocabParams v;
+    COLA_TRY(vocab_params(d, src, dst, true, &v));
+    if (c->reserved != 0 || c->history_width < 0 || c->ld_history < 0 || c->n_masks < 0 || c->ld_masks < 0 || c->n_bias < 0)
+        return COLA_ERR_INVALID;
+    const int64_t ld_history = c->ld_history ? c->ld_history : c->history_width;
+    const int64_t ld_masks = c->ld_masks ? c->ld_masks : (d->vocab + 31) / 32;
+    if (c->history ? c->history_width < 1 || ld_history < c->history_width
+                   : c->history_len || c->prompt_len || c->repetition || c->frequency || c->presence)
+        return COLA_ERR_INVALID;
+    if ((c->bias_ids != nullptr) != (c->bias != nullptr) || (c->bias != nullptr) != (c->n_bias > 0)) return COLA_ERR_INVALID;
+    if (c->masks ? c->n_masks < (c->mask_of ? 1 : d->n) || ld_masks < (d->vocab + 31) / 32 : c->mask_of != nullptr)
+        return COLA_ERR_INVALID;
+    const int64_t lim = (int64_t(1) << 31) - 256;
+    if (c->history_width > HISTORY_MAX || ld_history > lim || ld_masks > lim || c->n_masks > lim || c->n_bias > BIAS_MAX)
+        return COLA_ERR_UNSUPPORTED;
+    for (const void* q : {static_cast<const void*>(c->history), static_cast<const void*>(c->history_len),
+                          static_cast<const void*>(c->prompt_len), static_cast<const void*>(c->bias_ids),
+                          static_cast<const void*>(c->mask_of)})
+        if (!aligned_to(q, 8)) return COLA_ERR_ALIGN;
+    for (const void* q : {static_cast<const void*>(c->repetition), static_cast<const void*>(c->frequency),
+                          static_cast<const void*>(c->presence), static_cast<const void*>(c->bias),
+                          static_cast<const void*>(c->masks)})
+        if (!aligned_to(q, 4)) return COLA_ERR_ALIGN;
+    if (logits && !aligned_to(logits, d->dtype == COLA_DTYPE_BF16 ? 2 : 4)) return COLA_ERR_ALIGN;
+    *p = ConstrainParams{};
+    p->logits = logits;
+    p->src = src;
+    p->dst = dst;
+    p->n = v.n;
+    p->ld = v.ld;
+    p->ld_src = v.ld_d;
+    p->ld_dst = v.ld_d;
+    p->vocab = v.vocab;
+    p->history = reinterpret_cast<const long long*>(c->history);
+    p->history_width = c->history_width;
+    p->ld_history = ld_history;
+    p->history_len = reinterpret_cast<const long long*>(c->history_len);
+    p->prompt_len = reinterpret_cast<const long long*>(c->prompt_len);
+    p->repetition = c->repetition;
+    p->frequency = c->frequency;
+    p->presence = c->presence;
+    p->bias_ids = reinterpret_cast<const long long*>(c->bias_ids);
+    p->bias = c->bias;
+    p->n_bias = c->n_bias;
+    p->masks = c->masks;
+    p->n_masks = c->n_masks;
+    p->ld_masks = ld_masks;
+    p->mask_of = reinterpret_cast<const long long*>(c->mask_of);
+    return COLA_OK;
+}
+
+cola_status_t run_constrain(const cola_vocab_desc_t* d, const ConstrainParams& p, bool backward, void* stream)
+{
+    int sms = 0;
+    COLA_TRY(device_info(&sms));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t mnk[1][3] = {{p.n, p.vocab, p.history ? p.history_width : 0}};
+    return launched(traced(COLA_KERNEL_CONSTRAIN, 1, mnk, 1, 0, st, [&] { return launch_constrain(p, d->dtype, backward, sms, st); }));
+}
+
+}  // namespace
+}  // namespace cola
+
+extern "C" {
+
+cola_status_t cola_constrain_logits_fwd(const cola_vocab_desc_t* desc, const cola_constraints_t* constraints,
+                                        const void* logits, void* out, void* stream)
+{
+    ConstrainParams p;
+    COLA_TRY(constrain_params(desc, constraints, logits, logits, out, &p));
+    p.ld_src = p.ld;
+    if (logits == out && p.ld != p.ld_dst) return COLA_ERR_INVALID;
+    return run_constrain(desc, p, false, stream);
+}
+
+cola_status_t cola_constrain_logits_bwd(const cola_vocab_desc_t* desc, const cola_constraints_t* constraints,
+                                        const void* logits, const void* dout, void* dlogits, void* stream)
+{
+    ConstrainParams p;
+    COLA_TRY(constrain_params(desc, constraints, logits, dout, dlogits, &p));
+    if (!constraints->repetition) p.history = nullptr;   // nothing else scales a gradient
+    if (p.history && !logits) return COLA_ERR_INVALID;
+    if (logits == dlogits && p.ld != p.ld_dst) return COLA_ERR_INVALID;
+    p.n_bias = 0;
+    return run_constrain(desc, p, true, stream);
+}
+
+// ----------------------------------------------------------- token embedding
+}  // extern "C"
+
+namespace cola {
+namespace {
+
+struct EmbedShape {
+    int64_t ld_e, ld_x, ld_de;
+};
+
+cola_status_t check_embed(const cola_embed_desc_t* d, EmbedShape* s)
+{
+    if (!d) return COLA_ERR_INVALID;
+    if (d->n < 1 || d->vocab < 1 || d->d < 1 || d->ld_e < 0 || d->ld_x < 0 || d->ld_de < 0 || d->reserved != 0)
+        return COLA_ERR_INVALID;
+    for (int32_t t : {d->dtype_e, d->dtype_x, d->dtype_de})
+        if (t != COLA_DTYPE_BF16 && t != COLA_DTYPE_F32) return COLA_ERR_INVALID;
+    if (d->accumulate != 0 && (d->accumulate != 1 || d->dtype_de != COLA_DTYPE_F32)) return COLA_ERR_INVALID;
+    if (!std::isfinite(d->scale)) return COLA_ERR_INVALID;
+    *s = EmbedShape{d->ld_e ? d->ld_e : d->d, d->ld_x ? d->ld_x : d->d, d->ld_de ? d->ld_de : d->d};
+    const int64_t lim = (int64_t(1) << 31) - 256;
+    for (int64_t ld : {s->ld_e, s->ld_x, s->ld_de}) {
+        if (ld < d->d || ld % 8) return COLA_ERR_INVALID;
+        if (ld > lim) return COLA_ERR_UNSUPPORTED;
+    }
+    // CTAs of 256 eight-column pieces are numbered in 31 bits
+    if (d->vocab > EMBED_VOCAB_MAX || d->d > EMBED_MAX_WIDTH || d->n >= EMBED_MAX_ROWS || d->n * ((d->d + 7) / 8) > lim * 256)
+        return COLA_ERR_UNSUPPORTED;
+    return COLA_OK;
+}
+
+}  // namespace
+}  // namespace cola
+
+extern "C" {
+
+cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const int64_t* ids, void* X, void* stream)
+{
+    EmbedShape s;
+    COLA_TRY(check_embed(desc, &s));
+    COLA_TRY(check_ptrs({E, X}));
+    if (!ids) return COLA_ERR_INVALID;
+    if (!aligned_to(ids, 8)) return COLA_ERR_ALIGN;
+    int sms = 0;
+    COLA_TRY(device_info(&sms));
+    EmbedParams p = {};
+    p.ids = reinterpret_cast<const long long*>(ids);
+    p.src = E;
+    p.dst = X;
+    p.n = desc->n;
+    p.ld_src = s.ld_e;
+    p.ld_dst = s.ld_x;
+    p.vocab = static_cast<int>(desc->vocab);
+    p.d = static_cast<int>(desc->d);
+    p.scale = desc->scale;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
+    return launched(traced(COLA_KERNEL_EMBED, 1, mnk, 1, 0, st,
+                           [&] { return launch_embed_rows(p, desc->dtype_e, desc->dtype_x, st); }));
+}
+
+cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* bytes)
+{
+    EmbedShape s;
+    COLA_TRY(check_embed(desc, &s));
+    if (!bytes) return COLA_ERR_INVALID;
+    int sms = 0;
+    COLA_TRY(device_info(&sms));
+    *bytes = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), sms, WS_HEADER).total;
+    return COLA_OK;
+}
+
+cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, const void* dX, void* dE, void* ws,
+                             size_t ws_bytes, void* stream)
+{
+    EmbedShape s;
+    COLA_TRY(check_embed(desc, &s));
+    COLA_TRY(check_ptrs({dX, dE}));
+    if (!ids || !ws) return COLA_ERR_INVALID;
+    if (!aligned_to(ids, 8) || !aligned_to(ws, WS_ALIGN)) return COLA_ERR_ALIGN;
+    int sms = 0;
+    COLA_TRY(device_info(&sms));
+    const EmbedLayout l = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), sms, WS_HEADER);
+    if (ws_bytes < l.total) return COLA_ERR_WORKSPACE;
+    unsigned char* base = static_cast<unsigned char*>(ws);
+    EmbedParams p = {};
+    p.ids = reinterpret_cast<const long long*>(ids);
+    p.src = dX;
+    p.dst = dE;
+    p.n = desc->n;
+    p.ld_src = s.ld_x;
+    p.ld_dst = s.ld_de;
+    p.vocab = static_cast<int>(desc->vocab);
+    p.d = static_cast<int>(desc->d);
+    p.scale = desc->scale;
+    p.accumulate = desc->accumulate;
+    p.pairs[0] = reinterpret_cast<uint2*>(base + l.pairs[0]);
+    p.pairs[1] = reinterpret_cast<uint2*>(base + l.pairs[1]);
+    p.count = reinterpret_cast<unsigned int*>(base + l.count);
+    p.present = reinterpret_cast<unsigned int*>(base + l.present);
+    p.partials = reinterpret_cast<float*>(base + l.partials);
+    p.chunk = l.chunk;
+    p.chunks = l.chunks;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
+    COLA_TRY(launched(traced(COLA_KERNEL_EMBED_SORT, 1, mnk, 1, 0, st, [&] { return launch_embed_sort(p, st); })));
+    COLA_TRY(launched(traced(COLA_KERNEL_EMBED_SUM, 1, mnk, p.chunks, 0, st,
+                             [&] { return launch_embed_sums(p, desc->dtype_x, desc->dtype_de, sms, st); })));
+    if (p.chunks == 1) return COLA_OK;
+    return launched(traced(COLA_KERNEL_EMBED_JOIN, 1, mnk, p.chunks, 0, st,
+                           [&] { return launch_embed_join(p, desc->dtype_de, st); }));
 }
 
 cola_status_t cola_check_status(void* ws, void* stream, uint32_t* code_out)

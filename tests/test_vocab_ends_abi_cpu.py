@@ -1,0 +1,151 @@
+"""Refusals of the embedding's and the constraints' entry points, before any
+device is touched, and the layouts of their descriptors."""
+import ctypes
+
+import pytest
+import torch
+
+from test_abi_cpu import FAKE, L  # noqa: F401
+
+
+# ------------------------------------------------------------------ embedding
+def _embed(L, name, d, args):   # noqa: F811
+    d = ctypes.byref(d) if d is not None else None
+    if name == "cola_embed_workspace_size":
+        return L.lib().cola_embed_workspace_size(d, *args)
+    return getattr(L.lib(), name)(d, *args, None)
+
+
+EMBED = {   # arguments after the descriptor that pass every check but the device's
+    "cola_embed_fwd": [FAKE] * 3,
+    "cola_embed_workspace_size": [ctypes.byref(ctypes.c_size_t(0))],
+    "cola_embed_bwd": [FAKE] * 4 + [1 << 40],
+}
+
+
+def test_layouts(L):   # noqa: F811
+    assert ctypes.sizeof(L.cola_embed_desc_t) == 6 * 8 + 6 * 4
+    assert ctypes.sizeof(L.cola_constraints_t) == 10 * 8 + 4 * 8 + 2 * 4
+
+
+@pytest.mark.parametrize("name", sorted(EMBED))
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), 1), (dict(n=-1), 1), (dict(vocab=0), 1), (dict(d=0), 1), (dict(d=-8), 1), (dict(ld_e=56), 1), (dict(ld_x=-64), 1),
+    (dict(ld_de=68), 1), (dict(d=60), 1), (dict(d=60, ld_e=64, ld_x=64), 1), (dict(scale=float("nan")), 1),
+    (dict(scale=float("inf")), 1), (dict(dtype_e="f16"), 1), (dict(dtype_x=7), 1), (dict(dtype_de=-2), 1), (dict(accumulate=True), 1),
+    (dict(vocab=(1 << 20) + 1), 3), (dict(n=1 << 28), 3), (dict(d=(1 << 20) + 8), 3), (dict(ld_x=1 << 31), 3),
+    (dict(n=(1 << 28) - 1, d=1 << 20), 3),
+])
+def test_bad_embed_descriptors(L, name, kw, code):   # noqa: F811
+    assert _embed(L, name, L.embed_desc(**{**dict(n=4, vocab=100, d=64), **kw}), EMBED[name]) == code
+
+
+@pytest.mark.parametrize("name", sorted(EMBED))
+def test_embed_reserved_and_missing(L, name):   # noqa: F811
+    assert _embed(L, name, None, EMBED[name]) == 1
+    for field, value in (("reserved", 1), ("accumulate", 2), ("accumulate", -1)):
+        d = L.embed_desc(4, 100, 64, dtype_de="f32")
+        setattr(d, field, value)
+        assert _embed(L, name, d, EMBED[name]) == 1
+
+
+def test_embed_pointers(L):   # noqa: F811
+    d = L.embed_desc(4, 100, 64)
+    for name, offsets in (("cola_embed_fwd", (8, 4, 8)), ("cola_embed_bwd", (4, 8, 8, 128))):   # E, ids, X; ids, dX, dE, ws
+        for i, off in enumerate(offsets):
+            for value, code in ((None, 1), (FAKE + off, 2)):
+                a = list(EMBED[name])
+                a[i] = value
+                assert _embed(L, name, d, a) == code, (name, i)
+    assert L.lib().cola_embed_workspace_size(ctypes.byref(d), None) == 1
+
+
+# the last values that pass (what comes next is that the ids are misaligned) and the first that do not
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=(1 << 28) - 1), 2), (dict(n=1 << 28), 3), (dict(vocab=1 << 20), 2), (dict(vocab=(1 << 20) + 1), 3), (dict(d=1 << 20), 2),
+    (dict(ld_e=(1 << 31) - 256), 2), (dict(ld_e=(1 << 31) - 248), 3), (dict(d=61, ld_e=64, ld_x=64, ld_de=72), 2),
+    (dict(accumulate=True, dtype_de="f32"), 2),
+])
+def test_edges_of_the_embed_limits(L, kw, code):   # noqa: F811
+    d = L.embed_desc(**{**dict(n=4, vocab=100, d=64), **kw})
+    assert _embed(L, "cola_embed_fwd", d, [FAKE, FAKE + 4, FAKE]) == code
+    assert _embed(L, "cola_embed_bwd", d, [FAKE + 4, FAKE, FAKE, FAKE, 1 << 40]) == code
+
+
+# ---------------------------------------------------------------- constraints
+CONSTRAIN = {"cola_constrain_logits_fwd": 2, "cola_constrain_logits_bwd": 3}   # pointers after the constraints
+
+
+def _limits(L, **kw):   # noqa: F811
+    c = L.constraints()
+    full = dict(history=FAKE, history_len=FAKE, prompt_len=FAKE, repetition=FAKE, frequency=FAKE, presence=FAKE, bias_ids=FAKE,
+                bias=FAKE, masks=FAKE, mask_of=FAKE, history_width=10, n_masks=2, n_bias=3)
+    for k, v in {**full, **kw}.items():
+        setattr(c, k, v)
+    return c
+
+
+def _constrain(L, name, d, c, args):   # noqa: F811
+    ref = lambda s: ctypes.byref(s) if s is not None else None   # noqa: E731
+    return getattr(L.lib(), name)(ref(d), ref(c), *args, None)
+
+
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+@pytest.mark.parametrize("kw,code", [
+    (dict(history=None), 1), (dict(history_width=0), 1), (dict(history_width=-1), 1), (dict(ld_history=9), 1), (dict(ld_history=-9), 1),
+    (dict(bias=None), 1), (dict(bias_ids=None), 1), (dict(n_bias=0), 1), (dict(n_bias=-1), 1), (dict(n_masks=0), 1), (dict(n_masks=-1), 1),
+    (dict(masks=None), 1), (dict(ld_masks=3), 1), (dict(ld_masks=-4), 1), (dict(mask_of=None, n_masks=3), 1), (dict(reserved=1), 1),
+    (dict(n_bias=1025), 3), (dict(history_width=1 << 28), 3), (dict(ld_history=1 << 31), 3), (dict(ld_masks=1 << 31), 3),
+    (dict(history=FAKE + 4), 2), (dict(history_len=FAKE + 4), 2), (dict(prompt_len=FAKE + 4), 2), (dict(bias_ids=FAKE + 4), 2),
+    (dict(mask_of=FAKE + 4), 2), (dict(repetition=FAKE + 2), 2), (dict(frequency=FAKE + 2), 2), (dict(presence=FAKE + 2), 2),
+    (dict(bias=FAKE + 2), 2), (dict(masks=FAKE + 2), 2),
+])
+def test_bad_constraints(L, name, kw, code):   # noqa: F811
+    assert _constrain(L, name, L.vocab_desc(4, 100), _limits(L, **kw), [FAKE, FAKE + 64, FAKE + 128][:CONSTRAIN[name]]) == code
+
+
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), 1), (dict(vocab=0), 1), (dict(ld=99), 1), (dict(ld_grad=99), 1), (dict(dtype="f16"), 1), (dict(temperature=0.0), 1),
+    (dict(vocab=(1 << 20) + 1), 3), (dict(n=1 << 28), 3), (dict(ld=1 << 31), 3), (dict(ld_grad=1 << 31), 3),
+])
+def test_bad_logit_descriptors(L, name, kw, code):   # noqa: F811
+    d = L.vocab_desc(**{**dict(n=4, vocab=100), **kw})
+    assert _constrain(L, name, d, _limits(L, mask_of=FAKE, ld_masks=1 << 20), [FAKE] * CONSTRAIN[name]) == code
+
+
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+def test_constrain_pointers(L, name):   # noqa: F811
+    d, c, count = L.vocab_desc(4, 100), _limits(L), CONSTRAIN[name]
+    assert _constrain(L, name, None, c, [FAKE] * count) == 1
+    assert _constrain(L, name, d, None, [FAKE] * count) == 1
+    for i in range(count):
+        for value, code in ((None, 1), (FAKE + 1, 2)):
+            a = [FAKE] * count
+            a[i] = value
+            assert _constrain(L, name, d, c, a) == code, i
+    # results over the logits go by one pitch
+    d = L.vocab_desc(4, 100, ld=104, ld_grad=112)
+    assert _constrain(L, name, d, c, [FAKE] * count) == 1
+    # a gradient without a repetition penalty needs no logits: what comes next is a misaligned gradient
+    if count == 3:
+        d = L.vocab_desc(4, 100)
+        assert _constrain(L, name, d, _limits(L, repetition=None), [None, FAKE, FAKE + 1]) == 2
+
+
+def test_the_builder_checks_types(L):   # noqa: F811
+    ids = torch.zeros((2, 5), dtype=torch.int64)
+    for kw in (dict(history=ids.int()), dict(history=ids[0]), dict(history=ids, history_len=torch.zeros(2)),
+               dict(history=ids, repetition=torch.ones(2, dtype=torch.float64)), dict(masks=ids), dict(bias_ids=ids, bias=torch.zeros(2, 4)),
+               dict(bias_ids=ids[:, ::2], bias=torch.zeros(2, 3)), dict(history=ids.t()), dict(bias=torch.zeros(2, 5))):
+        with pytest.raises(ValueError):
+            L.constraints(**kw)
+    c = L.constraints(ids[:, 1:4], masks=torch.zeros((3, 9), dtype=torch.int32)[:, :4])
+    assert (c.history_width, c.ld_history, c.n_masks, c.ld_masks, c.n_bias) == (3, 5, 3, 9, 0)
+
+
+def test_bindings_raise(L):   # noqa: F811
+    with pytest.raises(L.ColaError, match="cola_embed_fwd"):
+        L.cola_embed_fwd(L.embed_desc(0, 1, 8), FAKE, FAKE, FAKE, stream=0)
+    with pytest.raises(L.ColaError, match="cola_constrain_logits_fwd"):
+        L.cola_constrain_logits_fwd(L.vocab_desc(0, 1), L.constraints(), FAKE, FAKE, stream=0)
