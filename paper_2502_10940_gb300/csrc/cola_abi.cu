@@ -1909,7 +1909,7 @@ cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
     return launched(traced(COLA_KERNEL_EMBED, 1, mnk, 1, 0, st,
-                           [&] { return launch_embed_rows(p, desc->dtype_e, desc->dtype_x, st); }));
+                           [&] { return launch_embed_rows(p, desc->dtype_e, desc->dtype_x, sms, st); }));
 }
 
 cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* bytes)
@@ -1947,21 +1947,34 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
     p.d = static_cast<int>(desc->d);
     p.scale = desc->scale;
     p.accumulate = desc->accumulate;
-    p.pairs[0] = reinterpret_cast<uint2*>(base + l.pairs[0]);
-    p.pairs[1] = reinterpret_cast<uint2*>(base + l.pairs[1]);
-    p.count = reinterpret_cast<unsigned int*>(base + l.count);
-    p.present = reinterpret_cast<unsigned int*>(base + l.present);
+    p.sorted = reinterpret_cast<uint2*>(base + l.sorted);
+    p.count = reinterpret_cast<unsigned int*>(base + l.counts);
+    p.long_count = p.count + 1;
+    p.long_sums = reinterpret_cast<unsigned int*>(base + l.long_sums);
     p.partials = reinterpret_cast<float*>(base + l.partials);
     p.chunk = l.chunk;
     p.chunks = l.chunks;
+    p.between = reinterpret_cast<uint2*>(base + l.between);
+    p.present = reinterpret_cast<unsigned int*>(base + l.present);
+    for (int i = 0; i < 2; ++i) p.hist[i] = reinterpret_cast<unsigned int*>(base + l.hist[i]);
+    p.low = l.low;
+    p.high = l.high;
+    p.sort_ctas = l.sort_ctas;
+    p.sort_each = l.sort_each;
+    p.filled = p.accumulate ? p.vocab : 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
-    COLA_TRY(launched(traced(COLA_KERNEL_EMBED_SORT, 1, mnk, 1, 0, st, [&] { return launch_embed_sort(p, st); })));
+    const bool few = p.n <= EMBED_FEW;
+    const int sorts = few ? 1 : p.high ? 4 : 2;
+    for (int i = 0; i < sorts; ++i)
+        COLA_TRY(launched(traced(COLA_KERNEL_EMBED_SORT, 1, mnk, 1, 0, st, [&] {
+            return few ? launch_embed_order(p, desc->dtype_de, sms, st) : launch_embed_sort(p, i, desc->dtype_de, sms, st);
+        })));
     COLA_TRY(launched(traced(COLA_KERNEL_EMBED_SUM, 1, mnk, p.chunks, 0, st,
                              [&] { return launch_embed_sums(p, desc->dtype_x, desc->dtype_de, sms, st); })));
     if (p.chunks == 1) return COLA_OK;
     return launched(traced(COLA_KERNEL_EMBED_JOIN, 1, mnk, p.chunks, 0, st,
-                           [&] { return launch_embed_join(p, desc->dtype_de, st); }));
+                           [&] { return launch_embed_join(p, desc->dtype_de, sms, st); }));
 }
 
 cola_status_t cola_check_status(void* ws, void* stream, uint32_t* code_out)

@@ -17,6 +17,7 @@ namespace cola {
 constexpr int EMBED_VOCAB_MAX = 1 << 20;           // rows of a table: two digits of up to ten bits
 constexpr long long EMBED_MAX_ROWS = 1ll << 28;    // tokens of a call stay below it
 constexpr int EMBED_MAX_WIDTH = 1 << 20;
+constexpr int EMBED_FEW = 8192;                    // tokens that are ordered by counting
 
 struct EmbedParams {
     const long long* ids;
@@ -27,24 +28,37 @@ struct EmbedParams {
     float scale;
     int accumulate;
     // the gradient's workspace
-    uint2* pairs[2];          // n each: (id, token); the sorted ones in [1]
+    uint2* sorted;            // (id, token)
     unsigned int* count;      // tokens that name a row
-    unsigned int* present;    // a bit per row of the table
+    unsigned int* long_count; // sums that are split over chunks
+    unsigned int* long_sums;  // the chunks they begin in
     float* partials;          // 2 per chunk, d rounded up to 8: of a sum that began before the chunk, and of one that goes on behind it
     int chunk, chunks;        // sorted tokens of a chunk; chunks of n
+    // more than EMBED_FEW tokens
+    uint2* between;           // after the first pass of the sort
+    unsigned int* present;    // a bit for each row of the table that a token names
+    unsigned int* hist[2];
+    int low, high;            // bits of the two digits (high 0: one pass)
+    int sort_ctas;
+    unsigned int sort_each;
+    int filled;               // rows of no token below this one are 0 already
 };
 
-// Byte offsets in the gradient's workspace, from `at` on.
+// Byte offsets in the gradient's workspace, from `at` on, and the shares of the work.
 struct EmbedLayout {
-    size_t pairs[2], count, present, partials, total;
-    int chunk, chunks;
+    size_t sorted, counts, long_sums, partials, between, present, hist[2], total;
+    int chunk, chunks, low, high, sort_ctas;
+    unsigned int sort_each;
 };
 EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at);
 
 // dtypes: cola_dtype_t of src and dst
-cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, cudaStream_t stream);
-cudaError_t launch_embed_sort(const EmbedParams& p, cudaStream_t stream);
+cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
+// the order of up to EMBED_FEW tokens, and the rows of no token set to 0
+cudaError_t launch_embed_order(EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);
+// that of more, in launches 0 .. 3 (0 and 1 where high is 0); the last two set rows of no token to 0
+cudaError_t launch_embed_sort(EmbedParams& p, int launch, int dtype_dst, int sms, cudaStream_t stream);
 cudaError_t launch_embed_sums(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
-cudaError_t launch_embed_join(const EmbedParams& p, int dtype_dst, cudaStream_t stream);   // where chunks > 1
+cudaError_t launch_embed_join(const EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);   // where chunks > 1
 
 }  // namespace cola
