@@ -1919,7 +1919,7 @@ cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* b
     if (!bytes) return COLA_ERR_INVALID;
     int sms = 0;
     COLA_TRY(device_info(&sms));
-    *bytes = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), sms, WS_HEADER).total;
+    *bytes = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), desc->dtype_x, sms, WS_HEADER).total;
     return COLA_OK;
 }
 
@@ -1933,7 +1933,7 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
     if (!aligned_to(ids, 8) || !aligned_to(ws, WS_ALIGN)) return COLA_ERR_ALIGN;
     int sms = 0;
     COLA_TRY(device_info(&sms));
-    const EmbedLayout l = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), sms, WS_HEADER);
+    const EmbedLayout l = embed_layout(desc->n, static_cast<int>(desc->vocab), static_cast<int>(desc->d), desc->dtype_x, sms, WS_HEADER);
     if (ws_bytes < l.total) return COLA_ERR_WORKSPACE;
     unsigned char* base = static_cast<unsigned char*>(ws);
     EmbedParams p = {};
@@ -1950,7 +1950,7 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
     p.sorted = reinterpret_cast<uint2*>(base + l.sorted);
     p.count = reinterpret_cast<unsigned int*>(base + l.counts);
     p.long_count = p.count + 1;
-    p.long_sums = reinterpret_cast<unsigned int*>(base + l.long_sums);
+    p.long_sums = reinterpret_cast<uint4*>(base + l.long_sums);
     p.partials = reinterpret_cast<float*>(base + l.partials);
     p.chunk = l.chunk;
     p.chunks = l.chunks;

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "vocab_rows.cuh"
 
@@ -11,16 +12,18 @@ namespace {
 
 // ------------------------------------------------- eight columns of a row
 // Pitches are multiples of 8 elements, so that every eight columns begin on a
-// 16-byte boundary; the last of a row may be fewer.
+// 16-byte boundary.  WHOLE: the width is one too; else the last of a row may be
+// fewer, `left` of them.
 template <class T>
 struct Eight;
 
 template <>
 struct Eight<__nv_bfloat16> {
     uint4 u;
+    template <bool WHOLE>
     __device__ __forceinline__ void load(const __nv_bfloat16* p, int left)
     {
-        if (left >= 8) {
+        if (WHOLE || left >= 8) {
             u = *reinterpret_cast<const uint4*>(p);
         } else {
             float x[8] = {};
@@ -31,9 +34,10 @@ struct Eight<__nv_bfloat16> {
         }
     }
     __device__ __forceinline__ void values(float (&x)[8]) const { Elem<__nv_bfloat16>::unpack(u, x); }
+    template <bool WHOLE>
     __device__ __forceinline__ static void store(__nv_bfloat16* p, const float (&x)[8], int left)
     {
-        if (left >= 8) {
+        if (WHOLE || left >= 8) {
             *reinterpret_cast<uint4*>(p) = Elem<__nv_bfloat16>::pack(x);
         } else {
 #pragma unroll
@@ -45,28 +49,43 @@ struct Eight<__nv_bfloat16> {
 
 template <>
 struct Eight<float> {
-    float4 a, b;
+    float x[8];
+    // in one piece where it lies on a 32-byte boundary: two pieces would touch every
+    // sector twice
+    template <bool WHOLE>
     __device__ __forceinline__ void load(const float* p, int left)
     {
-        if (left >= 8) {
-            a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        if (WHOLE || left >= 8) {
+            if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
+                asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                             : "l"(p));
+            } else {
+                const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+                x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+            }
         } else {
-            float x[8] = {};
 #pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (i < left) x[i] = p[i];
-            a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(x[4], x[5], x[6], x[7]);
+            for (int i = 0; i < 8; ++i) x[i] = i < left ? p[i] : 0.f;
         }
     }
-    __device__ __forceinline__ void values(float (&x)[8]) const
+    __device__ __forceinline__ void values(float (&y)[8]) const
     {
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i];
     }
+    template <bool WHOLE>
     __device__ __forceinline__ static void store(float* p, const float (&x)[8], int left)
     {
-        if (left >= 8) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        if (WHOLE || left >= 8) {
+            if ((reinterpret_cast<uintptr_t>(p) & 16) == 0) {
+                asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]),
+                             "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "l"(p)
+                             : "memory");
+            } else {
+                reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+                reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 7; ++i)
@@ -75,51 +94,60 @@ struct Eight<float> {
     }
 };
 
+// `1 << shift` threads of a CTA of 256 share a row, eight columns each; wider rows are
+// shared by `tiles` such groups.
+struct Groups {
+    int shift, tiles;
+};
+
 // ------------------------------------------------------------------ lookup
-// UNITS pieces of eight columns a thread, 256 apart in the rows laid end to end:
-// their ids and then their rows are loaded together.
-template <class TE, class TX, int UNITS>
-__global__ void __launch_bounds__(256) embed_rows_kernel(const EmbedParams P)
+// ROWS rows a thread, whose ids and then whose columns are loaded together.
+template <class TE, class TX, bool WHOLE, int ROWS>
+__global__ void __launch_bounds__(256) embed_rows_kernel(const EmbedParams P, const Groups g)
 {
-    const unsigned int units = (P.d + 7) / 8;
-    const long long first = blockIdx.x * (256ll * UNITS), t0 = first / units;
-    const unsigned int c0 = static_cast<unsigned int>(first - t0 * units) + threadIdx.x;
-    long long id[UNITS];
-    Eight<TE> e[UNITS];
-    const auto row = [&](int u) { return t0 + (c0 + u * 256) / units; };
-    const auto col = [&](int u) { return static_cast<int>((c0 + u * 256) % units) * 8; };
+    const int c = (blockIdx.y << g.shift | (threadIdx.x & ((1 << g.shift) - 1))) * 8, step = 256 >> g.shift;
+    if (c >= P.d) return;
+    const long long t0 = static_cast<long long>(blockIdx.x) * (ROWS * step) + (threadIdx.x >> g.shift);
+    const TE* src = static_cast<const TE*>(P.src) + c;
+    TX* dst = static_cast<TX*>(P.dst) + c;
+    long long id[ROWS];
+    Eight<TE> e[ROWS];
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) id[u] = row(u) < P.n ? P.ids[row(u)] : -1;
+    for (int u = 0; u < ROWS; ++u) {
+        id[u] = t0 + u * step < P.n ? P.ids[t0 + u * step] : -1;
+        if (id[u] >= P.vocab) id[u] = -1;
+    }
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u)
-        if (id[u] >= 0 && id[u] < P.vocab) e[u].load(static_cast<const TE*>(P.src) + id[u] * P.ld_src + col(u), P.d - col(u));
+    for (int u = 0; u < ROWS; ++u)
+        if (id[u] >= 0) e[u].template load<WHOLE>(src + id[u] * P.ld_src, P.d - c);
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-        if (row(u) >= P.n) break;
+    for (int u = 0; u < ROWS; ++u) {
+        if (t0 + u * step >= P.n) break;
         float x[8] = {};
-        if (id[u] >= 0 && id[u] < P.vocab) {
+        if (id[u] >= 0) {
             e[u].values(x);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= P.scale;
         }
-        Eight<TX>::store(static_cast<TX*>(P.dst) + row(u) * P.ld_dst + col(u), x, P.d - col(u));
+        Eight<TX>::template store<WHOLE>(dst + (t0 + u * step) * P.ld_dst, x, P.d - c);
     }
 }
 
 // ------------------------------------------------------------- rows of no token
 // Rows [first, last) of the gradient := 0 but for those that `named` tells, by the
 // warps of `ctas` CTAs of which this is number `cta`.
-template <class TD, class F>
+template <class TD, bool WHOLE, class F>
 __device__ __forceinline__ void fill_rows(const EmbedParams& P, int first, int last, int cta, int ctas, const F& named)
 {
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const float zero[8] = {};
     for (int v = first + cta * warps + (threadIdx.x >> 5); v < last; v += ctas * warps)
         if (!named(v))
-            for (int c = lane * 8; c < P.d; c += 256) Eight<TD>::store(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
+            for (int c = lane * 8; c < P.d; c += 256)
+                Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
 }
 
-// ------------------------------------------------------- few tokens by counting
+// -------------------------------------------------------------- few tokens at once
 constexpr unsigned int NO_KEY = ~0u;
 
 __device__ __forceinline__ unsigned int key_of(long long id, int vocab)
@@ -127,56 +155,78 @@ __device__ __forceinline__ unsigned int key_of(long long id, int vocab)
     return id >= 0 && id < vocab ? static_cast<unsigned int>(id) : NO_KEY;
 }
 
-// A token's place is the number of tokens before it: of lower ids, or of its own id
-// and earlier.  Every CTA reads all ids; its eight warps count for 32 tokens, each
-// over an eighth of the ids.  Every CTA also has a share of the table's rows, and
-// sets those to 0 that no id names (TD, where `filled`).
-template <class TD>
-__global__ void __launch_bounds__(256) embed_order_kernel(const EmbedParams P, int order_ctas, int rows_each)
+// Up to EMBED_FEW tokens in one launch, in which no CTA waits for another: each sorts all
+// of them into bins by the lower ten bits of their ids, in shared memory and in any order,
+// and finds the places of its own tokens, by the number of tokens of lower bins and of
+// those in its bin that come before it (their order is by the ids' lower bits first).
+// The first CTAs do that, for ORDER_TOKENS each, and set the bits of the rows that are
+// named (`words_each` words each).  Each of the others has `rows_each` rows of the
+// table, and sets those to 0 that no id names.
+constexpr int ORDER_THREADS = 512, ORDER_TOKENS = 64, ORDER_EACH = EMBED_FEW / ORDER_THREADS, BIN_BITS = 10, INDEX_BITS = 13;
+static_assert(EMBED_FEW <= 1 << INDEX_BITS && EMBED_VOCAB_MAX <= 1 << (BIN_BITS + 32 - INDEX_BITS), "a token's word");
+
+template <class TD, bool WHOLE>
+__global__ void __launch_bounds__(ORDER_THREADS) embed_order_kernel(const EmbedParams P, int order_ctas, int words_each, int rows_each)
 {
-    extern __shared__ __align__(16) unsigned int keys[];   // n of them up to a multiple of 256, then a bit for each of this CTA's rows
-    __shared__ unsigned int count[8][32];
-    __shared__ unsigned int valid;
-    const int n = static_cast<int>(P.n), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all = (n + 255) / 256 * 256;
-    unsigned int* named = keys + all;
-    const int first = min(P.vocab, static_cast<int>(blockIdx.x) * rows_each), last = min(P.vocab, first + rows_each);
-    for (int i = tid; i < (rows_each + 31) / 32; i += 256) named[i] = 0;
-    if (tid == 0) valid = 0;
-    __syncthreads();
-    unsigned int mine = 0;
-#pragma unroll 8
-    for (int i = tid; i < all; i += 256) {
-        const unsigned int key = i < n ? key_of(P.ids[i], P.vocab) : NO_KEY;
-        keys[i] = key;
-        mine += key != NO_KEY;
-        if (key != NO_KEY && key >= first && key < last) atomicOr(named + ((key - first) >> 5), 1u << ((key - first) & 31));
+    extern __shared__ unsigned int bits[];   // of rows
+    __shared__ unsigned int first[1 << BIN_BITS], next[1 << BIN_BITS], warp_sum[ORDER_THREADS / 32];
+    __shared__ unsigned int binned[EMBED_FEW];
+    const int n = static_cast<int>(P.n), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool orders = static_cast<int>(blockIdx.x) < order_ctas;
+    grid_launch_dependents();
+    unsigned int key[ORDER_EACH];
+#pragma unroll
+    for (int j = 0; j < ORDER_EACH; ++j) {
+        const int i = j * ORDER_THREADS + tid;
+        key[j] = i < n ? key_of(P.ids[i], P.vocab) : NO_KEY;
     }
-    if (blockIdx.x == 0) atomicAdd(&valid, mine);
+    // the rows whose bits this CTA sets or uses
+    const unsigned int r0 = orders ? blockIdx.x * words_each * 32u : (blockIdx.x - order_ctas) * static_cast<unsigned int>(rows_each);
+    const unsigned int r1 = orders ? min(static_cast<unsigned int>(P.vocab), r0 + words_each * 32u)
+                                   : min(static_cast<unsigned int>(P.filled), r0 + rows_each);
+    const int words = r1 > r0 ? (r1 - r0 + 31) / 32 : 0;
+    for (int i = tid; i < words; i += ORDER_THREADS) bits[i] = 0;
+    if (orders) next[tid] = next[tid + 512] = 0;
     __syncthreads();
-    if (blockIdx.x == 0 && tid == 0) *P.count = valid, *P.long_count = 0;
-    if (static_cast<int>(blockIdx.x) < order_ctas) {
-        const int i0 = blockIdx.x * 32, eighth = all / 8, from = warp * eighth, to = from + eighth;
-        const unsigned int key = i0 + lane < n ? keys[i0 + lane] : NO_KEY;
-        unsigned int sum = 0;
-        const auto below = [&](int lo, int hi, unsigned int bound) {
-#pragma unroll 4
-            for (int j = lo; j < hi; j += 4) {
-                const uint4 k = *reinterpret_cast<const uint4*>(keys + j);
-                sum += (k.x < bound) + (k.y < bound) + (k.z < bound) + (k.w < bound);
-            }
-        };
-        below(from, min(to, i0), key + 1);
-        below(max(from, i0 + 32), to, key);
-        if (i0 >= from && i0 < to)
-            for (int j = 0; j < 32; ++j) sum += keys[i0 + j] < key + (j < lane);
-        count[warp][lane] = sum;
-        __syncthreads();
-        if (warp == 0 && key != NO_KEY) {
-            for (int w = 1; w < 8; ++w) sum += count[w][lane];
-            P.sorted[sum] = make_uint2(key, i0 + lane);
-        }
+#pragma unroll
+    for (int j = 0; j < ORDER_EACH; ++j) {
+        if (key[j] >= r0 && key[j] < r1) atomicOr(bits + ((key[j] - r0) >> 5), 1u << ((key[j] - r0) & 31));
+        if (orders && key[j] != NO_KEY) atomicAdd(next + (key[j] & 1023), 1u);
     }
-    if (rows_each) fill_rows<TD>(P, first, last, 0, 1, [&](int v) { return named[(v - first) >> 5] >> ((v - first) & 31) & 1; });
+    __syncthreads();
+    if (!orders) {
+        fill_rows<TD, WHOLE>(P, r0, r1, 0, 1, [&](int v) { return bits[(v - r0) >> 5] >> ((v - r0) & 31) & 1; });
+        return;
+    }
+    for (int i = tid; i < words; i += ORDER_THREADS) P.present[r0 / 32 + i] = bits[i];
+    // first places of the bins, two a thread
+    const unsigned int c0 = next[2 * tid], c1 = next[2 * tid + 1];
+    unsigned int up = c0 + c1;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+        const unsigned int v = __shfl_up_sync(~0u, up, k);
+        if (lane >= k) up += v;
+    }
+    if (lane == 31) warp_sum[warp] = up;
+    __syncthreads();
+    const unsigned int base = up - c0 - c1 + __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0u);
+    first[2 * tid] = next[2 * tid] = base, first[2 * tid + 1] = next[2 * tid + 1] = base + c0;
+    if (blockIdx.x == 0 && tid == ORDER_THREADS - 1) *P.count = base + c0 + c1, *P.long_count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ORDER_EACH; ++j)
+        if (key[j] != NO_KEY) binned[atomicAdd(next + (key[j] & 1023), 1u)] = key[j] >> BIN_BITS << INDEX_BITS | (j * ORDER_THREADS + tid);
+    __syncthreads();
+    // a warp a token (behind its last token, `next` is where a bin ends)
+    for (int i = blockIdx.x * ORDER_TOKENS + warp; i < min(n, static_cast<int>(blockIdx.x + 1) * ORDER_TOKENS); i += ORDER_THREADS / 32) {
+        const unsigned int k = key_of(P.ids[i], P.vocab);
+        if (k == NO_KEY) continue;
+        const unsigned int word = k >> BIN_BITS << INDEX_BITS | i, begin = first[k & 1023], end = next[k & 1023];
+        unsigned int before = 0;
+        for (unsigned int m = begin + lane; m < end; m += 32) before += binned[m] < word;
+        before = __reduce_add_sync(~0u, before);
+        if (lane == 0) P.sorted[begin + before] = make_uint2(k, i);
+    }
 }
 
 // --------------------------------------------------------- many tokens by digits
@@ -216,13 +266,15 @@ __device__ __forceinline__ void sort_load(const EmbedParams& P, const SortPass& 
     }
 }
 
-template <class TD, bool FIRST>
+template <class TD, bool WHOLE, bool FIRST>
 __global__ void __launch_bounds__(SORT_THREADS) embed_count_kernel(const EmbedParams P, const SortPass S)
 {
     __shared__ unsigned int total[1024];
     const int cta = blockIdx.x, digits = 1 << S.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (!FIRST) grid_dependency_wait();
+    grid_launch_dependents();
     if (!FIRST && cta >= S.ctas) {
-        fill_rows<TD>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
+        fill_rows<TD, WHOLE>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
         return;
     }
     if (FIRST) {
@@ -264,14 +316,16 @@ __device__ __forceinline__ unsigned int sort_rank(unsigned int key, int shift, i
     return rank;
 }
 
-template <class TD, bool FIRST>
+template <class TD, bool WHOLE, bool FIRST>
 __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedParams P, const SortPass S)
 {
     extern __shared__ unsigned int place[];   // [warp][digit]
     __shared__ unsigned int before[1024], all[1024], warp_sum[SORT_WARPS];
     const int cta = blockIdx.x, digits = 1 << S.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
+    // the launch before this one counts; what this one ranks was there before that launch
+    grid_launch_dependents();
     if (!FIRST && cta >= S.ctas) {
-        fill_rows<TD>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
+        fill_rows<TD, WHOLE>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
         return;
     }
     const unsigned int n = FIRST ? static_cast<unsigned int>(P.n) : *P.count;
@@ -295,6 +349,7 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedPa
         sort_load<FIRST>(P, S, b + lane, end, key, token);
     }
     __syncthreads();
+    grid_dependency_wait();
     // each digit's tokens of all CTAs and of those before this one, by 1024 / digits threads
     {
         const int d = tid & (digits - 1);
@@ -373,44 +428,90 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedPa
 }
 
 // ---------------------------------------------------------------------- sums
-// Eight columns' sum, in pairs.
+// A thread has 16 bytes of columns of each row of dX: four of fp32, eight of bf16.
+template <class TX>
+constexpr int COLS = 16 / sizeof(TX);
+
+template <int N>
 struct Sum {
-    Pair p[4];
-    __device__ __forceinline__ void clear() { p[0] = p[1] = p[2] = p[3] = 0; }
-    template <class T>
-    __device__ __forceinline__ void add(const Eight<T>& row)
+    Pair p[N / 2];
+    __device__ __forceinline__ void clear()
     {
-        float x[8];
-        row.values(x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = add2(p[k], pair(x[2 * k], x[2 * k + 1]));
+        for (int k = 0; k < N / 2; ++k) p[k] = 0;
     }
-    __device__ __forceinline__ void values(float (&x)[8]) const
+    template <class TX>
+    __device__ __forceinline__ void add(const uint4& row)
+    {
+        float x[N];
+        Elem<TX>::unpack(row, x);
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) p[k] = add2(p[k], pair(x[2 * k], x[2 * k + 1]));
+    }
+    __device__ __forceinline__ void values(float (&x)[N]) const
     {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) split(p[k], x[2 * k], x[2 * k + 1]);
+        for (int k = 0; k < N / 2; ++k) split(p[k], x[2 * k], x[2 * k + 1]);
     }
 };
 
-template <class TD>
-__device__ __forceinline__ void store_sum(const EmbedParams& P, unsigned int id, int c, const Sum& sum)
+// N columns at a multiple of N, `left` of them there.
+template <int N>
+__device__ __forceinline__ void store_columns(float* p, const float (&x)[N], int left)
+{
+    if (left >= N) {
+#pragma unroll
+        for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(p + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N - 1; ++k)
+            if (k < left) p[k] = x[k];
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_columns(__nv_bfloat16* p, const float (&x)[N], int left)
+{
+    if (left >= N) {
+        uint2 u[N / 4];
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x[k], x[k + 1]), hi = __floats2bfloat162_rn(x[k + 2], x[k + 3]);
+            u[k / 4] = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+        if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(u[0].x, u[0].y, u[1].x, u[1].y);
+        else *reinterpret_cast<uint2*>(p) = u[0];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N - 1; ++k)
+            if (k < left) p[k] = __float2bfloat16_rn(x[k]);
+    }
+}
+
+template <class TD, int N>
+__device__ __forceinline__ void store_sum(const EmbedParams& P, unsigned int id, int c, const Sum<N>& sum)
 {
     TD* p = static_cast<TD*>(P.dst) + id * P.ld_dst + c;
-    float x[8] = {}, s[8];
-    if (P.accumulate) {
-        Eight<TD> old;
-        old.load(p, P.d - c);
-        old.values(x);
-    }
+    float x[N], s[N];
     sum.values(s);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = fmaf(P.scale, s[k], x[k]);
-    Eight<TD>::store(p, x, P.d - c);
+    for (int k = 0; k < N; ++k) x[k] = fmaf(P.scale, s[k], P.accumulate && k < P.d - c ? Elem<TD>::get(p + k) : 0.f);
+    store_columns(p, x, P.d - c);
 }
 
 __device__ __forceinline__ float* partial_at(const EmbedParams& P, int chunk, int after, int c)
 {
     return P.partials + (chunk * 2ll + after) * ((P.d + 7) / 8 * 8) + c;
+}
+
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // The first place from `i` on, below `end`, whose id is not `id`; by a whole warp.
@@ -424,82 +525,132 @@ __device__ __forceinline__ unsigned int run_end(const uint2* items, unsigned int
     return end;
 }
 
-// `group` threads share a chunk of the sorted tokens, eight columns each; wider
-// rows are shared by `tiles` such groups.  A chunk's group takes the sums that begin
+// The last chunk that begins with the id, of those from `first` + 1 on (which does) below
+// `above`; by a whole warp: 32 chunks together, then every 33rd part of what is left.
+__device__ __forceinline__ int last_chunk(const EmbedParams& P, int first, int above, unsigned int id)
+{
+    int last = first + 1;
+    for (int step = 1; above - last > 1; step = max(1, (above - last + 31) / 33)) {
+        const long long chunk = last + ((threadIdx.x & 31) + 1ll) * step;
+        const int yes = __popc(__ballot_sync(~0u, chunk < above && P.sorted[chunk * P.chunk].x == id));
+        last += yes * step;
+        if (yes < 32) above = min(above, last + step);
+    }
+    return last;
+}
+
+// A group has a chunk of the sorted tokens.  It takes the sums that begin
 // in it, up to a chunk's length beyond its end.  Longer sums are split at the
 // chunks' bounds into parts that embed_join_kernel adds.
-template <class TX, class TD>
-__global__ void __launch_bounds__(256) embed_sum_kernel(const EmbedParams P, int group, int tiles, int sum_ctas, int fill_first)
+//
+// A thread copies its columns of every row into shared memory of its own, BATCHES
+// batches of BATCH rows ahead of the one that it adds: no thread waits for another, and
+// an SM has 192 KB of rows on their way.
+constexpr int BATCH = 4, BATCHES = 4;
+
+template <class TX, class TD, bool WHOLE>
+__global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, const Groups g, int sum_ctas, int fill_first)
 {
-    constexpr int U = sizeof(TX) == 2 ? 8 : 4;   // rows whose columns a thread has on their way: 128 bytes of them
-    if (static_cast<int>(blockIdx.x) >= sum_ctas) {
-        fill_rows<TD>(P, fill_first, P.vocab, blockIdx.x - sum_ctas, gridDim.x - sum_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
+    constexpr int N = COLS<TX>;
+    extern __shared__ uint4 ring[];   // [row of the batches][thread]
+    grid_dependency_wait();
+    grid_launch_dependents();
+    // the CTAs that set rows to 0 lie evenly between the others
+    const int fill_ctas = gridDim.x - sum_ctas, fills = static_cast<int>(static_cast<long long>(blockIdx.x) * fill_ctas / gridDim.x);
+    if (fills != static_cast<int>((blockIdx.x + 1ll) * fill_ctas / gridDim.x)) {
+        fill_rows<TD, WHOLE>(P, fill_first, P.vocab, fills, fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
         return;
     }
-    const int at = blockIdx.x * (256 / group) + threadIdx.x / group, chunk = at / tiles, tile = at - chunk * tiles;
-    const int c = (tile * group + threadIdx.x % group) * 8;
-    const unsigned int valid = *P.count, length = P.chunk, begin = static_cast<unsigned int>(chunk) * length;
-    if (chunk >= P.chunks || begin >= valid) return;
+    const int at = (blockIdx.x - fills) << (8 - g.shift) | threadIdx.x >> g.shift, chunk = at / g.tiles, tile = at - chunk * g.tiles;
+    const int member = threadIdx.x & ((1 << g.shift) - 1), c = (tile << g.shift | member) * N;
+    if (chunk >= P.chunks) return;
+    const int lane = threadIdx.x & 31;
+    const unsigned int n = static_cast<unsigned int>(P.n), length = P.chunk, begin = static_cast<unsigned int>(chunk) * length;
     const uint2* items = P.sorted;
-    const unsigned int end = min(valid, begin + length);
-    const unsigned int head = items[begin].x, tail = items[end - 1].x;
-    bool open = begin > 0 && items[begin - 1].x == head;
-    bool goes_on = end < valid && items[end].x == tail;
+    // what tells where the chunk's sums begin and end, and its first items, all loaded
+    // together (what lies behind the last token is not used)
+    const unsigned int valid = *P.count;
+    const auto id_at = [&](unsigned int k) { return items[min(k, n - 1)].x; };
+    const unsigned int before_chunk = id_at(max(begin, 1u) - 1), head = id_at(begin), two_before = id_at(max(begin, length + 1) - length - 1);
+    const unsigned int full_tail = id_at(begin + length - 1), behind = id_at(begin + length), far_behind = id_at(begin + 2 * length);
+    uint2 item = items[min(begin + lane, n - 1)];   // a lane holds an item of 32
+    if (begin >= valid) return;
+    const unsigned int end = min(valid, begin + length), tail = end == begin + length ? full_tail : items[end - 1].x;
+    bool open = begin > 0 && before_chunk == head;
+    bool goes_on = end < valid && behind == tail;
     unsigned int i = begin, stop = end;
-    if (open && (begin == length || items[begin - length - 1].x != head) && !(goes_on && head == tail)) {
+    if (open && (begin == length || two_before != head) && !(goes_on && head == tail)) {
         i = run_end(items, begin, end, head);   // the chunk before has it all
         open = false;
     }
     if (goes_on && !(open && head == tail)) {
-        if (end + length >= valid || items[end + length].x != tail) {
+        if (end + length >= valid || far_behind != tail) {
             stop = run_end(items, end, min(valid, end + length), tail);
             goes_on = false;
-        } else if (tile == 0 && threadIdx.x % group == 0) {
-            P.long_sums[atomicAdd(P.long_count, 1u)] = chunk;
+        } else if (tile == 0 && member < 32) {
+            const int last = last_chunk(P, chunk, (valid + length - 1) / length, tail);
+            if (lane == 0) P.long_sums[atomicAdd(P.long_count, 1u)] = make_uint4(chunk, last, tail, 0);
         }
     }
     if (i >= stop) return;
     const bool mine = c < P.d;
+    const int bytes = min(P.d - c, N) * static_cast<int>(sizeof(TX));
     const TX* src = static_cast<const TX*>(P.src) + c;
-    const int lane = threadIdx.x & 31;
-    unsigned int cur = items[i].x;
-    Sum sum;
+    const unsigned int ld = static_cast<unsigned int>(P.ld_src);
+    const uint32_t slot = smem_u32(ring + threadIdx.x);
+    const auto get = [&](unsigned int k) { return k + lane < stop ? items[k + lane] : make_uint2(NO_KEY, 0); };
+    if (i != begin || i + 32 > stop) item = get(i);
+    // the rows of batch b of those 32 items, the first of them number `first`
+    const auto fetch = [&](unsigned int first, const uint2& from, int b) {
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const unsigned int t = __shfl_sync(~0u, from.y, b * BATCH + u);
+            if (mine && first + b * BATCH + u < stop)
+                copy_async(slot + (b % BATCHES * BATCH + u) * 4096, src + static_cast<unsigned long long>(t) * ld, bytes);
+        }
+        copy_commit();
+    };
+#pragma unroll
+    for (int b = 0; b < BATCHES; ++b) fetch(i, item, b);
+    unsigned int cur = __shfl_sync(~0u, item.x, 0);
+    Sum<N> sum;
     sum.clear();
     const auto flush = [&](bool part, int after) {
         if (!mine) return;
         if (part) {
-            float x[8];
+            float x[N];
             sum.values(x);
-            Eight<float>::store(partial_at(P, chunk, after, c), x, 8);
+            store_columns(partial_at(P, chunk, after, c), x, N);
         } else {
             store_sum<TD>(P, cur, c, sum);
         }
     };
-    for (; i < stop; i += 32) {   // a lane holds an item of the next 32
-        const uint2 item = i + lane < stop ? items[i + lane] : make_uint2(NO_KEY, 0);
+    for (; i < stop; i += 32) {
+        const uint2 next = get(i + 32);
         unsigned int before = __shfl_up_sync(~0u, item.x, 1);
         if (lane == 0) before = cur;
         const unsigned int begins = __ballot_sync(~0u, item.x != before);
         const int count = min(32u, stop - i);
-        for (int j = 0; j < count; j += U) {
-            Eight<TX> row[U];
+#pragma unroll 1
+        for (int b = 0; b < 32 / BATCH; ++b) {
+            copy_wait<BATCHES - 1>();
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const unsigned int t = __shfl_sync(~0u, item.y, j + u);
-                if (mine && j + u < count) row[u].load(src + t * P.ld_src, P.d - c);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (j + u >= count) break;
-                if (begins >> (j + u) & 1) {
+            for (int u = 0; u < BATCH; ++u) {
+                const int j = b * BATCH + u;
+                if (j >= count) break;
+                if (begins >> j & 1) {
                     flush(open, 0);
-                    cur = __shfl_sync(~0u, item.x, j + u), open = false;
+                    cur = __shfl_sync(~0u, item.x, j), open = false;
                     sum.clear();
                 }
-                sum.add(row[u]);
+                sum.template add<TX>(ring[(b % BATCHES * BATCH + u) * 256 + threadIdx.x]);
             }
+            if (b + BATCHES < 32 / BATCH) fetch(i, item, b + BATCHES);
+            else fetch(i + 32, next, b + BATCHES - 32 / BATCH);
         }
+        item = next;
     }
+    copy_wait<0>();
     flush(open || goes_on, open ? 0 : 1);
 }
 
@@ -510,22 +661,14 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const EmbedParams P)
 {
     __shared__ float4 share[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const unsigned int slices = (P.d + 127) / 128, valid = *P.count, work = *P.long_count * slices;
-    const int filled = (valid + P.chunk - 1) / P.chunk;   // chunks that hold tokens
-    for (unsigned int w = blockIdx.x; w < work; w += gridDim.x) {
-        const int first = P.long_sums[w / slices], c = (w % slices) * 128 + lane * 4;
-        const unsigned int id = P.sorted[(first + 1ll) * P.chunk].x;
-        // the chunks behind the first that begin with the id: 32 are looked at together, then
-        // every 32nd part of what is left
-        int last = first, above = filled;
-        for (int step = 1; above - last > 1;) {
-            const long long chunk = last + (lane + 1ll) * step;
-            const unsigned int yes = __ballot_sync(~0u, chunk < above && P.sorted[chunk * P.chunk].x == id);
-            const int count = __popc(yes);
-            last += count * step;
-            if (count < 32) above = static_cast<int>(min(static_cast<long long>(above), last + static_cast<long long>(step)));
-            step = max(1, (above - last + 31) / 33);
-        }
+    const int slices = (P.d + 127) / 128;
+    grid_dependency_wait();
+    const int work = static_cast<int>(*P.long_count) * slices;   // (at most chunks x slices)
+    for (int w = blockIdx.x; w < P.chunks * slices; w += gridDim.x) {
+        const uint4 item = P.long_sums[w / slices];   // with the count, on its way together with it
+        if (w >= work) return;
+        const int first = item.x, last = item.y, c = (w % slices) * 128 + lane * 4;
+        const unsigned int id = item.z;
         // part i: of chunk first + i
         const int parts = last - first + 1, each = (parts + 7) / 8, from = warp * each, to = min(parts, from + each);
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -553,35 +696,16 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const EmbedParams P)
     }
 }
 
-struct Groups {
-    int group, tiles;
-};
-Groups groups(int d)
+// The widest groups that leave few threads without columns.
+Groups groups(int d, int columns)
 {
-    const int units = (d + 7) / 8;
-    int group = 32;
-    while (group < 256 && group < units) group *= 2;
-    return {group, (units + group - 1) / group};
-}
-
-template <class TS, class TD>
-cudaError_t rows(const EmbedParams& p, int sms, cudaStream_t stream)
-{
-    const long long units = (p.d + 7) / 8 * p.n;
-    if (units < 2048ll * sms) embed_rows_kernel<TS, TD, 1><<<static_cast<unsigned int>((units + 255) / 256), 256, 0, stream>>>(p);
-    else embed_rows_kernel<TS, TD, 4><<<static_cast<unsigned int>((units + 1023) / 1024), 256, 0, stream>>>(p);
-    return cudaGetLastError();
-}
-
-template <class TS, class TD>
-cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
-{
-    const Groups g = groups(p.d);
-    const int per = 256 / g.group;
-    const int ctas = static_cast<int>((static_cast<long long>(p.chunks) * g.tiles + per - 1) / per);
-    const int fill = p.filled < p.vocab ? std::min(4 * sms, (p.vocab - p.filled + 7) / 8) : 0;
-    embed_sum_kernel<TS, TD><<<ctas + fill, 256, 0, stream>>>(p, g.group, g.tiles, ctas, p.filled);
-    return cudaGetLastError();
+    const int units = (d + columns - 1) / columns;
+    Groups best = {5, (units + 31) / 32};
+    for (int shift = 6; shift <= 8; ++shift) {
+        const int tiles = (units + (1 << shift) - 1) >> shift;
+        if (tiles << shift <= best.tiles << best.shift || (tiles << shift) * 16 <= units * 17) best = {shift, tiles};
+    }
+    return best;
 }
 
 template <class K>
@@ -598,42 +722,94 @@ cudaError_t allow_smem(K kern, size_t bytes, std::atomic<unsigned long long>& co
     return cudaSuccess;
 }
 
-template <class TD>
-cudaError_t order(const EmbedParams& p, int sms, cudaStream_t stream)
+// A launch that may begin while the one before it in the stream still runs, and waits for
+// it on the device.
+template <class K, class... A>
+cudaError_t launch_behind(K kern, int ctas, int threads, size_t smem, cudaStream_t stream, const A&... args)
 {
-    const int n = static_cast<int>(p.n), order_ctas = (n + 31) / 32;
-    const int ctas = p.accumulate ? order_ctas : std::max(order_ctas, std::min(2 * sms, (p.vocab + 7) / 8));
-    const int rows_each = p.accumulate ? 0 : (p.vocab + ctas - 1) / ctas;
-    const size_t smem = sizeof(unsigned int) * ((n + 255) / 256 * 256 + (rows_each + 31) / 32);
-    if (smem > 40 * 1024) {   // beyond what a launch may have without asking for more
-        static std::atomic<unsigned long long> configured{0};
-        const cudaError_t e = allow_smem(embed_order_kernel<TD>, sizeof(unsigned int) * (EMBED_FEW + EMBED_VOCAB_MAX / 32 + 1), configured);
-        if (e != cudaSuccess) return e;
-    }
-    embed_order_kernel<TD><<<ctas, 256, smem, stream>>>(p, order_ctas, rows_each);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+template <class TE, class TX, bool WHOLE, int ROWS>
+cudaError_t rows(const EmbedParams& p, const Groups& g, cudaStream_t stream)
+{
+    const int each = ROWS * (256 >> g.shift);
+    embed_rows_kernel<TE, TX, WHOLE, ROWS><<<dim3(static_cast<unsigned int>((p.n + each - 1) / each), g.tiles), 256, 0, stream>>>(p, g);
     return cudaGetLastError();
 }
 
-template <class TD, bool FIRST>
+template <class TE, class TX, bool WHOLE>
+cudaError_t rows(const EmbedParams& p, int sms, cudaStream_t stream)
+{
+    const Groups g = groups(p.d, 8);
+    return (p.n * g.tiles << g.shift) < 2048ll * sms ? rows<TE, TX, WHOLE, 1>(p, g, stream) : rows<TE, TX, WHOLE, 4>(p, g, stream);
+}
+
+template <class TX, class TD, bool WHOLE>
+cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
+{
+    static std::atomic<unsigned long long> configured{0};
+    constexpr size_t smem = BATCH * BATCHES * 256 * sizeof(uint4);
+    const cudaError_t e = allow_smem(embed_sum_kernel<TX, TD, WHOLE>, smem, configured);
+    if (e != cudaSuccess) return e;
+    const Groups g = groups(p.d, COLS<TX>);
+    const int per = 256 >> g.shift;
+    const int ctas = static_cast<int>((static_cast<long long>(p.chunks) * g.tiles + per - 1) / per);
+    const int fill = p.filled < p.vocab ? std::min(4 * sms, (p.vocab - p.filled + 7) / 8) : 0;
+    return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, ctas, p.filled);
+}
+
+// Rows of the table that the CTAs beside one of the sort's launches set to 0 (from
+// p.filled on, to the result): what HBM takes in the time that the launch takes anyway.
+constexpr double FILL_BYTES = 24e6;
+int fill_to(const EmbedParams& p, size_t element)
+{
+    return static_cast<int>(std::min<double>(p.vocab, p.filled + FILL_BYTES / (static_cast<double>(p.d) * element)));
+}
+
+template <class TD, bool WHOLE>
+cudaError_t order(EmbedParams& p, int sms, cudaStream_t stream)
+{
+    const int n = static_cast<int>(p.n), order_ctas = (n + ORDER_TOKENS - 1) / ORDER_TOKENS;
+    p.filled = p.accumulate ? 0 : fill_to(p, sizeof(TD));
+    const int fill = std::min(2 * sms, (p.filled + 7) / 8), rows_each = fill ? (p.filled + fill - 1) / fill : 0;
+    const int words_each = p.accumulate || p.filled == p.vocab ? 0 : ((p.vocab + 31) / 32 + order_ctas - 1) / order_ctas;
+    const size_t smem = sizeof(unsigned int) * std::max(words_each, (rows_each + 31) / 32);
+    static std::atomic<unsigned long long> configured{0};
+    const cudaError_t e = allow_smem(embed_order_kernel<TD, WHOLE>, EMBED_VOCAB_MAX / 8, configured);
+    if (e != cudaSuccess) return e;
+    embed_order_kernel<TD, WHOLE><<<order_ctas + fill, ORDER_THREADS, smem, stream>>>(p, order_ctas, words_each, rows_each);
+    if (p.accumulate) p.filled = p.vocab;
+    return cudaGetLastError();
+}
+
+template <class TD, bool WHOLE, bool FIRST>
 cudaError_t count(const EmbedParams& p, const SortPass& s, cudaStream_t stream)
 {
-    embed_count_kernel<TD, FIRST><<<s.ctas + s.fill_ctas, SORT_THREADS, 0, stream>>>(p, s);
+    if (!FIRST) return launch_behind(embed_count_kernel<TD, WHOLE, FIRST>, s.ctas + s.fill_ctas, SORT_THREADS, 0, stream, p, s);
+    embed_count_kernel<TD, WHOLE, FIRST><<<s.ctas, SORT_THREADS, 0, stream>>>(p, s);
     return cudaGetLastError();
 }
 
-template <class TD, bool FIRST>
+template <class TD, bool WHOLE, bool FIRST>
 cudaError_t place(const EmbedParams& p, const SortPass& s, cudaStream_t stream)
 {
     static std::atomic<unsigned long long> configured{0};
-    const cudaError_t e = allow_smem(embed_place_kernel<TD, FIRST>, sizeof(unsigned int) * SORT_WARPS << 10, configured);
+    const cudaError_t e = allow_smem(embed_place_kernel<TD, WHOLE, FIRST>, sizeof(unsigned int) * SORT_WARPS << 10, configured);
     if (e != cudaSuccess) return e;
-    embed_place_kernel<TD, FIRST><<<s.ctas + s.fill_ctas, SORT_THREADS, sizeof(unsigned int) * SORT_WARPS << s.bits, stream>>>(p, s);
-    return cudaGetLastError();
+    return launch_behind(embed_place_kernel<TD, WHOLE, FIRST>, s.ctas + s.fill_ctas, SORT_THREADS,
+                         sizeof(unsigned int) * SORT_WARPS << s.bits, stream, p, s);
 }
-
-// Rows of the table that the CTAs beside one of the sort's launches set to 0: what HBM
-// takes in the time that the launch takes anyway.
-constexpr double FILL_BYTES = 16e6;
 
 SortPass sort_pass(const EmbedParams& p, int step)   // 0: by the lower digit, 1: by the upper
 {
@@ -648,31 +824,28 @@ SortPass sort_pass(const EmbedParams& p, int step)   // 0: by the lower digit, 1
     return s;
 }
 
-template <class TD>
+template <class TD, bool WHOLE>
 cudaError_t sort_launch(EmbedParams& p, int launch, int sms, cudaStream_t stream)
 {
     SortPass s = sort_pass(p, launch / 2);
-    if (launch < 2) return launch == 0 ? count<TD, true>(p, s, stream) : place<TD, true>(p, s, stream);
-    if (!p.accumulate) {   // (the first pass found out which rows the tokens name)
-        const double row = static_cast<double>(p.d) * sizeof(TD);
+    if (launch < 2) return launch == 0 ? count<TD, WHOLE, true>(p, s, stream) : place<TD, WHOLE, true>(p, s, stream);
+    if (!p.accumulate && sms > s.ctas) {   // (the first pass found out which rows the tokens name)
         s.fill_first = p.filled;
-        s.fill_last = p.filled = static_cast<int>(std::min<double>(p.vocab, p.filled + FILL_BYTES / row));
-        s.fill_ctas = s.fill_last > s.fill_first && sms > s.ctas ? sms - s.ctas : 0;
-        if (!s.fill_ctas) p.filled = s.fill_first;
+        s.fill_last = p.filled = fill_to(p, sizeof(TD));
+        s.fill_ctas = s.fill_last > s.fill_first ? sms - s.ctas : 0;
     }
-    return launch == 2 ? count<TD, false>(p, s, stream) : place<TD, false>(p, s, stream);
+    return launch == 2 ? count<TD, WHOLE, false>(p, s, stream) : place<TD, WHOLE, false>(p, s, stream);
 }
 
 template <class TD>
 cudaError_t join(const EmbedParams& p, int sms, cudaStream_t stream)
 {
-    embed_join_kernel<TD><<<8 * sms, 256, 0, stream>>>(p);
-    return cudaGetLastError();
+    return launch_behind(embed_join_kernel<TD>, 8 * sms, 256, 0, stream, p);
 }
 
 }  // namespace
 
-EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at)
+EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, size_t at)
 {
     EmbedLayout l = {};
     const auto take = [&](size_t bytes) {
@@ -680,15 +853,16 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at)
         at = (at + bytes + 255) / 256 * 256;
         return a;
     };
-    const Groups g = groups(d);
+    const Groups g = groups(d, dtype_x == 0 ? COLS<__nv_bfloat16> : COLS<float>);
     // eight CTAs' worth of groups for every SM, of eight tokens at least
-    const double per = static_cast<double>(n) * g.tiles * g.group / (8.0 * sms * 256);
+    const double per = static_cast<double>(n) * (g.tiles << g.shift) / (8.0 * sms * 256);
     l.chunk = std::max(8, static_cast<int>(std::min(per / 8 + 1, 1e6)) * 8);
     l.chunks = static_cast<int>((n + l.chunk - 1) / l.chunk);
     l.sorted = take(n * sizeof(uint2));
     l.counts = take(2 * sizeof(unsigned int));
-    l.long_sums = take(l.chunks * sizeof(unsigned int));
+    l.long_sums = take(l.chunks * sizeof(uint4));
     l.partials = take(sizeof(float) * 2 * l.chunks * static_cast<size_t>((d + 7) / 8 * 8));
+    l.present = take((vocab + 31) / 32 * sizeof(unsigned int));
     if (n > EMBED_FEW) {
         int bits = 1;
         while ((1 << bits) < vocab) ++bits;
@@ -699,7 +873,6 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at)
         l.sort_each = static_cast<unsigned int>(std::max(std::min<long long>(rounds, ROUNDS), most) * 32);
         l.sort_ctas = static_cast<int>((n + l.sort_each * SORT_WARPS - 1) / (l.sort_each * SORT_WARPS));
         l.between = take(n * sizeof(uint2));
-        l.present = take((vocab + 31) / 32 * sizeof(unsigned int));
         l.hist[0] = take(sizeof(unsigned int) * l.sort_ctas << l.low);
         l.hist[1] = take(sizeof(unsigned int) * l.sort_ctas << l.high);
     }
@@ -707,30 +880,46 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at)
     return l;
 }
 
+namespace {
+
+// f with the types and the width's rest of a call
+template <class F>
+cudaError_t by_type(int dtype, int d, const F& f)
+{
+    if (dtype == 0) return d % 8 ? f(__nv_bfloat16(), std::false_type()) : f(__nv_bfloat16(), std::true_type());
+    return d % 8 ? f(float(), std::false_type()) : f(float(), std::true_type());
+}
+
+}  // namespace
+
 cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream)
 {
-    using bf16 = __nv_bfloat16;
-    if (dtype_src == 0) return dtype_dst == 0 ? rows<bf16, bf16>(p, sms, stream) : rows<bf16, float>(p, sms, stream);
-    return dtype_dst == 0 ? rows<float, bf16>(p, sms, stream) : rows<float, float>(p, sms, stream);
+    return by_type(dtype_dst, p.d, [&](auto x, auto whole) {
+        using TX = decltype(x);
+        constexpr bool WHOLE = decltype(whole)::value;
+        return dtype_src == 0 ? rows<__nv_bfloat16, TX, WHOLE>(p, sms, stream) : rows<float, TX, WHOLE>(p, sms, stream);
+    });
 }
 
 cudaError_t launch_embed_order(EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream)
 {
-    const cudaError_t e = dtype_dst == 0 ? order<__nv_bfloat16>(p, sms, stream) : order<float>(p, sms, stream);
-    p.filled = p.vocab;
-    return e;
+    return by_type(dtype_dst, p.d, [&](auto x, auto whole) { return order<decltype(x), decltype(whole)::value>(p, sms, stream); });
 }
 
 cudaError_t launch_embed_sort(EmbedParams& p, int launch, int dtype_dst, int sms, cudaStream_t stream)
 {
-    return dtype_dst == 0 ? sort_launch<__nv_bfloat16>(p, launch, sms, stream) : sort_launch<float>(p, launch, sms, stream);
+    return by_type(dtype_dst, p.d, [&](auto x, auto whole) {
+        return sort_launch<decltype(x), decltype(whole)::value>(p, launch, sms, stream);
+    });
 }
 
 cudaError_t launch_embed_sums(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream)
 {
-    using bf16 = __nv_bfloat16;
-    if (dtype_src == 0) return dtype_dst == 0 ? sums<bf16, bf16>(p, sms, stream) : sums<bf16, float>(p, sms, stream);
-    return dtype_dst == 0 ? sums<float, bf16>(p, sms, stream) : sums<float, float>(p, sms, stream);
+    return by_type(dtype_dst, p.d, [&](auto x, auto whole) {
+        using TD = decltype(x);
+        constexpr bool WHOLE = decltype(whole)::value;
+        return dtype_src == 0 ? sums<__nv_bfloat16, TD, WHOLE>(p, sms, stream) : sums<float, TD, WHOLE>(p, sms, stream);
+    });
 }
 
 cudaError_t launch_embed_join(const EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream)

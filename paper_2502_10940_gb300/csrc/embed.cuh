@@ -31,17 +31,17 @@ struct EmbedParams {
     uint2* sorted;            // (id, token)
     unsigned int* count;      // tokens that name a row
     unsigned int* long_count; // sums that are split over chunks
-    unsigned int* long_sums;  // the chunks they begin in
+    uint4* long_sums;         // of each the chunks that it begins and ends in, and its id
     float* partials;          // 2 per chunk, d rounded up to 8: of a sum that began before the chunk, and of one that goes on behind it
     int chunk, chunks;        // sorted tokens of a chunk; chunks of n
+    unsigned int* present;    // a bit for each row of the table that a token names
+    int filled;               // rows of no token below this one are 0 already
     // more than EMBED_FEW tokens
     uint2* between;           // after the first pass of the sort
-    unsigned int* present;    // a bit for each row of the table that a token names
     unsigned int* hist[2];
     int low, high;            // bits of the two digits (high 0: one pass)
     int sort_ctas;
     unsigned int sort_each;
-    int filled;               // rows of no token below this one are 0 already
 };
 
 // Byte offsets in the gradient's workspace, from `at` on, and the shares of the work.
@@ -50,13 +50,13 @@ struct EmbedLayout {
     int chunk, chunks, low, high, sort_ctas;
     unsigned int sort_each;
 };
-EmbedLayout embed_layout(long long n, int vocab, int d, int sms, size_t at);
+EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, size_t at);
 
 // dtypes: cola_dtype_t of src and dst
 cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
-// the order of up to EMBED_FEW tokens, and the rows of no token set to 0
+// the order of up to EMBED_FEW tokens; sets rows of no token to 0, up to p.filled then
 cudaError_t launch_embed_order(EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);
-// that of more, in launches 0 .. 3 (0 and 1 where high is 0); the last two set rows of no token to 0
+// that of more, in launches 0 .. 3 (0 and 1 where high is 0); the last two set rows of no token to 0 too
 cudaError_t launch_embed_sort(EmbedParams& p, int launch, int dtype_dst, int sms, cudaStream_t stream);
 cudaError_t launch_embed_sums(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
 cudaError_t launch_embed_join(const EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);   // where chunks > 1
