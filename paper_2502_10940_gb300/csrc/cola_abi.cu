@@ -1961,7 +1961,7 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
     p.high = l.high;
     p.sort_ctas = l.sort_ctas;
     p.sort_each = l.sort_each;
-    p.filled = p.accumulate ? p.vocab : 0;
+    p.unfilled = p.accumulate ? 0 : p.vocab;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
     const bool few = p.n <= EMBED_FEW;

@@ -134,18 +134,25 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const EmbedParams P, co
 }
 
 // ------------------------------------------------------------- rows of no token
-// Rows [first, last) of the gradient := 0 but for those that `named` tells, by the
-// warps of `ctas` CTAs of which this is number `cta`.
-template <class TD, bool WHOLE, class F>
-__device__ __forceinline__ void fill_rows(const EmbedParams& P, int first, int last, int cta, int ctas, const F& named)
+// Rows [first, last) of the gradient := 0, by the warps of `ctas` CTAs of which this is
+// number `cta`; NAMED: but for those that tokens name.
+template <class TD, bool WHOLE, bool NAMED>
+__device__ __forceinline__ void fill_rows(const EmbedParams& P, int first, int last, int cta, int ctas)
 {
     const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const float zero[8] = {};
     for (int v = first + cta * warps + (threadIdx.x >> 5); v < last; v += ctas * warps)
-        if (!named(v))
+        if (!NAMED || !(P.present[v >> 5] >> (v & 31) & 1))
             for (int c = lane * 8; c < P.d; c += 256)
                 Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
 }
+
+// While tokens are sorted, CTAs of the same launches set rows [first, last) to 0, the
+// last rows of the table first, whether or not a token names them: the sums are stored
+// later, HBM has nothing else to do, and where ids go by frequency few of those are named.
+struct Fill {
+    int first, last, ctas;
+};
 
 // -------------------------------------------------------------- few tokens at once
 constexpr unsigned int NO_KEY = ~0u;
@@ -159,45 +166,39 @@ __device__ __forceinline__ unsigned int key_of(long long id, int vocab)
 // of them into bins by the lower ten bits of their ids, in shared memory and in any order,
 // and finds the places of its own tokens, by the number of tokens of lower bins and of
 // those in its bin that come before it (their order is by the ids' lower bits first).
-// The first CTAs do that, for ORDER_TOKENS each, and set the bits of the rows that are
-// named (`words_each` words each).  Each of the others has `rows_each` rows of the
-// table, and sets those to 0 that no id names.
+// They also set the bits of the rows that are named (`words_each` words each).
 constexpr int ORDER_THREADS = 512, ORDER_TOKENS = 64, ORDER_EACH = EMBED_FEW / ORDER_THREADS, BIN_BITS = 10, INDEX_BITS = 13;
 static_assert(EMBED_FEW <= 1 << INDEX_BITS && EMBED_VOCAB_MAX <= 1 << (BIN_BITS + 32 - INDEX_BITS), "a token's word");
 
 template <class TD, bool WHOLE>
-__global__ void __launch_bounds__(ORDER_THREADS) embed_order_kernel(const EmbedParams P, int order_ctas, int words_each, int rows_each)
+__global__ void __launch_bounds__(ORDER_THREADS) embed_order_kernel(const EmbedParams P, const Fill fill, int order_ctas, int words_each)
 {
     extern __shared__ unsigned int bits[];   // of rows
     __shared__ unsigned int first[1 << BIN_BITS], next[1 << BIN_BITS], warp_sum[ORDER_THREADS / 32];
     __shared__ unsigned int binned[EMBED_FEW];
     const int n = static_cast<int>(P.n), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool orders = static_cast<int>(blockIdx.x) < order_ctas;
     grid_launch_dependents();
+    if (static_cast<int>(blockIdx.x) >= order_ctas) {
+        fill_rows<TD, WHOLE, false>(P, fill.first, fill.last, blockIdx.x - order_ctas, fill.ctas);
+        return;
+    }
     unsigned int key[ORDER_EACH];
 #pragma unroll
     for (int j = 0; j < ORDER_EACH; ++j) {
         const int i = j * ORDER_THREADS + tid;
         key[j] = i < n ? key_of(P.ids[i], P.vocab) : NO_KEY;
     }
-    // the rows whose bits this CTA sets or uses
-    const unsigned int r0 = orders ? blockIdx.x * words_each * 32u : (blockIdx.x - order_ctas) * static_cast<unsigned int>(rows_each);
-    const unsigned int r1 = orders ? min(static_cast<unsigned int>(P.vocab), r0 + words_each * 32u)
-                                   : min(static_cast<unsigned int>(P.filled), r0 + rows_each);
+    const unsigned int r0 = blockIdx.x * words_each * 32u, r1 = min(static_cast<unsigned int>(P.unfilled), r0 + words_each * 32u);
     const int words = r1 > r0 ? (r1 - r0 + 31) / 32 : 0;
     for (int i = tid; i < words; i += ORDER_THREADS) bits[i] = 0;
-    if (orders) next[tid] = next[tid + 512] = 0;
+    next[tid] = next[tid + 512] = 0;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < ORDER_EACH; ++j) {
         if (key[j] >= r0 && key[j] < r1) atomicOr(bits + ((key[j] - r0) >> 5), 1u << ((key[j] - r0) & 31));
-        if (orders && key[j] != NO_KEY) atomicAdd(next + (key[j] & 1023), 1u);
+        if (key[j] != NO_KEY) atomicAdd(next + (key[j] & 1023), 1u);
     }
     __syncthreads();
-    if (!orders) {
-        fill_rows<TD, WHOLE>(P, r0, r1, 0, 1, [&](int v) { return bits[(v - r0) >> 5] >> ((v - r0) & 31) & 1; });
-        return;
-    }
     for (int i = tid; i < words; i += ORDER_THREADS) P.present[r0 / 32 + i] = bits[i];
     // first places of the bins, two a thread
     const unsigned int c0 = next[2 * tid], c1 = next[2 * tid + 1];
@@ -245,7 +246,7 @@ struct SortPass {
     unsigned int* hist;       // [CTA][digit]
     int shift, bits, ctas;
     unsigned int each;        // tokens of a warp, a multiple of 32
-    int fill_first, fill_last, fill_ctas;   // rows that CTAs behind the others set to 0 where no token names them
+    Fill fill;                // by the CTAs behind the others
 };
 
 // A batch of a warp's tokens: NO_KEY where there is none.
@@ -266,19 +267,15 @@ __device__ __forceinline__ void sort_load(const EmbedParams& P, const SortPass& 
     }
 }
 
-template <class TD, bool WHOLE, bool FIRST>
+template <bool FIRST>
 __global__ void __launch_bounds__(SORT_THREADS) embed_count_kernel(const EmbedParams P, const SortPass S)
 {
     __shared__ unsigned int total[1024];
     const int cta = blockIdx.x, digits = 1 << S.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (!FIRST) grid_dependency_wait();
     grid_launch_dependents();
-    if (!FIRST && cta >= S.ctas) {
-        fill_rows<TD, WHOLE>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
-        return;
-    }
     if (FIRST) {
-        for (int i = cta * SORT_THREADS + threadIdx.x; i < (P.vocab + 31) / 32; i += S.ctas * SORT_THREADS) P.present[i] = 0;
+        for (int i = cta * SORT_THREADS + threadIdx.x; i < (P.unfilled + 31) / 32; i += S.ctas * SORT_THREADS) P.present[i] = 0;
         if (cta == 0 && threadIdx.x == 0) *P.long_count = 0;
     }
     if (threadIdx.x < digits) total[threadIdx.x] = 0;
@@ -324,8 +321,8 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedPa
     const int cta = blockIdx.x, digits = 1 << S.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
     // the launch before this one counts; what this one ranks was there before that launch
     grid_launch_dependents();
-    if (!FIRST && cta >= S.ctas) {
-        fill_rows<TD, WHOLE>(P, S.fill_first, S.fill_last, cta - S.ctas, S.fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
+    if (cta >= S.ctas) {
+        fill_rows<TD, WHOLE, false>(P, S.fill.first, S.fill.last, cta - S.ctas, S.fill.ctas);
         return;
     }
     const unsigned int n = FIRST ? static_cast<unsigned int>(P.n) : *P.count;
@@ -407,11 +404,11 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedPa
             }
         }
     }
-    if (!FIRST || P.accumulate) return;
+    if (!FIRST || P.unfilled == 0) return;
     // the rows that the CTA's tokens name, in shared memory first: a few frequent tokens'
     // bits set one by one in L2 would take 20 us of 131072 tokens
     __syncthreads();
-    const int words = (P.vocab + 31) / 32;
+    const int words = (P.unfilled + 31) / 32;
     for (int i = tid; i < words; i += SORT_THREADS) place[i] = 0;
     __syncthreads();
     for (unsigned int b = begin; b < end; b += ROUNDS * 32) {
@@ -419,7 +416,7 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(const EmbedPa
 #pragma unroll
         for (int j = 0; j < ROUNDS; ++j) {
             const unsigned int k = key[j] & ((1u << KEY_BITS) - 1);
-            if (key[j] != NO_KEY) atomicOr(place + (k >> 5), 1u << (k & 31));
+            if (key[j] != NO_KEY && k < P.unfilled) atomicOr(place + (k >> 5), 1u << (k & 31));
         }
     }
     __syncthreads();
@@ -487,14 +484,35 @@ __device__ __forceinline__ void store_columns(__nv_bfloat16* p, const float (&x)
     }
 }
 
+// Four columns of fp32 are added to, without waiting for what they were.  (Nobody else
+// adds to them in this call: the order of the addition is no matter.  Values below the
+// smallest normal number count as 0 there.)
+__device__ __forceinline__ void add_four(float* p, float a, float b, float c, float d)
+{
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
+
 template <class TD, int N>
 __device__ __forceinline__ void store_sum(const EmbedParams& P, unsigned int id, int c, const Sum<N>& sum)
 {
     TD* p = static_cast<TD*>(P.dst) + id * P.ld_dst + c;
-    float x[N], s[N];
-    sum.values(s);
+    float x[N];
+    sum.values(x);
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = fmaf(P.scale, s[k], P.accumulate && k < P.d - c ? Elem<TD>::get(p + k) : 0.f);
+    for (int k = 0; k < N; ++k) x[k] *= P.scale;
+    if constexpr (sizeof(TD) == 4) {
+        if (P.accumulate) {
+            if (P.d - c >= N) {
+#pragma unroll
+                for (int k = 0; k < N; k += 4) add_four(p + k, x[k], x[k + 1], x[k + 2], x[k + 3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < N - 1; ++k)
+                    if (k < P.d - c) p[k] += x[k];
+            }
+            return;
+        }
+    }
     store_columns(p, x, P.d - c);
 }
 
@@ -549,7 +567,7 @@ __device__ __forceinline__ int last_chunk(const EmbedParams& P, int first, int a
 constexpr int BATCH = 4, BATCHES = 4;
 
 template <class TX, class TD, bool WHOLE>
-__global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, const Groups g, int sum_ctas, int fill_first)
+__global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, const Groups g, int sum_ctas)
 {
     constexpr int N = COLS<TX>;
     extern __shared__ uint4 ring[];   // [row of the batches][thread]
@@ -558,7 +576,7 @@ __global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, 
     // the CTAs that set rows to 0 lie evenly between the others
     const int fill_ctas = gridDim.x - sum_ctas, fills = static_cast<int>(static_cast<long long>(blockIdx.x) * fill_ctas / gridDim.x);
     if (fills != static_cast<int>((blockIdx.x + 1ll) * fill_ctas / gridDim.x)) {
-        fill_rows<TD, WHOLE>(P, fill_first, P.vocab, fills, fill_ctas, [&](int v) { return P.present[v >> 5] >> (v & 31) & 1; });
+        fill_rows<TD, WHOLE, true>(P, 0, P.unfilled, fills, fill_ctas);
         return;
     }
     const int at = (blockIdx.x - fills) << (8 - g.shift) | threadIdx.x >> g.shift, chunk = at / g.tiles, tile = at - chunk * g.tiles;
@@ -765,39 +783,41 @@ cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
     const Groups g = groups(p.d, COLS<TX>);
     const int per = 256 >> g.shift;
     const int ctas = static_cast<int>((static_cast<long long>(p.chunks) * g.tiles + per - 1) / per);
-    const int fill = p.filled < p.vocab ? std::min(4 * sms, (p.vocab - p.filled + 7) / 8) : 0;
-    return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, ctas, p.filled);
+    const int fill = std::min(4 * sms, (p.unfilled + 7) / 8);
+    return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, ctas);
 }
 
-// Rows of the table that the CTAs beside one of the sort's launches set to 0 (from
-// p.filled on, to the result): what HBM takes in the time that the launch takes anyway.
+// What a launch that places tokens sets to 0 beside that: what HBM takes in the 6 us that it
+// runs anyway (a launch that counts is too short to gain from it).
 constexpr double FILL_BYTES = 24e6;
-int fill_to(const EmbedParams& p, size_t element)
+
+Fill take_fill(EmbedParams& p, size_t element, int ctas)
 {
-    return static_cast<int>(std::min<double>(p.vocab, p.filled + FILL_BYTES / (static_cast<double>(p.d) * element)));
+    Fill f = {p.unfilled, p.unfilled, 0};
+    if (ctas > 0) f.first = static_cast<int>(std::max(0.0, p.unfilled - FILL_BYTES / (static_cast<double>(p.d) * element)));
+    f.ctas = std::min(ctas, f.last - f.first);
+    p.unfilled = f.first;
+    return f;
 }
 
 template <class TD, bool WHOLE>
 cudaError_t order(EmbedParams& p, int sms, cudaStream_t stream)
 {
     const int n = static_cast<int>(p.n), order_ctas = (n + ORDER_TOKENS - 1) / ORDER_TOKENS;
-    p.filled = p.accumulate ? 0 : fill_to(p, sizeof(TD));
-    const int fill = std::min(2 * sms, (p.filled + 7) / 8), rows_each = fill ? (p.filled + fill - 1) / fill : 0;
-    const int words_each = p.accumulate || p.filled == p.vocab ? 0 : ((p.vocab + 31) / 32 + order_ctas - 1) / order_ctas;
-    const size_t smem = sizeof(unsigned int) * std::max(words_each, (rows_each + 31) / 32);
+    const Fill fill = take_fill(p, sizeof(TD), sms);
+    const int words_each = ((p.unfilled + 31) / 32 + order_ctas - 1) / order_ctas;
     static std::atomic<unsigned long long> configured{0};
     const cudaError_t e = allow_smem(embed_order_kernel<TD, WHOLE>, EMBED_VOCAB_MAX / 8, configured);
     if (e != cudaSuccess) return e;
-    embed_order_kernel<TD, WHOLE><<<order_ctas + fill, ORDER_THREADS, smem, stream>>>(p, order_ctas, words_each, rows_each);
-    if (p.accumulate) p.filled = p.vocab;
+    embed_order_kernel<TD, WHOLE><<<order_ctas + fill.ctas, ORDER_THREADS, sizeof(unsigned int) * words_each, stream>>>(p, fill, order_ctas, words_each);
     return cudaGetLastError();
 }
 
-template <class TD, bool WHOLE, bool FIRST>
+template <bool FIRST>
 cudaError_t count(const EmbedParams& p, const SortPass& s, cudaStream_t stream)
 {
-    if (!FIRST) return launch_behind(embed_count_kernel<TD, WHOLE, FIRST>, s.ctas + s.fill_ctas, SORT_THREADS, 0, stream, p, s);
-    embed_count_kernel<TD, WHOLE, FIRST><<<s.ctas, SORT_THREADS, 0, stream>>>(p, s);
+    if (!FIRST) return launch_behind(embed_count_kernel<FIRST>, s.ctas, SORT_THREADS, 0, stream, p, s);
+    embed_count_kernel<FIRST><<<s.ctas, SORT_THREADS, 0, stream>>>(p, s);
     return cudaGetLastError();
 }
 
@@ -807,7 +827,7 @@ cudaError_t place(const EmbedParams& p, const SortPass& s, cudaStream_t stream)
     static std::atomic<unsigned long long> configured{0};
     const cudaError_t e = allow_smem(embed_place_kernel<TD, WHOLE, FIRST>, sizeof(unsigned int) * SORT_WARPS << 10, configured);
     if (e != cudaSuccess) return e;
-    return launch_behind(embed_place_kernel<TD, WHOLE, FIRST>, s.ctas + s.fill_ctas, SORT_THREADS,
+    return launch_behind(embed_place_kernel<TD, WHOLE, FIRST>, s.ctas + s.fill.ctas, SORT_THREADS,
                          sizeof(unsigned int) * SORT_WARPS << s.bits, stream, p, s);
 }
 
@@ -828,13 +848,13 @@ template <class TD, bool WHOLE>
 cudaError_t sort_launch(EmbedParams& p, int launch, int sms, cudaStream_t stream)
 {
     SortPass s = sort_pass(p, launch / 2);
-    if (launch < 2) return launch == 0 ? count<TD, WHOLE, true>(p, s, stream) : place<TD, WHOLE, true>(p, s, stream);
-    if (!p.accumulate && sms > s.ctas) {   // (the first pass found out which rows the tokens name)
-        s.fill_first = p.filled;
-        s.fill_last = p.filled = fill_to(p, sizeof(TD));
-        s.fill_ctas = s.fill_last > s.fill_first ? sms - s.ctas : 0;
+    s.fill = take_fill(p, sizeof(TD), launch % 2 ? sms - s.ctas : 0);
+    switch (launch) {
+    case 0: return count<true>(p, s, stream);
+    case 1: return place<TD, WHOLE, true>(p, s, stream);
+    case 2: return count<false>(p, s, stream);
+    default: return place<TD, WHOLE, false>(p, s, stream);
     }
-    return launch == 2 ? count<TD, WHOLE, false>(p, s, stream) : place<TD, WHOLE, false>(p, s, stream);
 }
 
 template <class TD>
@@ -854,8 +874,9 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, si
         return a;
     };
     const Groups g = groups(d, dtype_x == 0 ? COLS<__nv_bfloat16> : COLS<float>);
-    // eight CTAs' worth of groups for every SM, of eight tokens at least
-    const double per = static_cast<double>(n) * (g.tiles << g.shift) / (8.0 * sms * 256);
+    // twelve CTAs' worth of groups for every SM, of eight tokens at least (131072 x 4096 bf16:
+    // 209 us, with eight 217, five 233, three 262)
+    const double per = static_cast<double>(n) * (g.tiles << g.shift) / (12.0 * sms * 256);
     l.chunk = std::max(8, static_cast<int>(std::min(per / 8 + 1, 1e6)) * 8);
     l.chunks = static_cast<int>((n + l.chunk - 1) / l.chunk);
     l.sorted = take(n * sizeof(uint2));

@@ -34,8 +34,8 @@ struct EmbedParams {
     uint4* long_sums;         // of each the chunks that it begins and ends in, and its id
     float* partials;          // 2 per chunk, d rounded up to 8: of a sum that began before the chunk, and of one that goes on behind it
     int chunk, chunks;        // sorted tokens of a chunk; chunks of n
-    unsigned int* present;    // a bit for each row of the table that a token names
-    int filled;               // rows of no token below this one are 0 already
+    unsigned int* present;    // a bit for each row below `unfilled` that a token names
+    int unfilled;             // the rows of no token that are still to be set to 0 lie below this one
     // more than EMBED_FEW tokens
     uint2* between;           // after the first pass of the sort
     unsigned int* hist[2];
@@ -54,9 +54,9 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, si
 
 // dtypes: cola_dtype_t of src and dst
 cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
-// the order of up to EMBED_FEW tokens; sets rows of no token to 0, up to p.filled then
+// The order of up to EMBED_FEW tokens; that of more, in launches 0 .. 3 (0 and 1 where high
+// is 0).  They also set rows to 0, and lower p.unfilled.
 cudaError_t launch_embed_order(EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);
-// that of more, in launches 0 .. 3 (0 and 1 where high is 0); the last two set rows of no token to 0 too
 cudaError_t launch_embed_sort(EmbedParams& p, int launch, int dtype_dst, int sms, cudaStream_t stream);
 cudaError_t launch_embed_sums(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
 cudaError_t launch_embed_join(const EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);   // where chunks > 1
