@@ -9,21 +9,20 @@
 namespace cola {
 namespace {
 
-// of a token that the history or the biases name: flags above its count
-constexpr unsigned int SEEN = 1u << 31, BIASED = 1u << 30, COUNT = BIASED - 1;
-constexpr int MOST_TOKENS = 24576;            // of a CTA
 constexpr int SMEM_MOST = 200 * 1024;
+constexpr long long FILL = 8;
 
+// A row's mask, the words of the CTA's tokens in shared memory.
 struct Mask {
     const unsigned int* words;   // nullptr: everything is allowed
-    __device__ __forceinline__ bool allows(int token) const { return !words || (words[token >> 5] >> (token & 31) & 1); }
-    // of the E tokens from `token` on, which all lie in the row
+    int first;                   // the token of the first word's first bit
+    __device__ __forceinline__ bool allows(int token) const { return !words || (words[(token - first) >> 5] >> ((token - first) & 31) & 1); }
+    // of the E tokens from `token` on
     template <int E>
     __device__ __forceinline__ unsigned int banned(int token) const
     {
-        const int w = token >> 5, s = token & 31;
-        const unsigned int lo = words[w], hi = s + E > 32 ? words[w + 1] : 0;
-        return ~__funnelshift_r(lo, hi, s) & ((1u << E) - 1);
+        const int w = (token - first) >> 5;
+        return ~__funnelshift_r(words[w], words[w + 1], (token - first) & 31) & ((1u << E) - 1);
     }
 };
 
@@ -43,28 +42,25 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
     }
 }
 
-// A CTA has a share of a row's tokens.  In one loop
-//   - it counts those of them that the row's history and biases name, each in a slot of its
-//     own in shared memory: one per token of the share, or, where the history may name few
-//     of the share, slots found by a hash of the id.  Whoever finds a slot empty lists it.
-//   - it copies the share, masked logits replaced: neither waits for the other.
-// Then the listed tokens' results are stored over the copies.  The counts do not depend on
-// the order of the atomics, and a listed token's place in the list does not matter.
-template <class T, bool BWD, int THREADS>
+// A CTA has a share of a row's tokens.  In one loop it copies them, masked logits replaced,
+// and counts, in shared memory, those that the row's history names behind the prompt
+// (COUNTS: in 16 or 32 bits, where anything depends on it; 0: not).  Then the tokens that
+// history and biases name are gone through again: whoever claims one first, by a bit of its
+// own, stores its result over the copy.  The counts do not depend on the order of the
+// atomics, and it does not matter who claims.
+template <class T, bool BWD, int COUNTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
     constexpr int E = Elem<T>::E, U = 4, IDS = 4;
-    extern __shared__ __align__(16) unsigned int count[];   // P.slots of them, P.room of the list, P.slots of keys (hashed)
-    __shared__ int bias_ids[BWD ? 1 : BIAS_MAX];
-    __shared__ float bias[BWD ? 1 : BIAS_MAX];
-    __shared__ unsigned int listed;
-    unsigned int *list = count + P.slots, *keys = list + P.room;
+    // bits of the share's tokens (P.words each): claimed, masked, biased or (a gradient) of a
+    // positive logit; counts; biases
+    extern __shared__ __align__(16) unsigned int claimed[];
+    const int n_bias = BWD ? 0 : P.n_bias;
+    unsigned int *words = claimed + P.words, *extra = words + P.words, *counts = extra + P.words;
+    int* bias_ids = reinterpret_cast<int*>(counts + P.counts);
+    float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
     const long long i = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31;
-    const long long* h = P.history + i * P.ld_history;
-    const long long length = !P.history ? 0 : P.history_len ? P.history_len[i] : P.history_width;
-    const long long prompt = P.prompt_len ? P.prompt_len[i] : 0;
-    const long long which = !P.masks ? -1 : P.mask_of ? P.mask_of[i] : i;
     const T* logits = static_cast<const T*>(P.logits) + i * P.ld;
     const T* in = static_cast<const T*>(P.src) + i * P.ld_src;
     T* out = static_cast<T*>(P.dst) + i * P.ld_dst;
@@ -74,125 +70,150 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const int begin = blockIdx.y == 0 ? 0 : row.head + v0 * E, end = last ? P.vocab : row.head + v1 * E;
     const bool in_place = static_cast<const void*>(in) == static_cast<void*>(out);
     const bool same = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
-    const uint4* src = row.vec();
-    T* dst = out + row.head;
-    for (int k = tid; k < P.slots; k += THREADS) count[k] = 0;
-    if (P.hashed)
-        for (int k = tid; k < P.slots; k += THREADS) keys[k] = 0;
-    if (tid == 0) listed = 0;
-    const int n = static_cast<int>(min(max(length, 0ll), P.history_width));
-    const Mask mask{which >= 0 && which < P.n_masks ? P.masks + which * P.ld_masks : nullptr};
+    // the first ids on their way with what tells how many count
+    const long long* h = P.history + i * P.ld_history;
+    const int width = P.history ? static_cast<int>(P.history_width) : 0;
+    long long id[IDS];
+    const auto get_ids = [&](int k, int stop) {
+#pragma unroll
+        for (int j = 0; j < IDS; ++j) id[j] = k + j * THREADS < stop ? h[k + j * THREADS] : -1;
+    };
+    get_ids(tid, width);
+    const long long length = !P.history ? 0 : P.history_len ? P.history_len[i] : P.history_width;
+    const long long prompt = COUNTS && P.prompt_len ? P.prompt_len[i] : 0;
+    const long long which = !P.masks ? -1 : P.mask_of ? P.mask_of[i] : i;
+    for (int k = tid; k < P.words; k += THREADS) claimed[k] = extra[k] = 0;
+    if (COUNTS)
+        for (int k = tid * 4; k < P.counts; k += THREADS * 4) *reinterpret_cast<uint4*>(counts + k) = make_uint4(0, 0, 0, 0);
+    const int n = static_cast<int>(min(max(length, 0ll), static_cast<long long>(width)));
+    const bool masked = which >= 0 && which < P.n_masks;
+    if (masked) {
+        const unsigned int* m = P.masks + which * P.ld_masks;
+        for (int w = begin / 32 + tid; w < (end + 31) / 32; w += THREADS) words[w - begin / 32] = m[w];
+    }
+    const Mask mask{masked ? words : nullptr, begin / 32 * 32};
     __syncthreads();
-    const auto name = [&](long long id, unsigned int flag) {   // flag 0: counted
-        if (id < begin || id >= end) return;
-        unsigned int slot = static_cast<unsigned int>(id - begin);
-        if (P.hashed) {
-            const unsigned int key = slot + 1;
-            slot = __umulhi(key * 2654435769u, P.slots);
-            for (unsigned int old; (old = atomicCAS(keys + slot, 0u, key)) != 0 && old != key;)
-                if (++slot == static_cast<unsigned int>(P.slots)) slot = 0;   // (more slots than names: there is one)
-        }
-        if ((flag ? atomicOr(count + slot, flag) : atomicAdd(count + slot, 1u)) == 0) list[atomicAdd(&listed, 1u)] = slot;
+    // an id's number in the share, -1 where it is not of the share
+    const auto number = [&](long long t) {
+        return static_cast<unsigned long long>(t - begin) < static_cast<unsigned long long>(end - begin) ? static_cast<int>(t - begin) : -1;
     };
     if constexpr (!BWD)
-        for (int k = tid; k < P.n_bias; k += THREADS) {
-            const long long id = P.bias_ids[i * P.n_bias + k];
-            bias_ids[k] = id >= begin && id < end ? static_cast<int>(id) : -1;
-            bias[k] = P.bias[i * P.n_bias + k];
-            name(id, BIASED);
+        for (int k = tid; k < n_bias; k += THREADS) {
+            const int t = number(P.bias_ids[i * n_bias + k]);
+            bias_ids[k] = t;
+            bias[k] = P.bias[i * n_bias + k];
+            if (t >= 0) atomicOr(extra + (t >> 5), 1u << (t & 31));
         }
-    // (a gradient over the logits: their signs are read before they are gone)
-    const bool over = BWD && !in_place && static_cast<const void*>(logits) == static_cast<void*>(out);
-    const int stop = (!in_place || mask.words) && !over ? v1 : v0;
-    const auto copy = [&](int from, int to, bool ids) {
-        for (int v = from + tid - lane, k = tid; v < to || (ids && k - lane < n); v += U * THREADS, k += IDS * THREADS) {
-            long long id[IDS];
-            uint4 d[U];
-            unsigned int banned[U];
-#pragma unroll
-            for (int j = 0; j < IDS; ++j) id[j] = ids && k + j * THREADS < n ? h[k + j * THREADS] : -1;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = v + u * THREADS + lane;
-                banned[u] = 0;
-                d[u] = make_uint4(0, 0, 0, 0);
-                if (at >= to) continue;
-                if (mask.words) banned[u] = mask.template banned<E>(row.head + at * E);
-                if (banned[u] != (1u << E) - 1 && (!in_place || banned[u])) d[u] = src[at];
-            }
-#pragma unroll
-            for (int j = 0; j < IDS; ++j) name(id[j], BWD || k + j * THREADS < prompt ? SEEN : 0);
-            __syncwarp();
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = v + u * THREADS + lane;
-                if (v + u * THREADS >= to) break;
-                if (banned[u]) ban<T, BWD>(d[u], banned[u]);
-                if (!same) store_apart(dst + at * E, d[u], at < to);
-                else if (at < to && (!in_place || banned[u])) reinterpret_cast<uint4*>(dst)[at] = d[u];
-            }
+    if (BWD && P.over) {   // a gradient over the logits: their signs are read before they are gone
+        for (int k = tid; k < n; k += THREADS) {
+            const int t = number(h[k]);
+            if (t >= 0 && Elem<T>::get(logits + begin + t) > 0.f) atomicOr(extra + (t >> 5), 1u << (t & 31));
         }
-    };
-    const auto copy_edges = [&] {
-        for (int k = tid; k < row.edges(); k += THREADS) {
-            const int id = row.edge(k);
-            if (id < row.head ? blockIdx.y != 0 : !last) continue;
-            if (!mask.allows(id)) Elem<T>::put(out + id, BWD ? 0.f : NEG_INF);
-            else if (!in_place) out[id] = in[id];
-        }
-    };
-    copy(v0, stop, true);
-    if (!over) copy_edges();
-    __syncthreads();
-    const int names = listed;
-    const float r = P.repetition ? P.repetition[i] : 1.f;
-    const float f = !BWD && P.frequency ? P.frequency[i] : 0.f, p = !BWD && P.presence ? P.presence[i] : 0.f;
-    const auto token_of = [&](unsigned int slot) { return begin + static_cast<int>(P.hashed ? keys[slot] - 1 : slot); };
-    const auto result = [&](unsigned int slot, int token) -> float {
-        const unsigned int c = count[slot], times = c & COUNT;
-        float x = Elem<T>::get(logits + token);
-        if constexpr (BWD) {
-            const float g = Elem<T>::get(in + token);
-            return x > 0.f ? g / r : g * r;
-        }
-        if (c & ~BIASED) x = x > 0.f ? x / r : x * r;
-        if (times) x = x - f * static_cast<float>(times) - p;
-        if (c & BIASED) {
-            float sum = 0.f;
-            for (int e = 0; e < P.n_bias; ++e)
-                if (bias_ids[e] == token) sum += bias[e];
-            x += sum;
-        }
-        return x;
-    };
-    if (over) {
-        for (int k = tid; k < names; k += THREADS) count[list[k]] = __float_as_uint(result(list[k], token_of(list[k])));
-        __syncthreads();
-        copy(v0, v1, false);
-        copy_edges();
         __syncthreads();
     }
-#pragma unroll 2
-    for (int k = tid; k < names; k += THREADS) {
-        const unsigned int slot = list[k];
-        const int token = token_of(slot);
-        if (!mask.allows(token)) continue;
-        Elem<T>::put(out + token, over ? __uint_as_float(count[slot]) : result(slot, token));
+    const uint4* src = row.vec();
+    T* dst = out + row.head;
+    const int stop = !in_place || masked ? v1 : v0, ids = COUNTS ? n : 0;
+    for (int v = v0 + tid - lane, k = tid; v < stop || k - lane < ids; v += U * THREADS, k += IDS * THREADS) {
+        uint4 d[U];
+        unsigned int banned[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = v + u * THREADS + lane;
+            banned[u] = 0;
+            d[u] = make_uint4(0, 0, 0, 0);
+            if (at >= stop) continue;
+            if (masked) banned[u] = mask.template banned<E>(row.head + at * E);
+            if (banned[u] != (1u << E) - 1 && (!in_place || banned[u])) d[u] = src[at];
+        }
+        if (k - lane < ids) {
+#pragma unroll
+            for (int j = 0; j < IDS; ++j) {
+                const int t = number(id[j]), at = k + j * THREADS;
+                if (t < 0 || at >= n || at < prompt) continue;
+                if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
+                else atomicAdd(counts + t, 1u);
+            }
+            get_ids(k + IDS * THREADS, n);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = v + u * THREADS + lane;
+            if (v + u * THREADS >= stop) break;
+            if (banned[u]) ban<T, BWD>(d[u], banned[u]);
+            if (!same) store_apart(dst + at * E, d[u], at < stop);
+            else if (at < stop && (!in_place || banned[u])) reinterpret_cast<uint4*>(dst)[at] = d[u];
+        }
+    }
+    for (int k = tid; k < row.edges(); k += THREADS) {
+        const int t = row.edge(k);
+        if (t < row.head ? blockIdx.y != 0 : !last) continue;
+        if (!mask.allows(t)) Elem<T>::put(out + t, BWD ? 0.f : NEG_INF);
+        else if (!in_place) out[t] = in[t];
+    }
+    const float r = P.repetition ? P.repetition[i] : 1.f;
+    const float f = COUNTS && P.frequency ? P.frequency[i] : 0.f, p = COUNTS && P.presence ? P.presence[i] : 0.f;
+    if (COUNTS || n > IDS * THREADS) get_ids(tid, n);
+    __syncthreads();
+    const auto claim = [&](int t) {
+        const unsigned int bit = 1u << (t & 31);
+        if (t < 0 || !mask.allows(begin + t) || (*static_cast<volatile unsigned int*>(claimed + (t >> 5)) & bit)) return false;
+        return !(atomicOr(claimed + (t >> 5), bit) & bit);
+    };
+    const auto biased = [&](int t) -> float {
+        if (BWD || !(extra[t >> 5] >> (t & 31) & 1)) return 0.f;
+        float sum = 0.f;
+        for (int e = 0; e < n_bias; ++e)
+            if (bias_ids[e] == t) sum += bias[e];
+        return sum;
+    };
+    for (int k = tid; k < n; k += IDS * THREADS) {
+        int mine[IDS];
+        float x[IDS], g[IDS];
+#pragma unroll
+        for (int j = 0; j < IDS; ++j) {
+            mine[j] = k + j * THREADS < n ? number(id[j]) : -1;
+            if (!claim(mine[j])) mine[j] = -1;
+        }
+        if (k + IDS * THREADS < n) get_ids(k + IDS * THREADS, n);
+#pragma unroll
+        for (int j = 0; j < IDS; ++j)
+            if (mine[j] >= 0) {
+                if (!BWD || !P.over) x[j] = Elem<T>::get(logits + begin + mine[j]);
+                if (BWD) g[j] = Elem<T>::get(in + begin + mine[j]);
+            }
+#pragma unroll
+        for (int j = 0; j < IDS; ++j) {
+            const int t = mine[j];
+            if (t < 0) continue;
+            float y;
+            if constexpr (BWD) {
+                const bool positive = P.over ? extra[t >> 5] >> (t & 31) & 1 : x[j] > 0.f;
+                y = positive ? g[j] / r : g[j] * r;
+            } else {
+                y = x[j] > 0.f ? x[j] / r : x[j] * r;
+                if (COUNTS) {
+                    const unsigned int times = COUNTS == 16 ? counts[t >> 1] >> (t & 1) * 16 & 0xffffu : counts[t];
+                    if (times) y = y - f * static_cast<float>(times) - p;
+                }
+                if (n_bias) y += biased(t);
+            }
+            Elem<T>::put(out + begin + t, y);
+        }
+    }
+    if (!BWD && n_bias) {
+        __syncthreads();
+        for (int k = tid; k < n_bias; k += THREADS) {
+            const int t = bias_ids[k];
+            if (claim(t)) Elem<T>::put(out + begin + t, Elem<T>::get(logits + begin + t) + biased(t));
+        }
     }
 }
 
-template <class T, bool BWD, int THREADS>
-cudaError_t constrain(ConstrainParams& p, int parts, cudaStream_t stream)
+template <class T, bool BWD, int COUNTS, int THREADS>
+cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStream_t stream)
 {
-    constexpr int E = Elem<T>::E;
-    const int full = p.vocab / E;
-    p.each = (full + parts - 1) / parts;
-    const long long tokens = p.each * E + 2 * E, names = (p.history ? p.history_width : 0) + p.n_bias;
-    p.room = static_cast<int>(std::min(tokens, names));
-    p.hashed = names + names / 2 < tokens;
-    p.slots = static_cast<int>(p.hashed ? names + names / 2 + 1 : p.room ? tokens : 0);
-    const size_t smem = sizeof(unsigned int) * ((p.hashed ? 2 : 1) * p.slots + p.room);
-    auto kern = constrain_kernel<T, BWD, THREADS>;
+    auto kern = constrain_kernel<T, BWD, COUNTS, THREADS>;
     static std::atomic<unsigned long long> configured{0};   // bit d: set on device d
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -206,30 +227,38 @@ cudaError_t constrain(ConstrainParams& p, int parts, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-// Many rows: CTAs of 256 threads and up to 32768 tokens, eight an SM if there are as many.
-// Few: more CTAs a row, to a vector per thread; but every CTA of a row reads all of its
-// history, so that a CTA has a sixteenth as many vectors as the history has ids at least.
-template <class T, bool BWD>
+template <class T, bool BWD, int COUNTS>
 cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
 {
-    constexpr int E = Elem<T>::E;
+    constexpr int E = Elem<T>::E, MOST = COUNTS == 32 ? 16384 : 32768;   // tokens of a CTA
     const int full = p.vocab / E;
     const long long width = p.history ? p.history_width : 0;
-    const long long wanted = std::min<long long>((8ll * sms + p.n - 1) / p.n, full / std::max(256ll, width / 16));
-    // (shared memory: 12 bytes for each token at most, or 16 for each name)
-    const long long least = (full * static_cast<long long>(E) + MOST_TOKENS - 1) / MOST_TOKENS;
-    const int parts = static_cast<int>(std::max({wanted, least, 1ll}));
-    if (width > 16 * 256 && p.n * parts <= 2ll * sms) return constrain<T, BWD, 1024>(p, parts, stream);
-    return constrain<T, BWD, 256>(p, parts, stream);
+    const int threads = width > 4096 ? 1024 : 256;
+    const long long fill = threads == 1024 ? sms / p.n : (FILL * sms + p.n - 1) / p.n;
+    const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads, width / 16));
+    const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + MOST - 1) / MOST), 1ll}));
+    p.each = (full + parts - 1) / parts;
+    const int tokens = p.each * E + 2 * E;
+    p.words = (tokens / 32 + 3 + 3) / 4 * 4;
+    p.counts = COUNTS ? (tokens / (32 / COUNTS) + 4) / 4 * 4 : 0;
+    p.over = BWD && p.logits == p.dst && p.logits != p.src;
+    const size_t smem = 4 * static_cast<size_t>(3 * p.words + p.counts + 2 * p.n_bias);
+    return threads == 256 ? constrain<T, BWD, COUNTS, 256>(p, parts, smem, stream) : constrain<T, BWD, COUNTS, 1024>(p, parts, smem, stream);
+}
+
+template <class T>
+cudaError_t constrain_counts(const ConstrainParams& p, bool backward, int sms, cudaStream_t stream)
+{
+    if (backward) return constrain_plan<T, true, 0>(p, sms, stream);
+    if (!p.history || !(p.frequency || p.presence)) return constrain_plan<T, false, 0>(p, sms, stream);
+    return p.history_width < 65536 ? constrain_plan<T, false, 16>(p, sms, stream) : constrain_plan<T, false, 32>(p, sms, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_constrain(const ConstrainParams& p, int dtype, bool backward, int sms, cudaStream_t stream)
 {
-    using bf16 = __nv_bfloat16;
-    if (dtype == 0) return backward ? constrain_plan<bf16, true>(p, sms, stream) : constrain_plan<bf16, false>(p, sms, stream);
-    return backward ? constrain_plan<float, true>(p, sms, stream) : constrain_plan<float, false>(p, sms, stream);
+    return dtype == 0 ? constrain_counts<__nv_bfloat16>(p, backward, sms, stream) : constrain_counts<float>(p, backward, sms, stream);
 }
 
 }  // namespace cola

@@ -23,7 +23,8 @@ struct ConstrainParams {
     long long n, ld, ld_src, ld_dst;
     int vocab;
     int each;                 // 16-byte vectors of a row per CTA (the grid's y)
-    int slots, room, hashed;  // of a CTA: slots for the tokens that are named, most of them that there are, how a slot is found
+    int words, counts;        // of a CTA's tokens: words of a bit each, words of counts
+    int over;                 // the gradient lies over the logits
     const long long* history;
     long long history_width, ld_history;
     const long long* history_len;
