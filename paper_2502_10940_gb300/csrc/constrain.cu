@@ -43,22 +43,24 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 }
 
 // A CTA has a share of a row's tokens.  In one loop it copies them, masked logits replaced,
-// and counts, in shared memory, those that the row's history names behind the prompt
-// (COUNTS: in 16 or 32 bits, where anything depends on it; 0: not).  Then the tokens that
-// history and biases name are gone through again: whoever claims one first, by a bit of its
-// own, stores its result over the copy.  The counts do not depend on the order of the
-// atomics, and it does not matter who claims.
+// and goes through the row's history: a bit of shared memory tells of each token whether the
+// history names it, who sets it lists the token, and those behind the prompt are counted
+// (COUNTS: in 16 or 32 bits, where anything depends on it; 0: not).  Then the listed
+// tokens' results are stored over the copies.  Counts do not depend on the order of the
+// atomics, and a token's place in the list does not matter.
 template <class T, bool BWD, int COUNTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
-    constexpr int E = Elem<T>::E, U = 4, IDS = 4;
-    // bits of the share's tokens (P.words each): claimed, masked, biased or (a gradient) of a
-    // positive logit; counts; biases
-    extern __shared__ __align__(16) unsigned int claimed[];
+    constexpr int E = Elem<T>::E, U = 4, IDS = 4, NAMES = 4;
+    // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
+    // gradient over the logits) of a positive logit; counts; biases; the list
+    extern __shared__ __align__(16) unsigned int seen[];
+    __shared__ unsigned int listed;
     const int n_bias = BWD ? 0 : P.n_bias;
-    unsigned int *words = claimed + P.words, *extra = words + P.words, *counts = extra + P.words;
+    unsigned int *words = seen + P.words, *extra = words + P.words, *counts = extra + P.words;
     int* bias_ids = reinterpret_cast<int*>(counts + P.counts);
     float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
+    unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias);
     const long long i = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31;
     const T* logits = static_cast<const T*>(P.logits) + i * P.ld;
@@ -82,9 +84,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const long long length = !P.history ? 0 : P.history_len ? P.history_len[i] : P.history_width;
     const long long prompt = COUNTS && P.prompt_len ? P.prompt_len[i] : 0;
     const long long which = !P.masks ? -1 : P.mask_of ? P.mask_of[i] : i;
-    for (int k = tid; k < P.words; k += THREADS) claimed[k] = extra[k] = 0;
+    const float r = P.repetition ? P.repetition[i] : 1.f;
+    const float f = COUNTS && P.frequency ? P.frequency[i] : 0.f, p = COUNTS && P.presence ? P.presence[i] : 0.f;
+    for (int k = tid; k < P.words; k += THREADS) seen[k] = extra[k] = 0;
     if (COUNTS)
         for (int k = tid * 4; k < P.counts; k += THREADS * 4) *reinterpret_cast<uint4*>(counts + k) = make_uint4(0, 0, 0, 0);
+    if (tid == 0) listed = 0;
     const int n = static_cast<int>(min(max(length, 0ll), static_cast<long long>(width)));
     const bool masked = which >= 0 && which < P.n_masks;
     if (masked) {
@@ -97,53 +102,69 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const auto number = [&](long long t) {
         return static_cast<unsigned long long>(t - begin) < static_cast<unsigned long long>(end - begin) ? static_cast<int>(t - begin) : -1;
     };
-    if constexpr (!BWD)
+    const auto get_bit = [](const unsigned int* bits, int t) { return bits[t >> 5] >> (t & 31) & 1; };
+    const auto set_bit = [](unsigned int* bits, int t) { return atomicOr(bits + (t >> 5), 1u << (t & 31)) >> (t & 31) & 1; };
+    const auto append = [&](int t) {   // (one atomic for all that get here together)
+        const unsigned int together = __activemask(), first = __ffs(together) - 1;
+        unsigned int at = 0;
+        if (lane == first) at = atomicAdd(&listed, static_cast<unsigned int>(__popc(together)));
+        at = __shfl_sync(together, at, first) + __popc(together & ((1u << lane) - 1));
+        list[at] = static_cast<unsigned short>(t);
+    };
+    if (!BWD && n_bias) {
         for (int k = tid; k < n_bias; k += THREADS) {
             const int t = number(P.bias_ids[i * n_bias + k]);
             bias_ids[k] = t;
             bias[k] = P.bias[i * n_bias + k];
-            if (t >= 0) atomicOr(extra + (t >> 5), 1u << (t & 31));
-        }
-    if (BWD && P.over) {   // a gradient over the logits: their signs are read before they are gone
-        for (int k = tid; k < n; k += THREADS) {
-            const int t = number(h[k]);
-            if (t >= 0 && Elem<T>::get(logits + begin + t) > 0.f) atomicOr(extra + (t >> 5), 1u << (t & 31));
+            if (t >= 0 && !set_bit(extra, t)) append(t);
         }
         __syncthreads();
     }
     const uint4* src = row.vec();
     T* dst = out + row.head;
-    const int stop = !in_place || masked ? v1 : v0, ids = COUNTS ? n : 0;
-    for (int v = v0 + tid - lane, k = tid; v < stop || k - lane < ids; v += U * THREADS, k += IDS * THREADS) {
-        uint4 d[U];
-        unsigned int banned[U];
+    // (a gradient over the logits: first the names, then their logits' signs, then the copy)
+    for (int step = BWD && P.over ? 0 : 1; step < 2; ++step) {
+        const int stop = step && (!in_place || masked) ? v1 : v0, ids = step && BWD && P.over ? 0 : n;
+        for (int v = v0 + tid - lane, k = tid; v < stop || k - lane < ids; v += U * THREADS, k += IDS * THREADS) {
+            uint4 d[U];
+            unsigned int banned[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = v + u * THREADS + lane;
-            banned[u] = 0;
-            d[u] = make_uint4(0, 0, 0, 0);
-            if (at >= stop) continue;
-            if (masked) banned[u] = mask.template banned<E>(row.head + at * E);
-            if (banned[u] != (1u << E) - 1 && (!in_place || banned[u])) d[u] = src[at];
-        }
-        if (k - lane < ids) {
-#pragma unroll
-            for (int j = 0; j < IDS; ++j) {
-                const int t = number(id[j]), at = k + j * THREADS;
-                if (t < 0 || at >= n || at < prompt) continue;
-                if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
-                else atomicAdd(counts + t, 1u);
+            for (int u = 0; u < U; ++u) {
+                const int at = v + u * THREADS + lane;
+                banned[u] = 0;
+                d[u] = make_uint4(0, 0, 0, 0);
+                if (at >= stop) continue;
+                if (masked) banned[u] = mask.template banned<E>(row.head + at * E);
+                if (banned[u] != (1u << E) - 1 && (!in_place || banned[u])) d[u] = src[at];
             }
-            get_ids(k + IDS * THREADS, n);
-        }
+            if (k - lane < ids) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = v + u * THREADS + lane;
-            if (v + u * THREADS >= stop) break;
-            if (banned[u]) ban<T, BWD>(d[u], banned[u]);
-            if (!same) store_apart(dst + at * E, d[u], at < stop);
-            else if (at < stop && (!in_place || banned[u])) reinterpret_cast<uint4*>(dst)[at] = d[u];
+                for (int j = 0; j < IDS; ++j) {
+                    const int t = number(id[j]), at = k + j * THREADS;
+                    if (t < 0 || at >= n) continue;
+                    if (COUNTS && at >= prompt) {
+                        if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
+                        else atomicAdd(counts + t, 1u);
+                    }
+                    if (!get_bit(seen, t) && !set_bit(seen, t) && !(n_bias && get_bit(extra, t))) append(t);
+                }
+                __syncwarp();
+                get_ids(k + IDS * THREADS, n);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = v + u * THREADS + lane;
+                if (v + u * THREADS >= stop) break;
+                if (banned[u]) ban<T, BWD>(d[u], banned[u]);
+                if (!same) store_apart(dst + at * E, d[u], at < stop);
+                else if (at < stop && (!in_place || banned[u])) reinterpret_cast<uint4*>(dst)[at] = d[u];
+            }
         }
+        if (step == 1) break;
+        __syncthreads();
+        for (int k = tid; k < static_cast<int>(listed); k += THREADS)
+            if (Elem<T>::get(logits + begin + list[k]) > 0.f) set_bit(extra, list[k]);
+        __syncthreads();
     }
     for (int k = tid; k < row.edges(); k += THREADS) {
         const int t = row.edge(k);
@@ -151,61 +172,41 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         if (!mask.allows(t)) Elem<T>::put(out + t, BWD ? 0.f : NEG_INF);
         else if (!in_place) out[t] = in[t];
     }
-    const float r = P.repetition ? P.repetition[i] : 1.f;
-    const float f = COUNTS && P.frequency ? P.frequency[i] : 0.f, p = COUNTS && P.presence ? P.presence[i] : 0.f;
-    if (COUNTS || n > IDS * THREADS) get_ids(tid, n);
     __syncthreads();
-    const auto claim = [&](int t) {
-        const unsigned int bit = 1u << (t & 31);
-        if (t < 0 || !mask.allows(begin + t) || (*static_cast<volatile unsigned int*>(claimed + (t >> 5)) & bit)) return false;
-        return !(atomicOr(claimed + (t >> 5), bit) & bit);
-    };
-    const auto biased = [&](int t) -> float {
-        if (BWD || !(extra[t >> 5] >> (t & 31) & 1)) return 0.f;
-        float sum = 0.f;
-        for (int e = 0; e < n_bias; ++e)
-            if (bias_ids[e] == t) sum += bias[e];
-        return sum;
-    };
-    for (int k = tid; k < n; k += IDS * THREADS) {
-        int mine[IDS];
-        float x[IDS], g[IDS];
+    const int names = listed;
+    for (int k = tid; k < names; k += NAMES * THREADS) {
+        int token[NAMES];
+        float x[NAMES], g[NAMES];
 #pragma unroll
-        for (int j = 0; j < IDS; ++j) {
-            mine[j] = k + j * THREADS < n ? number(id[j]) : -1;
-            if (!claim(mine[j])) mine[j] = -1;
+        for (int j = 0; j < NAMES; ++j) {
+            const int t = k + j * THREADS < names ? list[k + j * THREADS] : -1;
+            token[j] = t >= 0 && mask.allows(begin + t) ? t : -1;
+            if (token[j] < 0) continue;
+            if (!BWD || !P.over) x[j] = Elem<T>::get(logits + begin + t);
+            if (BWD) g[j] = Elem<T>::get(in + begin + t);
         }
-        if (k + IDS * THREADS < n) get_ids(k + IDS * THREADS, n);
 #pragma unroll
-        for (int j = 0; j < IDS; ++j)
-            if (mine[j] >= 0) {
-                if (!BWD || !P.over) x[j] = Elem<T>::get(logits + begin + mine[j]);
-                if (BWD) g[j] = Elem<T>::get(in + begin + mine[j]);
-            }
-#pragma unroll
-        for (int j = 0; j < IDS; ++j) {
-            const int t = mine[j];
+        for (int j = 0; j < NAMES; ++j) {
+            const int t = token[j];
             if (t < 0) continue;
             float y;
             if constexpr (BWD) {
-                const bool positive = P.over ? extra[t >> 5] >> (t & 31) & 1 : x[j] > 0.f;
-                y = positive ? g[j] / r : g[j] * r;
+                y = (P.over ? get_bit(extra, t) != 0 : x[j] > 0.f) ? g[j] / r : g[j] * r;
             } else {
-                y = x[j] > 0.f ? x[j] / r : x[j] * r;
+                y = x[j];
+                if (get_bit(seen, t)) y = y > 0.f ? y / r : y * r;
                 if (COUNTS) {
                     const unsigned int times = COUNTS == 16 ? counts[t >> 1] >> (t & 1) * 16 & 0xffffu : counts[t];
                     if (times) y = y - f * static_cast<float>(times) - p;
                 }
-                if (n_bias) y += biased(t);
+                if (n_bias && get_bit(extra, t)) {
+                    float sum = 0.f;
+                    for (int e = 0; e < n_bias; ++e)
+                        if (bias_ids[e] == t) sum += bias[e];
+                    y += sum;
+                }
             }
             Elem<T>::put(out + begin + t, y);
-        }
-    }
-    if (!BWD && n_bias) {
-        __syncthreads();
-        for (int k = tid; k < n_bias; k += THREADS) {
-            const int t = bias_ids[k];
-            if (claim(t)) Elem<T>::put(out + begin + t, Elem<T>::get(logits + begin + t) + biased(t));
         }
     }
 }
@@ -242,7 +243,7 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     p.words = (tokens / 32 + 3 + 3) / 4 * 4;
     p.counts = COUNTS ? (tokens / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
-    const size_t smem = 4 * static_cast<size_t>(3 * p.words + p.counts + 2 * p.n_bias);
+    const size_t smem = 4 * static_cast<size_t>(3 * p.words + p.counts + 2 * p.n_bias) + 2 * std::min<long long>(tokens, width + p.n_bias);
     return threads == 256 ? constrain<T, BWD, COUNTS, 256>(p, parts, smem, stream) : constrain<T, BWD, COUNTS, 1024>(p, parts, smem, stream);
 }
 
