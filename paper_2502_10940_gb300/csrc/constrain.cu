@@ -53,11 +53,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
 {
     constexpr int E = Elem<T>::E, U = 4, IDS = 4, NAMES = 4;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
-    // gradient over the logits) of a positive logit; counts; biases; the list
+    // gradient over the logits) of a positive logit, named at all (where there are biases);
+    // counts; biases; the list
     extern __shared__ __align__(16) unsigned int seen[];
     __shared__ unsigned int listed;
     const int n_bias = BWD ? 0 : P.n_bias;
-    unsigned int *words = seen + P.words, *extra = words + P.words, *counts = extra + P.words;
+    unsigned int *words = seen + P.words, *extra = words + P.words, *named = extra + P.words;
+    unsigned int* counts = named + (n_bias ? P.words : 0);
     int* bias_ids = reinterpret_cast<int*>(counts + P.counts);
     float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
     unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias);
@@ -86,7 +88,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const long long which = !P.masks ? -1 : P.mask_of ? P.mask_of[i] : i;
     const float r = P.repetition ? P.repetition[i] : 1.f;
     const float f = COUNTS && P.frequency ? P.frequency[i] : 0.f, p = COUNTS && P.presence ? P.presence[i] : 0.f;
-    for (int k = tid; k < P.words; k += THREADS) seen[k] = extra[k] = 0;
+    for (int k = tid; k < P.words; k += THREADS) {
+        seen[k] = extra[k] = 0;
+        if (n_bias) named[k] = 0;
+    }
     if (COUNTS)
         for (int k = tid * 4; k < P.counts; k += THREADS * 4) *reinterpret_cast<uint4*>(counts + k) = make_uint4(0, 0, 0, 0);
     if (tid == 0) listed = 0;
@@ -111,23 +116,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         at = __shfl_sync(together, at, first) + __popc(together & ((1u << lane) - 1));
         list[at] = static_cast<unsigned short>(t);
     };
-    if (!BWD && n_bias) {
+    if constexpr (!BWD)
         for (int k = tid; k < n_bias; k += THREADS) {
             const int t = number(P.bias_ids[i * n_bias + k]);
             bias_ids[k] = t;
             bias[k] = P.bias[i * n_bias + k];
-            if (t >= 0 && !set_bit(extra, t)) append(t);
+            if (t >= 0 && !set_bit(extra, t) && !set_bit(named, t)) append(t);
         }
-        __syncthreads();
-    }
     const uint4* src = row.vec();
     T* dst = out + row.head;
     // (a gradient over the logits: first the names, then their logits' signs, then the copy)
     for (int step = BWD && P.over ? 0 : 1; step < 2; ++step) {
         const int stop = step && (!in_place || masked) ? v1 : v0, ids = step && BWD && P.over ? 0 : n;
-        for (int v = v0 + tid - lane, k = tid; v < stop || k - lane < ids; v += U * THREADS, k += IDS * THREADS) {
-            uint4 d[U];
-            unsigned int banned[U];
+        int v = v0 + tid - lane;
+        uint4 d[U];
+        unsigned int banned[U];
+        const auto load = [&] {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int at = v + u * THREADS + lane;
@@ -137,20 +141,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
                 if (masked) banned[u] = mask.template banned<E>(row.head + at * E);
                 if (banned[u] != (1u << E) - 1 && (!in_place || banned[u])) d[u] = src[at];
             }
-            if (k - lane < ids) {
-#pragma unroll
-                for (int j = 0; j < IDS; ++j) {
-                    const int t = number(id[j]), at = k + j * THREADS;
-                    if (t < 0 || at >= n) continue;
-                    if (COUNTS && at >= prompt) {
-                        if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
-                        else atomicAdd(counts + t, 1u);
-                    }
-                    if (!get_bit(seen, t) && !set_bit(seen, t) && !(n_bias && get_bit(extra, t))) append(t);
-                }
-                __syncwarp();
-                get_ids(k + IDS * THREADS, n);
-            }
+        };
+        const auto store = [&] {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int at = v + u * THREADS + lane;
@@ -159,6 +151,27 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
                 if (!same) store_apart(dst + at * E, d[u], at < stop);
                 else if (at < stop && (!in_place || banned[u])) reinterpret_cast<uint4*>(dst)[at] = d[u];
             }
+        };
+        for (int k = tid; k - lane < ids; k += IDS * THREADS) {
+            if (v < stop) load();
+#pragma unroll
+            for (int j = 0; j < IDS; ++j) {
+                const int t = number(id[j]), at = k + j * THREADS;
+                if (t < 0 || at >= n) continue;
+                if (COUNTS && at >= prompt) {
+                    if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
+                    else atomicAdd(counts + t, 1u);
+                }
+                if (!get_bit(seen, t) && !set_bit(seen, t) && !(n_bias && set_bit(named, t))) append(t);
+            }
+            __syncwarp();
+            get_ids(k + IDS * THREADS, n);
+            if (v < stop) store();
+            v += U * THREADS;
+        }
+        for (; v < stop; v += U * THREADS) {
+            load();
+            store();
         }
         if (step == 1) break;
         __syncthreads();
@@ -234,16 +247,16 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     constexpr int E = Elem<T>::E, MOST = COUNTS == 32 ? 16384 : 32768;   // tokens of a CTA
     const int full = p.vocab / E;
     const long long width = p.history ? p.history_width : 0;
-    const int threads = width > 4096 ? 1024 : 256;
+    const int threads = width > 4096 || p.n * CLUSTER_MAX <= sms ? 1024 : 256;
     const long long fill = threads == 1024 ? sms / p.n : (FILL * sms + p.n - 1) / p.n;
-    const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads, width / 16));
+    const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads == 1024 ? 64 : 256, width / 16));
     const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + MOST - 1) / MOST), 1ll}));
     p.each = (full + parts - 1) / parts;
     const int tokens = p.each * E + 2 * E;
     p.words = (tokens / 32 + 3 + 3) / 4 * 4;
     p.counts = COUNTS ? (tokens / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
-    const size_t smem = 4 * static_cast<size_t>(3 * p.words + p.counts + 2 * p.n_bias) + 2 * std::min<long long>(tokens, width + p.n_bias);
+    const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) + 2 * std::min<long long>(tokens, width + p.n_bias);
     return threads == 256 ? constrain<T, BWD, COUNTS, 256>(p, parts, smem, stream) : constrain<T, BWD, COUNTS, 1024>(p, parts, smem, stream);
 }
 
