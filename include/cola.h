@@ -416,8 +416,9 @@ cola_status_t cola_constrain_logits_bwd(const cola_vocab_desc_t* desc, const col
  * ids, X_t = scale E[ids_t], and the table's gradient from dX.  (The paper
  * leaves the embedding full-rank.)
  *
- * Conventions as for the layer: E, X, dX and dE 16-byte aligned, row pitches a
- * multiple of 8 elements, whatever the width d; each bf16 or fp32.  ids: int64;
+ * Conventions as for the layer: E, X, dX and dE 16-byte aligned, the row pitches
+ * that a call goes by a multiple of 8 elements, whatever the width d; each bf16
+ * or fp32.  ids: int64;
  * those outside [0, vocab) name no token: their rows of X are 0, their rows of dX
  * are not used.  Limits: vocab and d <= 2^20, n < 2^28. */
 typedef struct {

@@ -1857,11 +1857,13 @@ cola_status_t cola_constrain_logits_bwd(const cola_vocab_desc_t* desc, const col
 namespace cola {
 namespace {
 
+// Row pitches in elements, the default filled in.
 struct EmbedShape {
     int64_t ld_e, ld_x, ld_de;
 };
 
-cola_status_t check_embed(const cola_embed_desc_t* d, EmbedShape* s)
+// e, x, de: the pitches that the call goes by.
+cola_status_t check_embed(const cola_embed_desc_t* d, bool e, bool x, bool de, EmbedShape* s)
 {
     if (!d) return COLA_ERR_INVALID;
     if (d->n < 1 || d->vocab < 1 || d->d < 1 || d->ld_e < 0 || d->ld_x < 0 || d->ld_de < 0 || d->reserved != 0)
@@ -1872,9 +1874,14 @@ cola_status_t check_embed(const cola_embed_desc_t* d, EmbedShape* s)
     if (!std::isfinite(d->scale)) return COLA_ERR_INVALID;
     *s = EmbedShape{d->ld_e ? d->ld_e : d->d, d->ld_x ? d->ld_x : d->d, d->ld_de ? d->ld_de : d->d};
     const int64_t lim = (int64_t(1) << 31) - 256;
-    for (int64_t ld : {s->ld_e, s->ld_x, s->ld_de}) {
-        if (ld < d->d || ld % 8) return COLA_ERR_INVALID;
-        if (ld > lim) return COLA_ERR_UNSUPPORTED;
+    const struct {
+        bool used;
+        int64_t ld;
+    } pitches[3] = {{e, s->ld_e}, {x, s->ld_x}, {de, s->ld_de}};
+    for (const auto& q : pitches) {
+        if (!q.used) continue;
+        if (q.ld < d->d || q.ld % 8) return COLA_ERR_INVALID;
+        if (q.ld > lim) return COLA_ERR_UNSUPPORTED;
     }
     // CTAs of 256 eight-column pieces are numbered in 31 bits
     if (d->vocab > EMBED_VOCAB_MAX || d->d > EMBED_MAX_WIDTH || d->n >= EMBED_MAX_ROWS || d->n * ((d->d + 7) / 8) > lim * 256)
@@ -1890,7 +1897,7 @@ extern "C" {
 cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const int64_t* ids, void* X, void* stream)
 {
     EmbedShape s;
-    COLA_TRY(check_embed(desc, &s));
+    COLA_TRY(check_embed(desc, true, true, false, &s));
     COLA_TRY(check_ptrs({E, X}));
     if (!ids) return COLA_ERR_INVALID;
     if (!aligned_to(ids, 8)) return COLA_ERR_ALIGN;
@@ -1915,7 +1922,7 @@ cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const
 cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* bytes)
 {
     EmbedShape s;
-    COLA_TRY(check_embed(desc, &s));
+    COLA_TRY(check_embed(desc, false, false, false, &s));
     if (!bytes) return COLA_ERR_INVALID;
     int sms = 0;
     COLA_TRY(device_info(&sms));
@@ -1927,7 +1934,7 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
                              size_t ws_bytes, void* stream)
 {
     EmbedShape s;
-    COLA_TRY(check_embed(desc, &s));
+    COLA_TRY(check_embed(desc, false, true, true, &s));
     COLA_TRY(check_ptrs({dX, dE}));
     if (!ids || !ws) return COLA_ERR_INVALID;
     if (!aligned_to(ids, 8) || !aligned_to(ws, WS_ALIGN)) return COLA_ERR_ALIGN;

@@ -51,7 +51,7 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 template <class T, bool BWD, int COUNTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
-    constexpr int E = Elem<T>::E, U = 4, IDS = 4, NAMES = 4;
+    constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
     // gradient over the logits) of a positive logit, named at all (where there are biases);
     // counts; biases; the list
@@ -153,19 +153,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
             }
         };
         for (int k = tid; k - lane < ids; k += IDS * THREADS) {
+            int here[IDS];
+#pragma unroll
+            for (int j = 0; j < IDS; ++j) here[j] = k + j * THREADS < n ? number(id[j]) : -1;
+            get_ids(k + IDS * THREADS, n);
             if (v < stop) load();
 #pragma unroll
             for (int j = 0; j < IDS; ++j) {
-                const int t = number(id[j]), at = k + j * THREADS;
-                if (t < 0 || at >= n) continue;
-                if (COUNTS && at >= prompt) {
+                const int t = here[j];
+                if (t < 0) continue;
+                if (COUNTS && k + j * THREADS >= prompt) {
                     if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
                     else atomicAdd(counts + t, 1u);
                 }
                 if (!get_bit(seen, t) && !set_bit(seen, t) && !(n_bias && set_bit(named, t))) append(t);
             }
             __syncwarp();
-            get_ids(k + IDS * THREADS, n);
             if (v < stop) store();
             v += U * THREADS;
         }

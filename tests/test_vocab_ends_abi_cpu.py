@@ -30,14 +30,25 @@ def test_layouts(L):   # noqa: F811
 
 @pytest.mark.parametrize("name", sorted(EMBED))
 @pytest.mark.parametrize("kw,code", [
-    (dict(n=0), 1), (dict(n=-1), 1), (dict(vocab=0), 1), (dict(d=0), 1), (dict(d=-8), 1), (dict(ld_e=56), 1), (dict(ld_x=-64), 1),
-    (dict(ld_de=68), 1), (dict(d=60), 1), (dict(d=60, ld_e=64, ld_x=64), 1), (dict(scale=float("nan")), 1),
+    (dict(n=0), 1), (dict(n=-1), 1), (dict(vocab=0), 1), (dict(d=0), 1), (dict(d=-8), 1), (dict(ld_e=-64), 1), (dict(ld_x=-64), 1),
+    (dict(ld_de=-64), 1), (dict(scale=float("nan")), 1),
     (dict(scale=float("inf")), 1), (dict(dtype_e="f16"), 1), (dict(dtype_x=7), 1), (dict(dtype_de=-2), 1), (dict(accumulate=True), 1),
-    (dict(vocab=(1 << 20) + 1), 3), (dict(n=1 << 28), 3), (dict(d=(1 << 20) + 8), 3), (dict(ld_x=1 << 31), 3),
-    (dict(n=(1 << 28) - 1, d=1 << 20), 3),
+    (dict(vocab=(1 << 20) + 1), 3), (dict(n=1 << 28), 3), (dict(d=(1 << 20) + 8), 3), (dict(n=(1 << 28) - 1, d=1 << 20), 3),
 ])
 def test_bad_embed_descriptors(L, name, kw, code):   # noqa: F811
     assert _embed(L, name, L.embed_desc(**{**dict(n=4, vocab=100, d=64), **kw}), EMBED[name]) == code
+
+
+# each call goes by the pitches of what it reads and writes
+@pytest.mark.parametrize("name,used", [("cola_embed_fwd", ("ld_e", "ld_x")), ("cola_embed_bwd", ("ld_x", "ld_de"))])
+@pytest.mark.parametrize("d,ld,code", [(64, 56, 1), (64, 68, 1), (60, 0, 1), (60, 60, 1), (60, 56, 1), (64, 1 << 31, 3)])
+def test_embed_pitches(L, name, used, d, ld, code):   # noqa: F811
+    for which in ("ld_e", "ld_x", "ld_de"):
+        kw = dict(ld_e=64, ld_x=64, ld_de=64)
+        kw[which] = ld
+        args = list(EMBED[name])
+        args[0] = FAKE + 4     # what comes next is that the first pointer is misaligned
+        assert _embed(L, name, L.embed_desc(4, 100, d, **kw), args) == (code if which in used else 2), which
 
 
 @pytest.mark.parametrize("name", sorted(EMBED))
@@ -63,7 +74,7 @@ def test_embed_pointers(L):   # noqa: F811
 # the last values that pass (what comes next is that the ids are misaligned) and the first that do not
 @pytest.mark.parametrize("kw,code", [
     (dict(n=(1 << 28) - 1), 2), (dict(n=1 << 28), 3), (dict(vocab=1 << 20), 2), (dict(vocab=(1 << 20) + 1), 3), (dict(d=1 << 20), 2),
-    (dict(ld_e=(1 << 31) - 256), 2), (dict(ld_e=(1 << 31) - 248), 3), (dict(d=61, ld_e=64, ld_x=64, ld_de=72), 2),
+    (dict(ld_x=(1 << 31) - 256), 2), (dict(ld_x=(1 << 31) - 248), 3), (dict(d=61, ld_e=64, ld_x=64, ld_de=72), 2),
     (dict(accumulate=True, dtype_de="f32"), 2),
 ])
 def test_edges_of_the_embed_limits(L, kw, code):   # noqa: F811
