@@ -246,17 +246,15 @@ def _own(s):
             pitch = lambda t: t.stride(0) if t is not None else 0   # noqa: E731
             s["desc"] = cola.embed_desc(case["n"], case["vocab"], case["d"], ld_e=pitch(s["E"]),
                                         ld_x=pitch(s["X"] if kind == "embed" else s["dX"][0]), ld_de=pitch(s["dE"]),
-                                        scale=case["scale"], dtype_e=t_e, dtype_x=t_x, dtype_de=t_e, accumulate=case["micro"] > 0)
+                                        scale=case["scale"], dtype_e=t_e, dtype_x=t_x, dtype_de=t_e)
             s["ws"] = cola.embed_workspace(s["desc"]) if kind == "grad" else None
         if kind == "embed":
             cola.cola_embed_fwd(s["desc"], s["E"], s["ids"], s["X"])
             return {"X": s["X"]}
-        if not case["micro"]:
-            cola.cola_embed_bwd(s["desc"], s["ids"], s["dX"][0], s["dE"], s["ws"])
-            return {"dE": s["dE"]}
-        s["dE"].zero_()
-        for i in range(case["micro"]):
-            cola.cola_embed_bwd(s["desc"], s["ids"][i], s["dX"][i], s["dE"], s["ws"])
+        s["desc"].accumulate = 0   # the first micro-batch overwrites, the others add
+        for ids, dX in zip(s["ids"] if case["micro"] else [s["ids"]], s["dX"]):
+            cola.cola_embed_bwd(s["desc"], ids, dX, s["dE"], s["ws"])
+            s["desc"].accumulate = 1
         return {"dE": s["dE"]}
     if "desc" not in s:
         result = s["out"] if kind == "limit" else s["dlogits"]
