@@ -139,12 +139,16 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const EmbedParams P, co
 template <class TD, bool WHOLE, bool NAMED>
 __device__ __forceinline__ void fill_rows(const EmbedParams& P, int first, int last, int cta, int ctas)
 {
-    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5, step = ctas * warps;
     const float zero[8] = {};
-    for (int v = first + cta * warps + (threadIdx.x >> 5); v < last; v += ctas * warps)
-        if (!NAMED || !(P.present[v >> 5] >> (v & 31) & 1))
-            for (int c = lane * 8; c < P.d; c += 256)
-                Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
+    const auto named = [&](int v) { return NAMED && v < last ? P.present[v >> 5] >> (v & 31) & 1 : 0u; };
+    int v = first + cta * warps + (threadIdx.x >> 5);
+    for (unsigned int skip = named(v), next; v < last; v += step, skip = next) {
+        next = named(v + step);   // (on its way while this row is stored)
+        if (skip) continue;
+        for (int c = lane * 8; c < P.d; c += 256)
+            Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
+    }
 }
 
 // While tokens are sorted, CTAs of the same launches set rows [first, last) to 0, the
@@ -783,7 +787,7 @@ cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
     const Groups g = groups(p.d, COLS<TX>);
     const int per = 256 >> g.shift;
     const int ctas = static_cast<int>((static_cast<long long>(p.chunks) * g.tiles + per - 1) / per);
-    const int fill = std::min(4 * sms, (p.unfilled + 7) / 8);
+    const int fill = std::min(3 * sms, (p.unfilled + 7) / 8);   // (as many as run at once)
     return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, ctas);
 }
 
