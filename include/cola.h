@@ -433,7 +433,8 @@ typedef struct {
     int32_t dtype_x;    /* of X and dX */
     int32_t dtype_de;   /* of dE */
     int32_t accumulate; /* 0: dE is overwritten, rows that no token names with 0;
-                           1: dE (fp32) is added into, rows that no token names are left alone */
+                           1: dE (fp32) is added into (values below the smallest normal
+                              number may count as 0), rows that no token names are left alone */
     int32_t reserved;   /* must be 0 */
 } cola_embed_desc_t;
 
@@ -446,8 +447,9 @@ cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* b
 
 /* dE_v = scale sum of dX_t over the tokens t with ids_t = v, [vocab x d] (ld_de).
  * The tokens are sorted by id, and each row's sum is taken in fp32 in an order
- * that depends on the ids, n, d and the device alone: two calls give the same
- * bits.  A tied table accumulates this onto the output embedding's gradient. */
+ * that depends on the ids, n, d, the type of dX and the device alone: two calls
+ * give the same bits.  A tied table accumulates this onto the output embedding's
+ * gradient.  Columns of dE between d and its pitch are left alone. */
 cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, const void* dX, void* dE, void* ws,
                              size_t ws_bytes, void* stream);
 

@@ -148,7 +148,9 @@ def test_gradient(n, vocab, d, kind, t_x, t_de):
 
 @pytest.mark.parametrize("n,vocab,d,kind", [(40000, 32000, 72, "zipf"), (40000, 300, 40, "same"), (300001, 50021, 16, "zipf"),
                                             (300001, 50021, 9, "rising"), (70000, 1 << 20, 8, "uniform"), (5000, 1 << 20, 8, "zipf"),
-                                            (20000, 700, 2056, "zipf"), (9000, 5, 8192, "uniform")])
+                                            (20000, 700, 2056, "zipf"), (9000, 5, 8192, "uniform"), (8192, 40000, 24, "zipf"),
+                                            (8193, 40000, 24, "zipf"), (2500001, 50021, 8, "zipf"), (2200001, 1000, 8, "same"),
+                                            (3, 70, 200003, "uniform"), (65536, 1 << 20, 8, "same")])
 def test_gradient_of_many(n, vocab, d, kind):
     rng = np.random.default_rng(n)
     backward(tokens(rng, n, vocab, kind), vocab, d, "bf16", "f32")
