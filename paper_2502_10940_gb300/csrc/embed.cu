@@ -798,7 +798,8 @@ constexpr double FILL_BYTES = 24e6;
 Fill take_fill(EmbedParams& p, size_t element, int ctas)
 {
     Fill f = {p.unfilled, p.unfilled, 0};
-    if (ctas > 0) f.first = static_cast<int>(std::max(0.0, p.unfilled - FILL_BYTES / (static_cast<double>(p.d) * element)));
+    if (ctas <= 0) return f;   // (the sort itself has a CTA for every SM)
+    f.first = static_cast<int>(std::max(0.0, p.unfilled - FILL_BYTES / (static_cast<double>(p.d) * element)));
     f.ctas = std::min(ctas, f.last - f.first);
     p.unfilled = f.first;
     return f;
