@@ -26,7 +26,8 @@ struct EmbedParams {
     long long n, ld_src, ld_dst;
     int vocab, d;
     float scale;
-    int accumulate;
+    int accumulate;           // the gradient is added into
+    int stream;               // X is stored past L2
     // the gradient's workspace
     uint2* sorted;            // (id, token)
     unsigned int* count;      // tokens that name a row

@@ -29,11 +29,12 @@ def pitch_of(d, pad):
 
 def rows(x, dtype, pad=False, fill=float("nan")):
     """x on the GPU at a pitch that is a multiple of 8; the view and its buffer,
-    whose other elements are `fill`."""
+    whose other elements are `fill`.  (fp32: on 16-byte boundaries, and padded
+    on no 32-byte ones.)"""
     n, d = x.shape
     ld = pitch_of(d, pad)
     buf = torch.full((n * ld + 16,), fill, dtype=TORCH[dtype], device="cuda")
-    view = torch.as_strided(buf, (n, d), (ld, 1), 8)
+    view = torch.as_strided(buf, (n, d), (ld, 1), 4 if pad and dtype == "f32" else 8)
     view.copy_(torch.as_tensor(x).to("cuda"))
     return view, buf
 
@@ -127,6 +128,14 @@ def test_lookup(n, vocab, d, t_e, t_x):
 
 
 @pytest.mark.parametrize("t_e,t_x", TYPES)
+@pytest.mark.parametrize("pad", [False, True])
+def test_lookup_of_many(pad, t_e, t_x):
+    """An X of 75 to 150 MB, which is stored past L2."""
+    forward(tokens(np.random.default_rng(7), 30011, 901, "zipf"), 901, 1251, t_e, t_x, scale=0.3, pad=pad)
+    forward(tokens(np.random.default_rng(8), 30011, 901, "uniform"), 901, 1248, t_e, t_x, pad=pad)
+
+
+@pytest.mark.parametrize("t_e,t_x", TYPES)
 def test_lookup_copies_what_is_not_finite(t_e, t_x):
     E, _ = rows(np.array([[np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-40, 3.0, 2.0], [1.0] * 8]), t_e)
     X, _ = rows(np.zeros((3, 8)), t_x)
@@ -135,6 +144,12 @@ def test_lookup_copies_what_is_not_finite(t_e, t_x):
     ref = (E.float() * 0.5).to(TORCH[t_x])
     assert torch.equal(torch.nan_to_num(X[:2].float(), nan=7.0), torch.nan_to_num(ref.float(), nan=7.0))
     assert not X[2].any()
+
+
+@pytest.mark.parametrize("t_x,t_de", TYPES)
+@pytest.mark.parametrize("n,vocab,d", [(40, 3000, 64), (500, 20, 136), (9000, 700, 72)])
+def test_gradient_padded(n, vocab, d, t_x, t_de):
+    backward(tokens(np.random.default_rng(n), n, vocab, "zipf"), vocab, d, t_x, t_de, pad=True)
 
 
 @pytest.mark.parametrize("t_x,t_de", TYPES)
