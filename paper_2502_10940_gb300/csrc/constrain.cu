@@ -10,7 +10,6 @@ namespace cola {
 namespace {
 
 constexpr int SMEM_MOST = 200 * 1024;
-constexpr long long FILL = 8;
 
 // A row's mask, the words of the CTA's tokens in shared memory.
 struct Mask {
@@ -46,8 +45,18 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // and goes through the row's history: a bit of shared memory tells of each token whether the
 // history names it, who sets it lists the token, and those behind the prompt are counted
 // (COUNTS: in 16 or 32 bits, where anything depends on it; 0: not).  Then the listed
-// tokens' results are stored over the copies.  Counts do not depend on the order of the
-// atomics, and a token's place in the list does not matter.
+// tokens' results are stored over the copies: every token once, by its list, so that
+// lanes are full and a result may lie over its input.  Counts do not depend on the order of
+// the atomics, and a token's place in the list does not matter.
+//
+// The copy is bound by HBM, alone 79 us for 4096 x 32000 bf16 (524 MB); the rest by latency,
+// a chain of the row's scalars, ids, atomics in shared memory and scattered logits.  With
+// both, us: the gradient of 4096 x 32000 bf16 with histories of 1024 101 (0.92 of the copy
+// rate of what it moves: a logit read for its sign costs 64 bytes), 256 x 128000 bf16 with
+// histories of 4096 39, 32 x 50021 fp32 with 32768 22, 1 x 128000 with 2048 4.8.  Named
+// tokens in hashed slots took 127, 51, 26 and 5.0 there, bits ranked by counting and
+// passed between the CTAs of a cluster 121, 73, 32 and 6.4.  Four vectors a thread at once
+// in a gradient, three in a forward: 101 against 107, 39 against 41.
 template <class T, bool BWD, int COUNTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
@@ -244,22 +253,29 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
     return cudaGetLastError();
 }
 
+// CTAs of a row.  Every CTA of a row reads all of its history, and 16 bits a token (32 for
+// histories of 65536 ids and more) limit what one holds.
+//   - Many rows: CTAs of 256 threads, two times what an SM runs at once (the half and twice
+//     as many took 41 and 58 us for 256 x 128000 instead of 39).
+//   - Few rows, and histories beyond 4096 ids: 1024 threads, an SM each, and a vector for
+//     every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).
 template <class T, bool BWD, int COUNTS>
 cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
 {
     constexpr int E = Elem<T>::E, MOST = COUNTS == 32 ? 16384 : 32768;   // tokens of a CTA
     const int full = p.vocab / E;
     const long long width = p.history ? p.history_width : 0;
-    const int threads = width > 4096 || p.n * CLUSTER_MAX <= sms ? 1024 : 256;
-    const long long fill = threads == 1024 ? sms / p.n : (FILL * sms + p.n - 1) / p.n;
+    const int threads = width > 4096 || 8 * p.n <= sms ? 1024 : 256;
+    const long long fill = threads == 1024 ? sms / p.n : (8ll * sms + p.n - 1) / p.n;
     const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads == 1024 ? 64 : 256, width / 16));
     const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + MOST - 1) / MOST), 1ll}));
     p.each = (full + parts - 1) / parts;
     const int tokens = p.each * E + 2 * E;
-    p.words = (tokens / 32 + 3 + 3) / 4 * 4;
+    p.words = (tokens / 32 + 3 + 3) / 4 * 4;   // (one more than a mask's, which is read in pairs)
     p.counts = COUNTS ? (tokens / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
-    const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) + 2 * std::min<long long>(tokens, width + p.n_bias);
+    const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) +
+                        2 * std::min<long long>(tokens, width + p.n_bias);
     return threads == 256 ? constrain<T, BWD, COUNTS, 256>(p, parts, smem, stream) : constrain<T, BWD, COUNTS, 1024>(p, parts, smem, stream);
 }
 
