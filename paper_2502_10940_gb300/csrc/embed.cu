@@ -590,21 +590,14 @@ __device__ __forceinline__ int last_chunk(const EmbedParams& P, int first, int a
 constexpr int BATCH = 4, BATCHES = 4;
 
 template <class TX, class TD, bool WHOLE>
-__global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, const Groups g, int sum_ctas)
+__global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, const Groups g, int fill_first)
 {
     constexpr int N = COLS<TX>;
     extern __shared__ uint4 ring[];   // [row of the batches][thread]
     grid_dependency_wait();
     grid_launch_dependents();
-    // the CTAs that set rows to 0 lie evenly between the others
-    const int fill_ctas = gridDim.x - sum_ctas, fills = static_cast<int>(static_cast<long long>(blockIdx.x) * fill_ctas / gridDim.x);
-    if (fills != static_cast<int>((blockIdx.x + 1ll) * fill_ctas / gridDim.x)) {
-        fill_rows<TD, WHOLE, true>(P, 0, P.unfilled, fills, fill_ctas);
-        return;
-    }
-    const int at = (blockIdx.x - fills) << (8 - g.shift) | threadIdx.x >> g.shift, chunk = at / g.tiles, tile = at - chunk * g.tiles;
+    const int at = blockIdx.x << (8 - g.shift) | threadIdx.x >> g.shift, chunk = at / g.tiles, tile = at - chunk * g.tiles;
     const int member = threadIdx.x & ((1 << g.shift) - 1), c = (tile << g.shift | member) * N;
-    if (chunk >= P.chunks) return;
     const int lane = threadIdx.x & 31;
     const unsigned int n = static_cast<unsigned int>(P.n), length = P.chunk, begin = static_cast<unsigned int>(chunk) * length;
     const uint2* items = P.sorted;
@@ -615,27 +608,29 @@ __global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, 
     const unsigned int before_chunk = id_at(max(begin, 1u) - 1), head = id_at(begin), two_before = id_at(max(begin, length + 1) - length - 1);
     const unsigned int full_tail = id_at(begin + length - 1), behind = id_at(begin + length), far_behind = id_at(begin + 2 * length);
     uint2 item = items[min(begin + lane, n - 1)];   // a lane holds an item of 32
-    if (begin >= valid) return;
-    const unsigned int end = min(valid, begin + length), tail = end == begin + length ? full_tail : items[end - 1].x;
-    bool open = begin > 0 && before_chunk == head;
-    bool goes_on = end < valid && behind == tail;
-    unsigned int i = begin, stop = end;
-    if (open && (begin == length || two_before != head) && !(goes_on && head == tail)) {
-        i = run_end(items, begin, end, head);   // the chunk before has it all
-        open = false;
-    }
-    if (goes_on && !(open && head == tail)) {
-        if (end + length >= valid || far_behind != tail) {
-            stop = run_end(items, end, min(valid, end + length), tail);
-            goes_on = false;
-        } else if (tile == 0 && member < 32) {
-            const int last = last_chunk(P, chunk, (valid + length - 1) / length, tail);
-            if (lane == 0) P.long_sums[atomicAdd(P.long_count, 1u)] = make_uint4(chunk, last, tail, 0);
+    unsigned int i = begin, stop = begin;
+    bool open = false, goes_on = false;
+    if (chunk < P.chunks && begin < valid) {
+        const unsigned int end = min(valid, begin + length), tail = end == begin + length ? full_tail : items[end - 1].x;
+        open = begin > 0 && before_chunk == head;
+        goes_on = end < valid && behind == tail;
+        stop = end;
+        if (open && (begin == length || two_before != head) && !(goes_on && head == tail)) {
+            i = run_end(items, begin, end, head);   // the chunk before has it all
+            open = false;
+        }
+        if (goes_on && !(open && head == tail)) {
+            if (end + length >= valid || far_behind != tail) {
+                stop = run_end(items, end, min(valid, end + length), tail);
+                goes_on = false;
+            } else if (tile == 0 && member < 32) {
+                const int last = last_chunk(P, chunk, (valid + length - 1) / length, tail);
+                if (lane == 0) P.long_sums[atomicAdd(P.long_count, 1u)] = make_uint4(chunk, last, tail, 0);
+            }
         }
     }
-    if (i >= stop) return;
     const bool mine = c < P.d;
-    const int bytes = min(P.d - c, N) * static_cast<int>(sizeof(TX));
+    const int bytes = max(0, min(P.d - c, N)) * static_cast<int>(sizeof(TX));
     const TX* src = static_cast<const TX*>(P.src) + c;
     const unsigned int ld = static_cast<unsigned int>(P.ld_src);
     const uint32_t slot = smem_u32(ring + threadIdx.x);
@@ -651,8 +646,14 @@ __global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, 
         }
         copy_commit();
     };
+    if (i < stop) {
 #pragma unroll
-    for (int b = 0; b < BATCHES; ++b) fetch(i, item, b);
+        for (int b = 0; b < BATCHES; ++b) fetch(i, item, b);
+    }
+    // rows that no token names, while the first rows come
+    const int fill = static_cast<int>(blockIdx.x) - fill_first;
+    if (fill >= 0) fill_rows<TD, WHOLE, true>(P, 0, P.unfilled, fill, gridDim.x - fill_first);
+    if (i >= stop) return;
     unsigned int cur = __shfl_sync(~0u, item.x, 0);
     Sum<N> sum;
     sum.clear();
@@ -812,8 +813,9 @@ cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
     const Groups g = groups(p.d, COLS<TX>);
     const int per = 256 >> g.shift;
     const int ctas = static_cast<int>((static_cast<long long>(p.chunks) * g.tiles + per - 1) / per);
-    const int fill = std::min(3 * sms, (p.unfilled + 7) / 8);   // (as many as run at once)
-    return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, ctas);
+    // rows of no token: by the CTAs of the sums, or, of fewer than run at once, by others beside them
+    const int fill = ctas < 3 * sms ? std::min(3 * sms, (p.unfilled + 7) / 8) : 0;
+    return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, fill ? ctas : 0);
 }
 
 // What a launch that places tokens sets to 0 beside that: what HBM takes in the 6 us that it
