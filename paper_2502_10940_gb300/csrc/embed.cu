@@ -145,19 +145,26 @@ __global__ void __launch_bounds__(256) embed_rows_kernel(const EmbedParams P, co
 
 // ------------------------------------------------------------- rows of no token
 // Rows [first, last) of the gradient := 0, by the warps of `ctas` CTAs of which this is
-// number `cta`; NAMED: but for those that tokens name.
+// number `cta`, in pieces of up to 2048 columns, alike in width (whole rows on a warp, 8083 of
+// 8099 columns in fp32 took 52 us instead of 47); NAMED: but for those that tokens name.
 template <class TD, bool WHOLE, bool NAMED>
 __device__ __forceinline__ void fill_rows(const EmbedParams& P, int first, int last, int cta, int ctas)
 {
-    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5, step = ctas * warps;
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5, pieces = (P.d + 2047) / 2048;
+    const int width = ((P.d + pieces - 1) / pieces + 255) / 256 * 256;
+    const unsigned int step = ctas * warps, end = static_cast<unsigned int>(last - first) * pieces;
     const float zero[8] = {};
-    const auto named = [&](int v) { return NAMED && v < last ? P.present[v >> 5] >> (v & 31) & 1 : 0u; };
-    int v = first + cta * warps + (threadIdx.x >> 5);
-    for (unsigned int skip = named(v), next; v < last; v += step, skip = next) {
-        next = named(v + step);   // (on its way while this row is stored)
+    const auto named = [&](unsigned int u) {
+        const int v = first + u / pieces;
+        return NAMED && u < end ? P.present[v >> 5] >> (v & 31) & 1 : 0u;
+    };
+    unsigned int u = cta * warps + (threadIdx.x >> 5);
+    for (unsigned int skip = named(u), next; u < end; u += step, skip = next) {
+        next = named(u + step);   // (on its way while this piece is stored)
         if (skip) continue;
-        for (int c = lane * 8; c < P.d; c += 256)
-            Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
+        const unsigned int v = first + u / pieces, from = u % pieces * width, to = min(P.d, static_cast<int>(from) + width);
+        TD* row = static_cast<TD*>(P.dst) + v * P.ld_dst;
+        for (int c = from + lane * 8; c < static_cast<int>(to); c += 256) Eight<TD>::template store<WHOLE>(row + c, zero, P.d - c);
     }
 }
 
