@@ -319,9 +319,17 @@ def cola_topk_distill_step(d, logits, t_ids, t_vals, t_lse, dloss, loss, dlogits
 
 
 def _of(name, t, dtype, dim):
-    if t is not None and (t.dtype != dtype or t.dim() != dim or t.stride(-1) != 1):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name}: {dim} dimension(s) of {dtype} with unit stride along the last, got {t.dtype} of strides {t.stride()}")
+    if dim == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows that overlap, strides {t.stride()}")
     return t
+
+
+def _pitch(t):
+    return t.stride(0) if t.shape[0] > 1 else 0
 
 
 def constraints(history=None, history_len=None, prompt_len=None, *, repetition=None, frequency=None, presence=None, bias_ids=None,
@@ -339,28 +347,38 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     if (bias_ids is None) != (bias is None) or (bias is not None and not (bias_ids.is_contiguous() and bias.is_contiguous()
                                                                            and bias.shape == bias_ids.shape)):
         raise ValueError("bias_ids and bias: both or neither, contiguous, of one shape")
+    rows = {t.shape[0] for name, t in kept.items() if t is not None and name != "masks"}
+    if len(rows) > 1:
+        raise ValueError(f"tensors of {sorted(rows)} rows")
     c = cola_constraints_t()
     for name, t in kept.items():
         setattr(c, name, _ptr(t))
     if history is not None:
-        c.history_width, c.ld_history = history.shape[1], history.stride(0)
+        c.history_width, c.ld_history = history.shape[1], _pitch(history)
     if masks is not None:
-        c.n_masks, c.ld_masks = masks.shape[0], masks.stride(0)
+        c.n_masks, c.ld_masks = masks.shape[0], _pitch(masks)
     c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
-    c.tensors = kept
+    c.tensors, c.rows = kept, rows.pop() if rows else None
     return c
+
+
+def _limits(d, c):
+    rows = getattr(c, "rows", None)
+    if rows is not None and rows != d.n:
+        raise ValueError(f"constraints of {rows} rows for {d.n} rows of logits")
+    return ctypes.byref(c)
 
 
 def cola_constrain_logits_fwd(d, c, logits, out, stream=None):
     """Penalties for tokens that occurred, biases and masks on rows of logits
     (d: vocab_desc, c: constraints); out may be the logits."""
-    _check(lib().cola_constrain_logits_fwd(ctypes.byref(d), ctypes.byref(c), _ptr(logits), _ptr(out), _stream(stream)),
+    _check(lib().cola_constrain_logits_fwd(ctypes.byref(d), _limits(d, c), _ptr(logits), _ptr(out), _stream(stream)),
            "cola_constrain_logits_fwd")
 
 
 def cola_constrain_logits_bwd(d, c, logits, dout, dlogits, stream=None):
     """The gradient at the logits from the one at the constrained logits."""
-    _check(lib().cola_constrain_logits_bwd(ctypes.byref(d), ctypes.byref(c), _ptr(logits), _ptr(dout), _ptr(dlogits),
+    _check(lib().cola_constrain_logits_bwd(ctypes.byref(d), _limits(d, c), _ptr(logits), _ptr(dout), _ptr(dlogits),
                                            _stream(stream)), "cola_constrain_logits_bwd")
 
 

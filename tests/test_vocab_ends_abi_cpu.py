@@ -148,10 +148,17 @@ def test_the_builder_checks_types(L):   # noqa: F811
     ids = torch.zeros((2, 5), dtype=torch.int64)
     for kw in (dict(history=ids.int()), dict(history=ids[0]), dict(history=ids, history_len=torch.zeros(2)),
                dict(history=ids, repetition=torch.ones(2, dtype=torch.float64)), dict(masks=ids), dict(bias_ids=ids, bias=torch.zeros(2, 4)),
-               dict(bias_ids=ids[:, ::2], bias=torch.zeros(2, 3)), dict(history=ids.t()), dict(bias=torch.zeros(2, 5))):
+               dict(bias_ids=ids[:, ::2], bias=torch.zeros(2, 3)), dict(history=ids.t()), dict(bias=torch.zeros(2, 5)),
+               dict(history=ids[:1].expand(3, 5)), dict(masks=torch.zeros((1, 4), dtype=torch.int32).expand(2, 4)),
+               dict(history=ids, repetition=torch.ones(1).expand(2)), dict(history=ids, repetition=torch.ones(3)),
+               dict(history=ids, masks=torch.zeros((3, 4), dtype=torch.int32), mask_of=torch.zeros(3, dtype=torch.int64))):
         with pytest.raises(ValueError):
             L.constraints(**kw)
-    c = L.constraints(ids[:, 1:4], masks=torch.zeros((3, 9), dtype=torch.int32)[:, :4])
+    with pytest.raises(ValueError, match="2 rows for 3"):
+        L.cola_constrain_logits_fwd(L.vocab_desc(3, 10), L.constraints(ids), FAKE, FAKE, stream=0)
+    c = L.constraints(ids[:1].expand(1, 5), masks=torch.zeros((1, 4), dtype=torch.int32)[:, :3])
+    assert (c.history_width, c.ld_history, c.ld_masks) == (5, 0, 0)
+    c = L.constraints(ids[:, 1:4], masks=torch.zeros((3, 9), dtype=torch.int32)[:, :4], mask_of=torch.zeros(2, dtype=torch.int64))
     assert (c.history_width, c.ld_history, c.n_masks, c.ld_masks, c.n_bias) == (3, 5, 3, 9, 0)
 
 
