@@ -43,29 +43,29 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 
 // A CTA has a share of a row's tokens.  In one loop it copies them, masked logits replaced,
 // and goes through the row's history: a bit of shared memory tells of each token whether the
-// history names it, who sets it lists the token, and those behind the prompt are counted
-// (COUNTS: in 16 or 32 bits, where anything depends on it; 0: not).  Then the listed
-// tokens' results are stored over the copies: every token once, by its list, so that
-// lanes are full and a result may lie over its input.  Counts do not depend on the order of
-// the atomics, and a token's place in the list does not matter.
+// history names it, and those behind the prompt are counted (COUNTS: in 16 or 32 bits, where
+// anything depends on it; 0: not).  Who sets a bit lists the token; or, LATE, those with a bit
+// are listed after the loop.  Then the listed tokens' results are stored over the copies:
+// every token once, so that lanes are full and a result may lie over its input.  Counts do
+// not depend on the order of the atomics, and a token's place in the list does not matter.
 //
 // The copy is bound by HBM, alone 79 us for 4096 x 32000 bf16 (524 MB); the rest by latency,
 // a chain of the row's scalars, ids, atomics in shared memory and scattered logits.  With
 // both, us: the gradient of 4096 x 32000 bf16 with histories of 1024 101 (0.92 of the copy
 // rate of what it moves: a logit read for its sign costs 64 bytes), 256 x 128000 bf16 with
-// histories of 4096 39, 32 x 50021 fp32 with 32768 22, 1 x 128000 with 2048 4.8.  Named
+// histories of 4096 39, 32 x 50021 fp32 with 32768 15.6, 1 x 128000 with 2048 4.8.  Named
 // tokens in hashed slots took 127, 51, 26 and 5.0 there, bits ranked by counting and
 // passed between the CTAs of a cluster 121, 73, 32 and 6.4.  Four vectors a thread at once
 // in a gradient, three in a forward: 101 against 107, 39 against 41.
-template <class T, bool BWD, int COUNTS, int THREADS>
+template <class T, bool BWD, int COUNTS, int THREADS, bool LATE>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
     constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
-    // gradient over the logits) of a positive logit, named at all (where there are biases);
-    // counts; biases; the list
+    // gradient over the logits) of a positive logit, listed (where there are biases); counts;
+    // biases; the list
     extern __shared__ __align__(16) unsigned int seen[];
-    __shared__ unsigned int listed;
+    __shared__ int listed, warp_sum[LATE ? THREADS / 32 : 1];
     const int n_bias = BWD ? 0 : P.n_bias;
     unsigned int *words = seen + P.words, *extra = words + P.words, *named = extra + P.words;
     unsigned int* counts = named + (n_bias ? P.words : 0);
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
     unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias);
     const long long i = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T* logits = static_cast<const T*>(P.logits) + i * P.ld;
     const T* in = static_cast<const T*>(P.src) + i * P.ld_src;
     T* out = static_cast<T*>(P.dst) + i * P.ld_dst;
@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const auto set_bit = [](unsigned int* bits, int t) { return atomicOr(bits + (t >> 5), 1u << (t & 31)) >> (t & 31) & 1; };
     const auto append = [&](int t) {   // (one atomic for all that get here together)
         const unsigned int together = __activemask(), first = __ffs(together) - 1;
-        unsigned int at = 0;
-        if (lane == first) at = atomicAdd(&listed, static_cast<unsigned int>(__popc(together)));
+        int at = 0;
+        if (lane == static_cast<int>(first)) at = atomicAdd(&listed, __popc(together));
         at = __shfl_sync(together, at, first) + __popc(together & ((1u << lane) - 1));
         list[at] = static_cast<unsigned short>(t);
     };
@@ -130,13 +130,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
             const int t = number(P.bias_ids[i * n_bias + k]);
             bias_ids[k] = t;
             bias[k] = P.bias[i * n_bias + k];
-            if (t >= 0 && !set_bit(extra, t) && !set_bit(named, t)) append(t);
+            if (t >= 0 && !set_bit(extra, t) && !LATE && !set_bit(named, t)) append(t);
         }
     const uint4* src = row.vec();
     T* dst = out + row.head;
     // (a gradient over the logits: first the names, then their logits' signs, then the copy)
-    for (int step = BWD && P.over ? 0 : 1; step < 2; ++step) {
-        const int stop = step && (!in_place || masked) ? v1 : v0, ids = step && BWD && P.over ? 0 : n;
+    const bool over = BWD && P.over;
+    for (int step = over ? 0 : 1; step < 2; ++step) {
+        const int stop = step && (!in_place || masked) ? v1 : v0, ids = step && over ? 0 : n;
         int v = v0 + tid - lane;
         uint4 d[U];
         unsigned int banned[U];
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
                     if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
                     else atomicAdd(counts + t, 1u);
                 }
-                if (!get_bit(seen, t) && !set_bit(seen, t) && !(n_bias && set_bit(named, t))) append(t);
+                if (!get_bit(seen, t) && !set_bit(seen, t) && !LATE && !(n_bias && set_bit(named, t))) append(t);
             }
             __syncwarp();
             if (v < stop) store();
@@ -187,8 +188,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         }
         if (step == 1) break;
         __syncthreads();
-        for (int k = tid; k < static_cast<int>(listed); k += THREADS)
-            if (Elem<T>::get(logits + begin + list[k]) > 0.f) set_bit(extra, list[k]);
+        for (int k = tid; k < end - begin; k += THREADS)
+            if (get_bit(seen, k) && Elem<T>::get(logits + begin + k) > 0.f) set_bit(extra, k);
         __syncthreads();
     }
     for (int k = tid; k < row.edges(); k += THREADS) {
@@ -198,6 +199,27 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         else if (!in_place) out[t] = in[t];
     }
     __syncthreads();
+    if constexpr (LATE) {
+        // every thread has every THREADS-th word of bits: frequent tokens' ids lie together
+        const int used = (end - begin + 31) / 32;
+        const auto bits_of = [&](int w) { return seen[w] | (over ? 0 : extra[w]); };
+        int sum = 0;
+        for (int w = tid; w < used; w += THREADS) sum += __popc(bits_of(w));
+        int up = sum;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const int v = __shfl_up_sync(~0u, up, k);
+            if (lane >= k) up += v;
+        }
+        if (lane == 31) warp_sum[warp] = up;
+        __syncthreads();
+        const int sums = lane < THREADS / 32 ? warp_sum[lane] : 0, all = __reduce_add_sync(~0u, sums);
+        int at = __reduce_add_sync(~0u, lane < warp ? sums : 0) + up - sum;
+        for (int w = tid; w < used; w += THREADS)
+            for (unsigned int bits = bits_of(w); bits; bits &= bits - 1) list[at++] = static_cast<unsigned short>(w * 32 + __ffs(bits) - 1);
+        if (tid == 0) listed = all;
+        __syncthreads();
+    }
     const int names = listed;
     for (int k = tid; k < names; k += NAMES * THREADS) {
         int token[NAMES];
@@ -207,7 +229,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
             const int t = k + j * THREADS < names ? list[k + j * THREADS] : -1;
             token[j] = t >= 0 && mask.allows(begin + t) ? t : -1;
             if (token[j] < 0) continue;
-            if (!BWD || !P.over) x[j] = Elem<T>::get(logits + begin + t);
+            if (!over) x[j] = Elem<T>::get(logits + begin + t);
             if (BWD) g[j] = Elem<T>::get(in + begin + t);
         }
 #pragma unroll
@@ -216,7 +238,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
             if (t < 0) continue;
             float y;
             if constexpr (BWD) {
-                y = (P.over ? get_bit(extra, t) != 0 : x[j] > 0.f) ? g[j] / r : g[j] * r;
+                y = (over ? get_bit(extra, t) != 0 : x[j] > 0.f) ? g[j] / r : g[j] * r;
             } else {
                 y = x[j];
                 if (get_bit(seen, t)) y = y > 0.f ? y / r : y * r;
@@ -236,10 +258,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     }
 }
 
-template <class T, bool BWD, int COUNTS, int THREADS>
+template <class T, bool BWD, int COUNTS, int THREADS, bool LATE>
 cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStream_t stream)
 {
-    auto kern = constrain_kernel<T, BWD, COUNTS, THREADS>;
+    auto kern = constrain_kernel<T, BWD, COUNTS, THREADS, LATE>;
     static std::atomic<unsigned long long> configured{0};   // bit d: set on device d
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -258,7 +280,10 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
 //   - Many rows: CTAs of 256 threads, two times what an SM runs at once (the half and twice
 //     as many took 41 and 58 us for 256 x 128000 instead of 39).
 //   - Few rows, and histories beyond 4096 ids: 1024 threads, an SM each, and a vector for
-//     every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).
+//     every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).  Of long
+//     histories the list is made after the loop: 15 us against 22 for 32 x 50021 and 32768
+//     ids, but 5.4 against 4.8 for 1 x 128000 and 2048, 114 against 101 for the gradient of
+//     4096 x 32000 and 1024.
 template <class T, bool BWD, int COUNTS>
 cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
 {
@@ -276,7 +301,9 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
     const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) +
                         2 * std::min<long long>(tokens, width + p.n_bias);
-    return threads == 256 ? constrain<T, BWD, COUNTS, 256>(p, parts, smem, stream) : constrain<T, BWD, COUNTS, 1024>(p, parts, smem, stream);
+    if (threads == 256) return constrain<T, BWD, COUNTS, 256, false>(p, parts, smem, stream);
+    return width > 4096 ? constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream)
+                        : constrain<T, BWD, COUNTS, 1024, false>(p, parts, smem, stream);
 }
 
 template <class T>
