@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(256, 3) embed_sum_kernel(const EmbedParams P, 
     constexpr int N = COLS<TX>;
     extern __shared__ uint4 ring[];   // [row of the batches][thread]
     grid_dependency_wait();
-    grid_launch_dependents();
+    if (P.chunks > 1) grid_launch_dependents();   // (embed_join_kernel, which waits)
     const int at = blockIdx.x << (8 - g.shift) | threadIdx.x >> g.shift, chunk = at / g.tiles, tile = at - chunk * g.tiles;
     const int member = threadIdx.x & ((1 << g.shift) - 1), c = (tile << g.shift | member) * N;
     const int lane = threadIdx.x & 31;

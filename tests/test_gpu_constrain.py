@@ -142,7 +142,8 @@ def same_bits(a, b):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,V,width", [(1, 1, 1), (3, 2, 5), (4, 7, 3), (2, 31, 40), (2, 33, 100), (5, 257, 64), (3, 1000, 5000), (2, 4099, 1),
-                                       (2, 33001, 700), (1, 131072, 3000), (2, 200003, 300), (1, 1 << 20, 1000), (700, 100, 20)])
+                                       (2, 33001, 700), (1, 131072, 3000), (2, 200003, 300), (1, 1 << 20, 1000), (700, 100, 20),
+                                       (40, 5003, 300), (25, 40007, 2000), (200, 601, 5000), (2, 3001, 70000)])
 def test_sizes(n, V, width, dtype):
     rng = np.random.default_rng(V + n)
     x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
@@ -209,6 +210,37 @@ def test_histories(dtype):
     c["prompt_len"] = np.array([0, V, 10, 3, 0, 3, width, -9, 2 ** 40])
     run(x, g, c, dtype)
     run(x, g, {k: v for k, v in c.items() if k not in ("history_len", "prompt_len")}, dtype)
+
+
+@pytest.mark.parametrize("width", [65535, 65536, 70001])
+def test_one_token_more_often_than_16_bits_count(width):
+    rng = np.random.default_rng(width)
+    n, V = 2, 501
+    x, g = H.logits(rng, n, V, "f32"), H.rounded(rng.standard_normal((n, V)), "f32")
+    c = limits(rng, n, V, width)
+    c["history"][0], c["history"][1] = 7, 500
+    c["history_len"], c["prompt_len"] = np.full(n, width), np.array([0, 3])
+    run(x, g, c, "f32")
+
+
+@pytest.mark.parametrize("n", [2, 30])
+def test_two_streams_at_once(n):
+    """Two calls that may run together, each with its own rows."""
+    rng = np.random.default_rng(n)
+    V = 30011
+    jobs = []
+    for k in range(2):
+        x, c = H.logits(rng, n, V, "bf16"), limits(rng, n, V, 700, biases=4, masks=3)
+        jobs.append((x, c, on_gpu(c), H.place(x, "bf16"), torch.cuda.Stream()))
+    outs = [torch.empty_like(j[3]) for j in jobs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (x, c, C, X, s), out in zip(jobs, outs):
+            with torch.cuda.stream(s):
+                cola.cola_constrain_logits_fwd(cola.vocab_desc(n, V), C, X, out)
+    torch.cuda.synchronize()
+    for (x, c, C, X, s), out in zip(jobs, outs):
+        check_fwd(x, c, "bf16", H.host(out))
 
 
 @pytest.mark.parametrize("biases", [1, 300, 1024])

@@ -263,6 +263,32 @@ def test_streams_and_graphs():
         assert torch.equal(dE, dE2)
 
 
+def test_two_streams_at_once():
+    """Two gradients that may run together, each with its own workspace, again and
+    again: their launches overlap the ones before and behind them."""
+    rng = np.random.default_rng(12)
+    jobs = []
+    for n, vocab, d in ((5000, 3000, 264), (20000, 9000, 264)):
+        ids = tokens(rng, n, vocab, "zipf")
+        m = cola.embed_desc(n, vocab, d, dtype_de="f32")
+        dX = torch.as_tensor(rng.standard_normal((n, d)), device="cuda").to(torch.bfloat16)
+        jobs.append((m, torch.as_tensor(ids, dtype=torch.int64, device="cuda"), dX, cola.embed_workspace(m),
+                     torch.cuda.Stream(), [torch.full((vocab, d), float("nan"), device="cuda") for _ in range(6)], ids))
+    torch.cuda.synchronize()
+    for i in range(6):
+        for m, I, dX, ws, s, dEs, _ in jobs:
+            with torch.cuda.stream(s):
+                cola.cola_embed_bwd(m, I, dX, dEs[i], ws)
+    torch.cuda.synchronize()
+    for m, I, dX, ws, s, dEs, ids in jobs:
+        assert all(torch.equal(dEs[0], e) for e in dEs[1:])
+        there = (ids >= 0) & (ids < m.vocab)
+        ref, mag, count = np.zeros((m.vocab, m.d)), np.zeros((m.vocab, m.d)), np.bincount(ids[there], minlength=m.vocab)
+        np.add.at(ref, ids[there], host(dX)[there])
+        np.add.at(mag, ids[there], np.abs(host(dX)[there]))
+        assert (np.abs(host(dEs[0]) - ref) <= (count[:, None] + 2) * U * mag).all()
+
+
 def test_traced_launches():
     m = cola.embed_desc(5000, 300, 64)
     I = torch.zeros(5000, dtype=torch.int64, device="cuda")
