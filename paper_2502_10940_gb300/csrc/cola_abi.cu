@@ -1971,6 +1971,9 @@ cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, 
     p.unfilled = p.accumulate ? 0 : p.vocab;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t mnk[1][3] = {{p.n, p.d, p.vocab}};
+    if (p.n <= EMBED_ONE && p.n * p.d * (desc->dtype_x == COLA_DTYPE_BF16 ? 2 : 4) <= EMBED_ONE_BYTES)
+        return launched(traced(COLA_KERNEL_EMBED_SUM, 1, mnk, 1, 0, st,
+                               [&] { return launch_embed_one(p, desc->dtype_x, desc->dtype_de, sms, st); }));
     const bool few = p.n <= EMBED_FEW;
     const int sorts = few ? 1 : p.high ? 4 : 2;
     for (int i = 0; i < sorts; ++i)

@@ -558,6 +558,131 @@ __device__ __forceinline__ void copy_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// ------------------------------------------------------- few tokens in one launch
+// A small gradient in one launch, without the workspace: row v of the table belongs to CTA
+// v % (CTAs), so that frequent tokens, whose ids lie together, are spread.  Every CTA reads
+// all ids and keeps those of its rows, sorts them by counting, adds their rows of dX, and
+// sets its other rows to 0.  Its warps share the sorted tokens in ranges and the columns in
+// tiles; a sum that crosses ranges is added from parts in shared memory.
+// Bound by latency, and by one SM where one token has most rows, whence its limits.
+constexpr int ONE_THREADS = 512, ONE_WARPS = 16, ONE_INDEX = 11;
+static_assert(EMBED_ONE == 1 << ONE_INDEX && EMBED_VOCAB_MAX <= 1 << (32 - ONE_INDEX), "a token's word");
+
+template <class TX, class TD, bool WHOLE>
+__global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParams P, int rows_each)
+{
+    constexpr int N = COLS<TX>, U = 8;
+    extern __shared__ __align__(16) unsigned int one_smem[];
+    __shared__ int kept;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = static_cast<int>(P.n), ctas = gridDim.x, cta = blockIdx.x;
+    unsigned int *list = one_smem, *sorted = list + EMBED_ONE, *bits = sorted + EMBED_ONE;   // (row << ONE_INDEX | token)
+    float* parts = reinterpret_cast<float*>(bits + (rows_each + 127) / 128 * 4);               // [range][open or not][column]
+    for (int i = tid; i < (rows_each + 31) / 32; i += ONE_THREADS) bits[i] = 0;
+    if (tid == 0) kept = 0;
+    unsigned int key[EMBED_ONE / ONE_THREADS];
+#pragma unroll
+    for (int j = 0; j < EMBED_ONE / ONE_THREADS; ++j) {
+        const int i = j * ONE_THREADS + tid;
+        key[j] = i < n ? key_of(P.ids[i], P.vocab) : NO_KEY;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < EMBED_ONE / ONE_THREADS; ++j) {
+        const unsigned int row = key[j] / ctas;
+        if (key[j] == NO_KEY || key[j] - row * ctas != static_cast<unsigned int>(cta)) continue;
+        list[atomicAdd(&kept, 1)] = row << ONE_INDEX | (j * ONE_THREADS + tid);
+        atomicOr(bits + (row >> 5), 1u << (row & 31));
+    }
+    __syncthreads();
+    const int m = kept;
+    if (tid < 4 && m + tid < (m + 3) / 4 * 4) list[m + tid] = NO_KEY;
+    __syncthreads();
+    for (int k = tid; k < m; k += ONE_THREADS) {
+        const unsigned int word = list[k];
+        int before = 0;
+        for (int q = 0; q < m; q += 4) {
+            const uint4 w = *reinterpret_cast<const uint4*>(list + q);
+            before += (w.x < word) + (w.y < word) + (w.z < word) + (w.w < word);
+        }
+        sorted[before] = word;
+    }
+    __syncthreads();
+    if (m > 0) {
+        const int tiles = (P.d + 32 * N - 1) / (32 * N), stride = tiles * 32 * N;
+        const int each = (m + max(1, ONE_WARPS / tiles) - 1) / max(1, ONE_WARPS / tiles), ranges = (m + each - 1) / each;
+        const auto row_at = [&](int i) { return sorted[i] >> ONE_INDEX; };
+        for (int u = warp; u < ranges * tiles; u += ONE_WARPS) {
+            const int range = u / tiles, c = ((u - range * tiles) * 32 + lane) * N, left = P.d - c;
+            const int begin = range * each, end = min(m, begin + each);
+            const TX* src = static_cast<const TX*>(P.src) + c;
+            unsigned int cur = row_at(begin);
+            bool open = begin > 0 && row_at(begin - 1) == cur;
+            const bool goes_on = end < m && row_at(end) == row_at(end - 1);
+            Sum<N> sum;
+            sum.clear();
+            const auto flush = [&](bool part, int after) {
+                if (left <= 0) return;
+                if (part) {
+                    float x[N];
+                    sum.values(x);
+                    store_columns(parts + (range * 2 + after) * stride + c, x, N);
+                } else {
+                    store_sum<TD>(P, cur * ctas + cta, c, sum);
+                }
+            };
+            for (int i = begin; i < end; i += U) {
+                uint4 row[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+                    if (i + k < end && left > 0) {
+                        const TX* at = src + (sorted[i + k] & (EMBED_ONE - 1)) * P.ld_src;
+                        if (WHOLE || left >= N) {
+                            row[k] = *reinterpret_cast<const uint4*>(at);
+                        } else {
+                            float x[N];
+#pragma unroll
+                            for (int e = 0; e < N; ++e) x[e] = e < left ? Elem<TX>::get(at + e) : 0.f;
+                            row[k] = Elem<TX>::pack(x);
+                        }
+                    }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    if (i + k >= end) break;
+                    if (row_at(i + k) != cur) {
+                        flush(open, 0);
+                        cur = row_at(i + k), open = false;
+                        sum.clear();
+                    }
+                    sum.template add<TX>(row[k]);
+                }
+            }
+            flush(open || goes_on, open ? 0 : 1);
+        }
+        __syncthreads();
+        // the sums that cross ranges, by the range that they begin in
+        for (int u = tid; u < (ranges - 1) * P.d; u += ONE_THREADS) {
+            const int range = u / P.d, c = u - range * P.d, begin = range * each, end = begin + each;
+            const unsigned int row = row_at(end);
+            if (row_at(end - 1) != row || (begin > 0 && row_at(begin - 1) == row)) continue;
+            float sum = parts[(range * 2 + 1) * stride + c];
+            for (int k = range + 1; k < ranges && row_at(k * each) == row; ++k) sum += parts[k * 2 * stride + c];
+            TD* p = static_cast<TD*>(P.dst) + (static_cast<long long>(row) * ctas + cta) * P.ld_dst + c;
+            Elem<TD>::put(p, fmaf(P.scale, sum, P.accumulate ? Elem<TD>::get(p) : 0.f));
+        }
+    }
+    if (P.accumulate) return;
+    const int pieces = (P.d + 2047) / 2048, width = ((P.d + pieces - 1) / pieces + 255) / 256 * 256;
+    const float zero[8] = {};
+    for (int u = warp; u < rows_each * pieces; u += ONE_WARPS) {
+        const int row = u / pieces, from = (u - row * pieces) * width, to = min(P.d, from + width);
+        const long long v = static_cast<long long>(row) * ctas + cta;
+        if (v >= P.vocab || (bits[row >> 5] >> (row & 31) & 1)) continue;
+        for (int c = from + lane * 8; c < to; c += 256)
+            Eight<TD>::template store<WHOLE>(static_cast<TD*>(P.dst) + v * P.ld_dst + c, zero, P.d - c);
+    }
+}
+
+// ------------------------------------------------------------- sums of many tokens
 // The first place from `i` on, below `end`, whose id is not `id`; by a whole warp.
 __device__ __forceinline__ unsigned int run_end(const uint2* items, unsigned int i, unsigned int end, unsigned int id)
 {
@@ -825,6 +950,22 @@ cudaError_t sums(const EmbedParams& p, int sms, cudaStream_t stream)
     return launch_behind(embed_sum_kernel<TX, TD, WHOLE>, ctas + fill, 256, smem, stream, p, g, fill ? ctas : 0);
 }
 
+template <class TX, class TD, bool WHOLE>
+cudaError_t one(const EmbedParams& p, int sms, cudaStream_t stream)
+{
+    const int ctas = std::min(2 * sms, p.vocab), rows_each = (p.vocab + ctas - 1) / ctas;
+    constexpr int tile = 32 * COLS<TX>;
+    const int tiles = (p.d + tile - 1) / tile, ranges = std::max(1, ONE_WARPS / tiles);
+    const size_t smem = sizeof(unsigned int) * (2 * EMBED_ONE + (rows_each + 127) / 128 * 4) +
+                        (ranges > 1 ? sizeof(float) * ranges * 2 * tiles * tile : 0);
+    static std::atomic<unsigned long long> configured{0};
+    const cudaError_t e = allow_smem(embed_one_kernel<TX, TD, WHOLE>, sizeof(unsigned int) * (2 * EMBED_ONE + EMBED_VOCAB_MAX / 32 + 4) +
+                                         sizeof(float) * ONE_WARPS * 2 * tile, configured);
+    if (e != cudaSuccess) return e;
+    embed_one_kernel<TX, TD, WHOLE><<<ctas, ONE_THREADS, smem, stream>>>(p, rows_each);
+    return cudaGetLastError();
+}
+
 // What a launch that places tokens sets to 0 beside that: what HBM takes in the 6 us that it
 // runs anyway (a launch that counts is too short to gain from it).
 constexpr double FILL_BYTES = 24e6;
@@ -958,6 +1099,15 @@ cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst
         using TX = decltype(x);
         constexpr bool WHOLE = decltype(whole)::value;
         return dtype_src == 0 ? rows<__nv_bfloat16, TX, WHOLE>(p, sms, stream) : rows<float, TX, WHOLE>(p, sms, stream);
+    });
+}
+
+cudaError_t launch_embed_one(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream)
+{
+    return by_type(dtype_dst, p.d, [&](auto x, auto whole) {
+        using TD = decltype(x);
+        constexpr bool WHOLE = decltype(whole)::value;
+        return dtype_src == 0 ? one<__nv_bfloat16, TD, WHOLE>(p, sms, stream) : one<float, TD, WHOLE>(p, sms, stream);
     });
 }
 

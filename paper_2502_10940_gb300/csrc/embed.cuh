@@ -17,7 +17,9 @@ namespace cola {
 constexpr int EMBED_VOCAB_MAX = 1 << 20;           // rows of a table: two digits of up to ten bits
 constexpr long long EMBED_MAX_ROWS = 1ll << 28;    // tokens of a call stay below it
 constexpr int EMBED_MAX_WIDTH = 1 << 20;
-constexpr int EMBED_FEW = 8192;                    // tokens that are ordered by counting
+constexpr int EMBED_FEW = 8192;                    // tokens that are ordered in one launch
+constexpr int EMBED_ONE = 2048;                    // tokens whose gradient is, of at most so many bytes of dX
+constexpr long long EMBED_ONE_BYTES = 2 << 20;
 
 struct EmbedParams {
     const long long* ids;
@@ -55,6 +57,8 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, si
 
 // dtypes: cola_dtype_t of src and dst
 cudaError_t launch_embed_rows(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
+// The gradient of up to EMBED_ONE tokens of EMBED_ONE_BYTES.
+cudaError_t launch_embed_one(const EmbedParams& p, int dtype_src, int dtype_dst, int sms, cudaStream_t stream);
 // The order of up to EMBED_FEW tokens; that of more, in launches 0 .. 3 (0 and 1 where high
 // is 0).  They also set rows to 0, and lower p.unfilled.
 cudaError_t launch_embed_order(EmbedParams& p, int dtype_dst, int sms, cudaStream_t stream);
