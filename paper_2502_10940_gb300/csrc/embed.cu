@@ -561,12 +561,18 @@ __device__ __forceinline__ void copy_wait()
 // ------------------------------------------------------- few tokens in one launch
 // A small gradient in one launch, without the workspace: row v of the table belongs to CTA
 // v % (CTAs), so that frequent tokens, whose ids lie together, are spread.  Every CTA reads
-// all ids and keeps those of its rows, sorts them by counting, adds their rows of dX, and
-// sets its other rows to 0.  Its warps share the sorted tokens in ranges and the columns in
-// tiles; a sum that crosses ranges is added from parts in shared memory.
-// Bound by latency, and by one SM where one token has most rows, whence its limits.
-constexpr int ONE_THREADS = 512, ONE_WARPS = 16, ONE_INDEX = 11;
+// all ids and keeps those of its rows, sorts them (few by counting the smaller ones, more by
+// a bitonic network, which takes 2,048 of one row from 110 us a call to 52 us), adds their
+// rows of dX, and sets its other rows to 0.  Its warps share the sorted tokens in ranges and
+// the columns in tiles; a sum that crosses ranges is added from parts in shared memory.
+// Bound by latency, and by one SM where one token has most rows, whence the limits.  bf16,
+// table of 32,000: 2,048 tokens of 512 columns 14.3 us, 16.5 us in two launches; if all of
+// them are one token 52 us and 22 us.  Twice the bytes (1,024 columns) would have 18.6 and
+// 90 us here against 20.0 and 28 us: it is left to the two launches.  Four micro-batches of
+// 2,048 x 512 in fp32, one overwriting and three adding: 42 us, 58 us in two launches each.
+constexpr int ONE_THREADS = 512, ONE_WARPS = 16, ONE_INDEX = 11, ONE_RANKED = 256;
 static_assert(EMBED_ONE == 1 << ONE_INDEX && EMBED_VOCAB_MAX <= 1 << (32 - ONE_INDEX), "a token's word");
+static_assert(ONE_RANKED <= ONE_THREADS && ONE_WARPS * 32 == ONE_THREADS, "one word a thread");
 
 template <class TX, class TD, bool WHOLE>
 __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParams P, int rows_each)
@@ -589,24 +595,45 @@ __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParam
 #pragma unroll
     for (int j = 0; j < EMBED_ONE / ONE_THREADS; ++j) {
         const unsigned int row = key[j] / ctas;
-        if (key[j] == NO_KEY || key[j] - row * ctas != static_cast<unsigned int>(cta)) continue;
-        list[atomicAdd(&kept, 1)] = row << ONE_INDEX | (j * ONE_THREADS + tid);
+        const bool keep = key[j] != NO_KEY && key[j] - row * ctas == static_cast<unsigned int>(cta);
+        const unsigned int mask = __ballot_sync(~0u, keep);
+        if (mask == 0) continue;
+        int base = lane == 0 ? atomicAdd(&kept, __popc(mask)) : 0;
+        base = __shfl_sync(~0u, base, 0);
+        if (!keep) continue;
+        list[base + __popc(mask & ((1u << lane) - 1))] = row << ONE_INDEX | (j * ONE_THREADS + tid);
         atomicOr(bits + (row >> 5), 1u << (row & 31));
     }
     __syncthreads();
     const int m = kept;
-    if (tid < 4 && m + tid < (m + 3) / 4 * 4) list[m + tid] = NO_KEY;
-    __syncthreads();
-    for (int k = tid; k < m; k += ONE_THREADS) {
-        const unsigned int word = list[k];
-        int before = 0;
-        for (int q = 0; q < m; q += 4) {
-            const uint4 w = *reinterpret_cast<const uint4*>(list + q);
-            before += (w.x < word) + (w.y < word) + (w.z < word) + (w.w < word);
+    if (m <= ONE_RANKED) {
+        if (tid < 4 && m + tid < (m + 3) / 4 * 4) list[m + tid] = NO_KEY;
+        __syncthreads();
+        if (tid < m) {
+            const unsigned int word = list[tid];
+            int before = 0;
+            for (int q = 0; q < m; q += 4) {
+                const uint4 w = *reinterpret_cast<const uint4*>(list + q);
+                before += (w.x < word) + (w.y < word) + (w.z < word) + (w.w < word);
+            }
+            sorted[before] = word;
         }
-        sorted[before] = word;
+        __syncthreads();
+    } else {
+        const int length = 1 << (32 - __clz(m - 1));
+        for (int i = m + tid; i < length; i += ONE_THREADS) list[i] = NO_KEY;
+        __syncthreads();
+        for (int run = 2; run <= length; run *= 2)
+            for (int apart = run / 2; apart > 0; apart /= 2) {
+                for (int k = tid; k < length / 2; k += ONE_THREADS) {
+                    const int i = 2 * k - (k & (apart - 1)), other = i + apart;
+                    const unsigned int a = list[i], b = list[other];
+                    if ((a > b) == ((i & run) == 0)) list[i] = b, list[other] = a;
+                }
+                __syncthreads();
+            }
+        sorted = list;
     }
-    __syncthreads();
     if (m > 0) {
         const int tiles = (P.d + 32 * N - 1) / (32 * N), stride = tiles * 32 * N;
         const int each = (m + max(1, ONE_WARPS / tiles) - 1) / max(1, ONE_WARPS / tiles), ranges = (m + each - 1) / each;

@@ -171,6 +171,23 @@ def test_gradient_of_many(n, vocab, d, kind):
     backward(tokens(rng, n, vocab, kind), vocab, d, "bf16", "f32")
 
 
+@pytest.mark.parametrize("t_x,t_de", TYPES)
+@pytest.mark.parametrize("n,vocab,d", [(2048, 1000, 64), (2049, 1000, 64), (2048, 700, 512), (2048, 700, 520), (2048, 700, 256), (2047, 2, 33),
+                                       (513, 2, 1030), (256, 1, 40), (257, 1, 40), (1500, 1 << 20, 8), (2, 305, 200001), (100, 304, 4104)])
+@pytest.mark.parametrize("kind", ["zipf", "same"])
+def test_gradient_in_one_launch(n, vocab, d, kind, t_x, t_de):
+    """Where a call is one launch or just no longer: by tokens and by bytes; few
+    and many tokens of a row, rows of one CTA and of all."""
+    rng = np.random.default_rng(n + d)
+    backward(tokens(rng, n, vocab, kind), vocab, d, t_x, t_de, scale=0.75)
+
+
+@pytest.mark.parametrize("kind", ["zipf", "same", "none"])
+@pytest.mark.parametrize("n,vocab,d", [(2048, 500, 64), (600, 3, 1001), (300, 5000, 700), (2048, 500, 513)])
+def test_accumulated_in_one_launch(n, vocab, d, kind):
+    backward(tokens(np.random.default_rng(n), n, vocab, kind), vocab, d, "bf16", "f32", scale=1.5, accumulate=True)
+
+
 @pytest.mark.parametrize("t_x", ["bf16", "f32"])
 @pytest.mark.parametrize("n,vocab,d,kind", [(1, 3, 5, "uniform"), (100, 50, 33, "zipf"), (5000, 700, 136, "same"), (5000, 9000, 136, "zipf"),
                                             (64, 64, 64, "none")])
@@ -300,6 +317,11 @@ def test_traced_launches():
         cola.cola_embed_bwd(m, I, X, E, ws)
     assert [r[0] for r in t.records()] == ["embed", "embed_sort", "embed_sum", "embed_join"]
     assert cola.cola_check_status(ws) == (0, 0)
+    for n, want in ((2048, ["embed_sum"]), (2049, ["embed_sort", "embed_sum", "embed_join"])):
+        m = cola.embed_desc(n, 300, 64)
+        with cola.Trace(8) as t:
+            cola.cola_embed_bwd(m, I[:n], X[:n], E, ws)
+        assert [r[0] for r in t.records()] == want
 
 
 def test_short_workspace():
