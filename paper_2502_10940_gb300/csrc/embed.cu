@@ -566,18 +566,20 @@ __device__ __forceinline__ void copy_wait()
 // rows of dX, and sets its other rows to 0.  Its warps share the sorted tokens in ranges and
 // the columns in tiles; a sum that crosses ranges is added from parts in shared memory.
 // Bound by latency, and by one SM where one token has most rows, whence the limits.  bf16,
-// table of 32,000: 2,048 tokens of 512 columns 14.3 us, 16.5 us in two launches; if all of
-// them are one token 52 us and 22 us.  Twice the bytes (1,024 columns) would have 18.6 and
-// 90 us here against 20.0 and 28 us: it is left to the two launches.  Four micro-batches of
-// 2,048 x 512 in fp32, one overwriting and three adding: 42 us, 58 us in two launches each.
+// table of 32,000: 2,048 tokens of 512 columns 10.6 us, 16.5 us in three launches; if all of
+// them are one token 44 us and 22 us.  Twice the bytes (1,024 columns) would have 14.3 and
+// 76 us here against 20.0 and 28 us: it is left to the three launches.  Four micro-batches of
+// 2,048 x 512 in fp32, one overwriting and three adding: 37 us, 57 us in three launches each.
+// Two CTAs an SM, in 64 registers with six rows on their way per warp: one alone, of the same
+// or twice as many threads, has 12 us with up to 16 rows on their way.
 constexpr int ONE_THREADS = 512, ONE_WARPS = 16, ONE_INDEX = 11, ONE_RANKED = 256;
 static_assert(EMBED_ONE == 1 << ONE_INDEX && EMBED_VOCAB_MAX <= 1 << (32 - ONE_INDEX), "a token's word");
 static_assert(ONE_RANKED <= ONE_THREADS && ONE_WARPS * 32 == ONE_THREADS, "one word a thread");
 
 template <class TX, class TD, bool WHOLE>
-__global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParams P, int rows_each)
+__global__ void __launch_bounds__(ONE_THREADS, 2) embed_one_kernel(const EmbedParams P, int rows_each)
 {
-    constexpr int N = COLS<TX>, U = 8;
+    constexpr int N = COLS<TX>, U = 6;
     extern __shared__ __align__(16) unsigned int one_smem[];
     __shared__ int kept;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = static_cast<int>(P.n), ctas = gridDim.x, cta = blockIdx.x;
@@ -602,7 +604,6 @@ __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParam
         base = __shfl_sync(~0u, base, 0);
         if (!keep) continue;
         list[base + __popc(mask & ((1u << lane) - 1))] = row << ONE_INDEX | (j * ONE_THREADS + tid);
-        atomicOr(bits + (row >> 5), 1u << (row & 31));
     }
     __syncthreads();
     const int m = kept;
@@ -634,6 +635,11 @@ __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParam
             }
         sorted = list;
     }
+    if (!P.accumulate)
+        for (int k = tid; k < m; k += ONE_THREADS) {
+            const unsigned int row = sorted[k] >> ONE_INDEX;
+            if (k == 0 || sorted[k - 1] >> ONE_INDEX != row) atomicOr(bits + (row >> 5), 1u << (row & 31));
+        }
     if (m > 0) {
         const int tiles = (P.d + 32 * N - 1) / (32 * N), stride = tiles * 32 * N;
         const int each = (m + max(1, ONE_WARPS / tiles) - 1) / max(1, ONE_WARPS / tiles), ranges = (m + each - 1) / each;
@@ -672,6 +678,11 @@ __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParam
                             row[k] = Elem<TX>::pack(x);
                         }
                     }
+                if (i + U <= end && row_at(i + U - 1) == cur) {   // (sorted: all of them)
+#pragma unroll
+                    for (int k = 0; k < U; ++k) sum.template add<TX>(row[k]);
+                    continue;
+                }
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
                     if (i + k >= end) break;
@@ -698,6 +709,7 @@ __global__ void __launch_bounds__(ONE_THREADS) embed_one_kernel(const EmbedParam
         }
     }
     if (P.accumulate) return;
+    __syncthreads();   // (the bits)
     const int pieces = (P.d + 2047) / 2048, width = ((P.d + pieces - 1) / pieces + 255) / 256 * 256;
     const float zero[8] = {};
     for (int u = warp; u < rows_each * pieces; u += ONE_WARPS) {
