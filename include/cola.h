@@ -447,8 +447,8 @@ cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* b
 
 /* dE_v = scale sum of dX_t over the tokens t with ids_t = v, [vocab x d] (ld_de).
  * The tokens are sorted by id, and each row's sum is taken in fp32 in an order
- * that depends on the ids, n, d, the type of dX and the device alone: two calls
- * give the same bits.  A tied table accumulates this onto the output embedding's
+ * that depends on the ids, n, vocab, d, the type of dX and the device alone: two
+ * calls give the same bits.  A tied table accumulates this onto the output embedding's
  * gradient.  Columns of dE between d and its pitch are left alone. */
 cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, const void* dX, void* dE, void* ws,
                              size_t ws_bytes, void* stream);
@@ -594,7 +594,8 @@ typedef enum {
     COLA_KERNEL_CONSTRAIN = 13,     /* cola_constrain_logits_*              (M=n, N=vocab, K=history width) */
     COLA_KERNEL_EMBED = 14,         /* cola_embed_fwd                       (M=n, N=d, K=vocab) */
     COLA_KERNEL_EMBED_SORT = 15,    /* cola_embed_bwd: tokens by id         (M=n, N=d, K=vocab) */
-    COLA_KERNEL_EMBED_SUM = 16,     /* cola_embed_bwd: sums within chunks of the sorted tokens (`splits` of them) */
+    COLA_KERNEL_EMBED_SUM = 16,     /* cola_embed_bwd: sums within chunks of the sorted tokens (`splits` of them); of few
+                                       tokens all of it */
     COLA_KERNEL_EMBED_JOIN = 17     /* cola_embed_bwd: sums that cross chunks */
 } cola_kernel_t;
 
