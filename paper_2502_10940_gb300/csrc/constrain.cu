@@ -45,7 +45,7 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // and goes through the row's history: a bit of shared memory tells of each token whether the
 // history names it, and those behind the prompt are counted (COUNTS: in 16 or 32 bits, where
 // anything depends on it; 0: not).  Who sets a bit lists the token; or, LATE, those with a bit
-// are listed after the loop.  Then the listed tokens' results are stored over the copies:
+// are listed after the loop, and on 256 threads counted by their place in the list.  Then the listed tokens' results are stored over the copies:
 // every token once, so that lanes are full and a result may lie over its input.  Counts do
 // not depend on the order of the atomics, and a token's place in the list does not matter.
 //
@@ -53,14 +53,15 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // a chain of the row's scalars, ids, atomics in shared memory and scattered logits.  With
 // both, us: the gradient of 4096 x 32000 bf16 with histories of 1024 101 (0.92 of the copy
 // rate of what it moves: a logit read for its sign costs 64 bytes), 256 x 128000 bf16 with
-// histories of 4096 39, 32 x 50021 fp32 with 32768 15.6, 1 x 128000 with 2048 4.8.  Named
+// histories of 4096 36, 32 x 50021 fp32 with 32768 15.6, 1 x 128000 with 2048 4.8.  Named
 // tokens in hashed slots took 127, 51, 26 and 5.0 there, bits ranked by counting and
 // passed between the CTAs of a cluster 121, 73, 32 and 6.4.  Four vectors a thread at once
-// in a gradient, three in a forward: 101 against 107, 39 against 41.
+// in a gradient, three in a forward: 101 against 107, 36.1 against 36.8.
 template <class T, bool BWD, int COUNTS, int THREADS, bool LATE>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
     constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4;
+    constexpr bool RANKED = COUNTS && LATE && THREADS == 256;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
     // gradient over the logits) of a positive logit, listed (where there are biases); counts;
     // biases; the list
@@ -72,6 +73,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     int* bias_ids = reinterpret_cast<int*>(counts + P.counts);
     float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
     unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias);
+    unsigned short* base = list + P.list;
     const long long i = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T* logits = static_cast<const T*>(P.logits) + i * P.ld;
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
             for (int j = 0; j < IDS; ++j) {
                 const int t = here[j];
                 if (t < 0) continue;
-                if (COUNTS && k + j * THREADS >= prompt) {
+                if (COUNTS && !RANKED && k + j * THREADS >= prompt) {
                     if (COUNTS == 16) atomicAdd(counts + (t >> 1), 1u << (t & 1) * 16);
                     else atomicAdd(counts + t, 1u);
                 }
@@ -215,10 +217,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         __syncthreads();
         const int sums = lane < THREADS / 32 ? warp_sum[lane] : 0, all = __reduce_add_sync(~0u, sums);
         int at = __reduce_add_sync(~0u, lane < warp ? sums : 0) + up - sum;
-        for (int w = tid; w < used; w += THREADS)
+        for (int w = tid; w < used; w += THREADS) {
+            if (RANKED) base[w] = static_cast<unsigned short>(at);
             for (unsigned int bits = bits_of(w); bits; bits &= bits - 1) list[at++] = static_cast<unsigned short>(w * 32 + __ffs(bits) - 1);
+        }
         if (tid == 0) listed = all;
         __syncthreads();
+        if constexpr (RANKED) {
+            constexpr int MORE = 8;
+            for (int k = tid; k < n; k += MORE * THREADS) {
+                long long again[MORE];
+#pragma unroll
+                for (int j = 0; j < MORE; ++j) again[j] = k + j * THREADS < n && k + j * THREADS >= prompt ? h[k + j * THREADS] : -1;
+#pragma unroll
+                for (int j = 0; j < MORE; ++j) {
+                    const int t = number(again[j]);
+                    if (t < 0) continue;
+                    const int at = base[t >> 5] + __popc(bits_of(t >> 5) & ((1u << (t & 31)) - 1));
+                    atomicAdd(counts + (at >> 1), 1u << (at & 1) * 16);
+                }
+            }
+            __syncthreads();
+        }
     }
     const int names = listed;
     for (int k = tid; k < names; k += NAMES * THREADS) {
@@ -243,7 +263,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
                 y = x[j];
                 if (get_bit(seen, t)) y = y > 0.f ? y / r : y * r;
                 if (COUNTS) {
-                    const unsigned int times = COUNTS == 16 ? counts[t >> 1] >> (t & 1) * 16 & 0xffffu : counts[t];
+                    const int c = RANKED ? k + j * THREADS : t;
+                    const unsigned int times = COUNTS == 16 ? counts[c >> 1] >> (c & 1) * 16 & 0xffffu : counts[c];
                     if (times) y = y - f * static_cast<float>(times) - p;
                 }
                 if (n_bias && get_bit(extra, t)) {
@@ -275,15 +296,21 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
     return cudaGetLastError();
 }
 
-// CTAs of a row.  Every CTA of a row reads all of its history, and 16 bits a token (32 for
-// histories of 65536 ids and more) limit what one holds.
-//   - Many rows: CTAs of 256 threads, two times what an SM runs at once (the half and twice
-//     as many took 41 and 58 us for 256 x 128000 instead of 39).
+// CTAs of a row.  Every CTA of a row reads all of its history, and its bits, list and counts
+// limit what one holds.
+//   - Many rows: CTAs of 256 threads, as many as run at once, four an SM (with counts, bf16,
+//     histories of 4096: 64 x 128000 13.9 us, twice as many 19.6, 256 x 50021 fp32 26.4 and
+//     29.4).  Without counts, where rows leave no more than one each, two times as many: the
+//     gradient of 509 x 50021 fp32 51 us against 53; of 256 x 128000 bf16 30 against 34.
 //   - Few rows, and histories beyond 4096 ids: 1024 threads, an SM each, and a vector for
 //     every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).  Of long
 //     histories the list is made after the loop: 15 us against 22 for 32 x 50021 and 32768
 //     ids, but 5.4 against 4.8 for 1 x 128000 and 2048, 114 against 101 for the gradient of
 //     4096 x 32000 and 1024.
+// Counts on 256 threads are one per listed token, on 1024 one per token: the list's places
+// are known after the loop alone, and finding them reads the history again (32768 ids too
+// many for few CTAs), but 16 bits a token leave room for three CTAs an SM: 64 x 128000 18
+// us against 14, 256 x 128000 39.6 against 36, 512 x 128000 87 against 71.
 template <class T, bool BWD, int COUNTS>
 cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
 {
@@ -291,19 +318,26 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     const int full = p.vocab / E;
     const long long width = p.history ? p.history_width : 0;
     const int threads = width > 4096 || 8 * p.n <= sms ? 1024 : 256;
-    const long long fill = threads == 1024 ? sms / p.n : (8ll * sms + p.n - 1) / p.n;
+    const long long wave = 4ll * sms / p.n;
+    const long long fill = threads == 1024 ? sms / p.n : COUNTS || wave > 1 ? wave : (8ll * sms + p.n - 1) / p.n;
     const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads == 1024 ? 64 : 256, width / 16));
     const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + MOST - 1) / MOST), 1ll}));
     p.each = (full + parts - 1) / parts;
     const int tokens = p.each * E + 2 * E;
     p.words = (tokens / 32 + 3 + 3) / 4 * 4;   // (one more than a mask's, which is read in pairs)
-    p.counts = COUNTS ? (tokens / (32 / COUNTS) + 4) / 4 * 4 : 0;
+    p.list = static_cast<int>(std::min<long long>(tokens, width + p.n_bias));
+    const bool ranked = COUNTS && threads == 256;
+    p.counts = COUNTS ? ((ranked ? p.list : tokens) / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
     const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) +
-                        2 * std::min<long long>(tokens, width + p.n_bias);
-    if (threads == 256) return constrain<T, BWD, COUNTS, 256, false>(p, parts, smem, stream);
-    return width > 4096 ? constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream)
-                        : constrain<T, BWD, COUNTS, 1024, false>(p, parts, smem, stream);
+                        2 * static_cast<size_t>(p.list + (ranked ? p.words : 0));
+    if constexpr (COUNTS == 32) {   // (histories of 65536 ids and more)
+        return constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream);
+    } else {
+        if (threads == 256) return constrain<T, BWD, COUNTS, 256, COUNTS != 0>(p, parts, smem, stream);
+        return width > 4096 ? constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream)
+                            : constrain<T, BWD, COUNTS, 1024, false>(p, parts, smem, stream);
+    }
 }
 
 template <class T>

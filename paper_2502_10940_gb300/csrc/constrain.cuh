@@ -14,7 +14,7 @@
 namespace cola {
 
 constexpr int BIAS_MAX = 1024;                          // entries of a row
-constexpr long long HISTORY_MAX = (1ll << 28) - 1;      // tokens of a row (flags lie above its counts)
+constexpr long long HISTORY_MAX = (1ll << 28) - 1;      // ids of a row
 
 struct ConstrainParams {
     const void* logits;
@@ -24,6 +24,7 @@ struct ConstrainParams {
     int vocab;
     int each;                 // 16-byte vectors of a row per CTA (the grid's y)
     int words, counts;        // of a CTA's tokens: words of a bit each, words of counts
+    int list;                 // tokens that a CTA may list
     int over;                 // the gradient lies over the logits
     const long long* history;
     long long history_width, ld_history;

@@ -212,6 +212,24 @@ def test_histories(dtype):
     run(x, g, {k: v for k, v in c.items() if k not in ("history_len", "prompt_len")}, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,width,layout", [(19, 5003, 4096, "dense"), (20, 5003, 4096, "dense"), (20, 5003, 4097, "dense"),
+                                              (24, 70001, 4096, "padded"), (21, 33000, 1, "shifted"), (77, 501, 4096, "odd"),
+                                              (304, 1003, 33, "dense"), (305, 1003, 33, "dense"), (609, 37, 300, "shifted")])
+def test_many_rows(n, V, width, layout, dtype):
+    """Rows on 256 threads, whose counts go by the tokens' places in the list: one
+    token over and over, every token once, nothing behind the prompt."""
+    rng = np.random.default_rng(n + V)
+    x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
+    c = limits(rng, n, V, width, biases=5, masks=3)
+    c["history"][0], c["history"][1] = V - 1, np.arange(width) % V
+    c["history"][2] = V - 1 - np.arange(width) % V
+    c["history_len"][:4] = width
+    c["prompt_len"][:4] = [0, 0, 1, width]
+    run(x, g, c, dtype, layout)
+    run(x, g, {k: v for k, v in c.items() if not k.startswith("bias") and k != "repetition"}, dtype, layout)
+
+
 @pytest.mark.parametrize("width", [65535, 65536, 70001])
 def test_one_token_more_often_than_16_bits_count(width):
     rng = np.random.default_rng(width)
