@@ -45,7 +45,7 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // and goes through the row's history: a bit of shared memory tells of each token whether the
 // history names it, and those behind the prompt are counted (COUNTS: in 16 or 32 bits, where
 // anything depends on it; 0: not).  Who sets a bit lists the token; or, LATE, those with a bit
-// are listed after the loop, and on 256 threads counted by their place in the list.  Then the listed tokens' results are stored over the copies:
+// are listed after the loop, and on fewer than 1024 threads counted by their place there.  Then the listed tokens' results are stored over the copies:
 // every token once, so that lanes are full and a result may lie over its input.  Counts do
 // not depend on the order of the atomics, and a token's place in the list does not matter.
 //
@@ -61,7 +61,7 @@ template <class T, bool BWD, int COUNTS, int THREADS, bool LATE>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
     constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4;
-    constexpr bool RANKED = COUNTS && LATE && THREADS == 256;
+    constexpr bool RANKED = COUNTS && LATE && THREADS < 1024;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
     // gradient over the logits) of a positive logit, listed (where there are biases); counts;
     // biases; the list
@@ -302,31 +302,38 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
 //     histories of 4096: 64 x 128000 13.9 us, twice as many 19.6, 256 x 50021 fp32 26.4 and
 //     29.4).  Without counts, where rows leave no more than one each, two times as many: the
 //     gradient of 509 x 50021 fp32 51 us against 53; of 256 x 128000 bf16 30 against 34.
-//   - Few rows, and histories beyond 4096 ids: 1024 threads, an SM each, and a vector for
-//     every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).  Of long
-//     histories the list is made after the loop: 15 us against 22 for 32 x 50021 and 32768
+//   - Many rows of longer histories, with counts up to 16384: 512 threads, two an SM, of up
+//     to 65024 tokens (histories of 8192: 256 x 128000 bf16 41 us against 55 on 1024 threads,
+//     its gradient 38 against 54; 64 rows 15.4 against 15.9, 32 rows 13.4 against 10.6; 16384:
+//     256 rows 58 against 65; 32768: 51 against 49 for 128 rows, but gradients of 512 x 32000
+//     59 against 63).
+//   - Few rows, and other histories beyond 4096 ids: 1024 threads, an SM each, and a vector
+//     for every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).  Of
+//     long histories the list is made after the loop: 15 us against 22 for 32 x 50021 and 32768
 //     ids, but 5.4 against 4.8 for 1 x 128000 and 2048, 114 against 101 for the gradient of
 //     4096 x 32000 and 1024.
-// Counts on 256 threads are one per listed token, on 1024 one per token: the list's places
-// are known after the loop alone, and finding them reads the history again (32768 ids too
-// many for few CTAs), but 16 bits a token leave room for three CTAs an SM: 64 x 128000 18
-// us against 14, 256 x 128000 39.6 against 36, 512 x 128000 87 against 71.
+// Counts on fewer than 1024 threads are one per listed token, on 1024 one per token: the
+// list's places are known after the loop alone, and finding them reads the history again
+// (32768 ids too many for few CTAs), but 16 bits a token leave room for three CTAs an SM: 64
+// x 128000 18 us against 14, 256 x 128000 39.6 against 36, 512 x 128000 87 against 71.
 template <class T, bool BWD, int COUNTS>
 cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
 {
-    constexpr int E = Elem<T>::E, MOST = COUNTS == 32 ? 16384 : 32768;   // tokens of a CTA
+    constexpr int E = Elem<T>::E;
     const int full = p.vocab / E;
     const long long width = p.history ? p.history_width : 0;
-    const int threads = width > 4096 || 8 * p.n <= sms ? 1024 : 256;
-    const long long wave = 4ll * sms / p.n;
-    const long long fill = threads == 1024 ? sms / p.n : COUNTS || wave > 1 ? wave : (8ll * sms + p.n - 1) / p.n;
+    const bool many = 2 * p.n > sms && (!COUNTS || width <= 16384);
+    const int threads = 8 * p.n <= sms ? 1024 : width <= 4096 ? 256 : many ? 512 : 1024;
+    const int most = COUNTS == 32 ? 16384 : threads == 512 ? 65024 : 32768;   // tokens of a CTA (their numbers have 16 bits)
+    const long long once = 1024 / threads * static_cast<long long>(sms) / p.n;   // CTAs of a row, of those that run at once
+    const long long fill = threads > 256 || COUNTS || once > 1 ? once : (8ll * sms + p.n - 1) / p.n;
     const long long wanted = std::min<long long>(fill, full / std::max<long long>(threads == 1024 ? 64 : 256, width / 16));
-    const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + MOST - 1) / MOST), 1ll}));
+    const int parts = static_cast<int>(std::max({wanted, static_cast<long long>((p.vocab + most - 1) / most), 1ll}));
     p.each = (full + parts - 1) / parts;
     const int tokens = p.each * E + 2 * E;
     p.words = (tokens / 32 + 3 + 3) / 4 * 4;   // (one more than a mask's, which is read in pairs)
     p.list = static_cast<int>(std::min<long long>(tokens, width + p.n_bias));
-    const bool ranked = COUNTS && threads == 256;
+    const bool ranked = COUNTS && threads < 1024;
     p.counts = COUNTS ? ((ranked ? p.list : tokens) / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
     const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) +
@@ -334,6 +341,7 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     if constexpr (COUNTS == 32) {   // (histories of 65536 ids and more)
         return constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream);
     } else {
+        if (threads == 512) return constrain<T, BWD, COUNTS, 512, true>(p, parts, smem, stream);
         if (threads == 256) return constrain<T, BWD, COUNTS, 256, COUNTS != 0>(p, parts, smem, stream);
         return width > 4096 ? constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream)
                             : constrain<T, BWD, COUNTS, 1024, false>(p, parts, smem, stream);

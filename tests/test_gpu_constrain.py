@@ -215,9 +215,11 @@ def test_histories(dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,V,width,layout", [(19, 5003, 4096, "dense"), (20, 5003, 4096, "dense"), (20, 5003, 4097, "dense"),
                                               (24, 70001, 4096, "padded"), (21, 33000, 1, "shifted"), (77, 501, 4096, "odd"),
-                                              (304, 1003, 33, "dense"), (305, 1003, 33, "dense"), (609, 37, 300, "shifted")])
+                                              (304, 1003, 33, "dense"), (305, 1003, 33, "dense"), (609, 37, 300, "shifted"),
+                                              (77, 66001, 4097, "shifted"), (77, 2003, 16384, "dense"), (77, 2003, 16385, "odd"),
+                                              (76, 2003, 5000, "dense"), (400, 37, 5000, "padded")])
 def test_many_rows(n, V, width, layout, dtype):
-    """Rows on 256 threads, whose counts go by the tokens' places in the list: one
+    """Rows on 256 and 512 threads, whose counts go by the tokens' places in the list: one
     token over and over, every token once, nothing behind the prompt."""
     rng = np.random.default_rng(n + V)
     x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
