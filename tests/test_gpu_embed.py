@@ -244,11 +244,12 @@ def test_gradient_against_differences():
         E[v, c] -= 2.0
 
 
-def test_streams_and_graphs():
+@pytest.mark.parametrize("n", [700, 3000, 9000])
+def test_streams_and_graphs(n):
     """On another stream, and captured and replayed with other tokens, which
     leave other rows without any; two captured graphs share a workspace."""
     rng = np.random.default_rng(1)
-    n, vocab, d = 3000, 5000, 136
+    vocab, d = 5000, 136
     m = cola.embed_desc(n, vocab, d, dtype_de="f32")
     ws = cola.embed_workspace(m)
     I = torch.zeros(n, dtype=torch.int64, device="cuda")
