@@ -53,7 +53,7 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // a chain of the row's scalars, ids, atomics in shared memory and scattered logits.  With
 // both, us: the gradient of 4096 x 32000 bf16 with histories of 1024 101 (0.92 of the copy
 // rate of what it moves: a logit read for its sign costs 64 bytes), 256 x 128000 bf16 with
-// histories of 4096 36, 32 x 50021 fp32 with 32768 15.6, 1 x 128000 with 2048 4.8.  Named
+// histories of 4096 35, 32 x 50021 fp32 with 32768 16.2, 1 x 128000 with 2048 5.0.  Named
 // tokens in hashed slots took 127, 51, 26 and 5.0 there, bits ranked by counting and
 // passed between the CTAs of a cluster 121, 73, 32 and 6.4.  Four vectors a thread at once
 // in a gradient, three in a forward: 101 against 107, 36.1 against 36.8.
@@ -280,8 +280,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     if constexpr (BWD) return;
     // The biased tokens, each by the first of its entries; only one that has several looks
     // through all.  (As every listed token with a bias did, 300 biases took 57 us instead of
-    // 39 for 256 x 128000 with histories of 4096, 47 instead of 36 for 64 rows with 1000; 20
-    // of one row 4.6 instead of 4.9.)
+    // 39 for 256 x 128000 with histories of 4096, 47 instead of 36 for 64 rows with 1000; but
+    // 20 of one row 4.6 instead of 4.9, and 300 of 3983 x 1624, where many are named again, 90
+    // instead of 107.)
     for (int k = k0; k < n_bias; k += THREADS) {
         const int t = biased(k);
         if (t < 0) continue;
