@@ -53,26 +53,26 @@ __device__ __forceinline__ void ban(uint4& v, unsigned int banned)
 // a chain of the row's scalars, ids, atomics in shared memory and scattered logits.  With
 // both, us: the gradient of 4096 x 32000 bf16 with histories of 1024 101 (0.92 of the copy
 // rate of what it moves: a logit read for its sign costs 64 bytes), 256 x 128000 bf16 with
-// histories of 4096 35, 32 x 50021 fp32 with 32768 16.2, 1 x 128000 with 2048 5.0.  Named
+// histories of 4096 35, 32 x 50021 fp32 with 32768 16.0, 1 x 128000 with 2048 4.8.  Named
 // tokens in hashed slots took 127, 51, 26 and 5.0 there, bits ranked by counting and
 // passed between the CTAs of a cluster 121, 73, 32 and 6.4.  Four vectors a thread at once
 // in a gradient, three in a forward: 101 against 107, 36.1 against 36.8.
 template <class T, bool BWD, int COUNTS, int THREADS, bool LATE>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(const ConstrainParams P)
 {
-    constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4;
+    constexpr int E = Elem<T>::E, U = BWD ? 4 : 3, IDS = 4, NAMES = 4, LOOKS = 4;
     constexpr bool RANKED = COUNTS && LATE && THREADS < 1024;
     // bits of the share's tokens (P.words each): named by the history, masked, biased or (a
     // gradient over the logits) of a positive logit, biased more than once; counts; biases;
     // the list
     extern __shared__ __align__(16) unsigned int seen[];
     __shared__ int listed, warp_sum[LATE ? THREADS / 32 : 1];
-    const int n_bias = BWD ? 0 : P.n_bias, n_bias4 = (n_bias + 3) / 4 * 4;
+    const int n_bias = BWD ? 0 : P.n_bias;
     unsigned int *words = seen + P.words, *extra = words + P.words, *again = extra + P.words;
     unsigned int* counts = again + (n_bias ? P.words : 0);
     int* bias_ids = reinterpret_cast<int*>(counts + P.counts);
-    float* bias = reinterpret_cast<float*>(bias_ids + n_bias4);
-    unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias4);
+    float* bias = reinterpret_cast<float*>(bias_ids + n_bias);
+    unsigned short* list = reinterpret_cast<unsigned short*>(bias + n_bias);
     unsigned short* base = list + P.list;
     const long long i = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -128,10 +128,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         list[at] = static_cast<unsigned short>(t);
     };
     if constexpr (!BWD)
-        for (int k = tid; k < n_bias4; k += THREADS) {
-            const int t = k < n_bias ? number(P.bias_ids[i * n_bias + k]) : -1;
+        for (int k = tid; k < n_bias; k += THREADS) {
+            const int t = number(P.bias_ids[i * n_bias + k]);
             bias_ids[k] = t;
-            bias[k] = k < n_bias ? P.bias[i * n_bias + k] : 0.f;
+            bias[k] = P.bias[i * n_bias + k];
             if (t >= 0 && set_bit(extra, t)) set_bit(again, t);
         }
     const auto place = [&](int t) { return base[t >> 5] + __popc(seen[t >> 5] & ((1u << (t & 31)) - 1)); };   // (RANKED)
@@ -252,9 +252,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
     const int names = listed;
     // (a thread's first biased token, its logit on its way with the listed ones; few of each
     // are on different warps)
-    const int k0 = THREADS - 1 - tid;
+    const int k0 = THREADS - 32 - warp * 32;
     const auto biased = [&](int k) { return k < n_bias && bias_ids[k] >= 0 && mask.allows(begin + bias_ids[k]) ? bias_ids[k] : -1; };
-    const int t0 = biased(k0);
+    const int t0 = biased(k0 + lane);
     const float x0 = t0 >= 0 ? Elem<T>::get(logits + begin + t0) : 0.f;
     for (int k = tid; k < names; k += NAMES * THREADS) {
         int token[NAMES];
@@ -278,29 +278,53 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) constrain_kernel(cons
         }
     }
     if constexpr (BWD) return;
-    // The biased tokens, each by the first of its entries; only one that has several looks
-    // through all.  (As every listed token with a bias did, 300 biases took 57 us instead of
-    // 39 for 256 x 128000 with histories of 4096, 47 instead of 36 for 64 rows with 1000; but
-    // 20 of one row 4.6 instead of 4.9, and 300 of 3983 x 1624, where many are named again, 90
-    // instead of 107.)
+    // The biased tokens, each by the first of its entries; for each of few that have several a
+    // warp looks through all, of many (small vocabularies) every thread for its own.  20 of one
+    // row 4.8 us, 300 of 256 x 128000 with histories of 4096 39 (57 where every listed token
+    // looked for its bias), 1000 of 64 rows 17 (every thread for its own: 36), 300 of 25 x 386
+    // 13 (by warps: 40).
     for (int k = k0; k < n_bias; k += THREADS) {
-        const int t = biased(k);
-        if (t < 0) continue;
-        const float x = k == k0 ? x0 : Elem<T>::get(logits + begin + t);
-        float sum = bias[k];
-        if (get_bit(again, t)) {
-            int found = k;
-            sum = 0.f;
-#pragma unroll 4
-            for (int e = 0; e < n_bias; e += 4) {
-                const int4 q = *reinterpret_cast<const int4*>(bias_ids + e);
-                const float4 b = *reinterpret_cast<const float4*>(bias + e);
-                const bool same[4] = {q.x == t, q.y == t, q.z == t, q.w == t};
-                sum += same[0] ? b.x : 0.f, sum += same[1] ? b.y : 0.f, sum += same[2] ? b.z : 0.f, sum += same[3] ? b.w : 0.f;
-                if (same[0] | same[1] | same[2] | same[3]) found = min(found, e + (same[0] ? 0 : same[1] ? 1 : same[2] ? 2 : 3));
-            }
-            if (found < k) continue;
+        const int t = biased(k + lane);
+        float x = x0, sum = 0.f;
+        if (t >= 0) {
+            if (k != k0) x = Elem<T>::get(logits + begin + t);
+            sum = bias[k + lane];
         }
+        bool stored = t < 0;   // or will be by another
+        unsigned int several = __ballot_sync(~0u, t >= 0 && get_bit(again, t));
+        if (__popc(several) > 6) {
+            if (several >> lane & 1) {
+                int found = k + lane;
+                sum = 0.f;
+#pragma unroll 4
+                for (int e = 0; e < n_bias; ++e)
+                    if (bias_ids[e] == t) sum += bias[e], found = min(found, e);
+                stored = found < k + lane;
+            }
+            several = 0;
+        }
+        for (; several; several &= several - 1) {
+            const int of = __ffs(several) - 1, token = __shfl_sync(~0u, t, of);
+            float all = 0.f;
+            bool first = true;
+            for (int e = lane; e - lane < n_bias && first; e += 32 * LOOKS) {
+                unsigned int entries[LOOKS];
+                float b[LOOKS];
+#pragma unroll
+                for (int u = 0; u < LOOKS; ++u) {
+                    const bool same = e + u * 32 < n_bias && bias_ids[e + u * 32] == token;
+                    b[u] = same ? bias[e + u * 32] : 0.f;
+                    entries[u] = __ballot_sync(~0u, same);
+                }
+#pragma unroll
+                for (int u = 0; u < LOOKS; ++u) {
+                    if (entries[u]) first = first && e - lane + u * 32 + __ffs(entries[u]) - 1 >= k + of;
+                    for (unsigned int left = entries[u]; left; left &= left - 1) all += __shfl_sync(~0u, b[u], __ffs(left) - 1);
+                }
+            }
+            if (lane == of) sum = all, stored = !first;
+        }
+        if (stored) continue;
         const float y = get_bit(seen, t) ? penalized(x, RANKED ? place(t) : t) : x;
         Elem<T>::put(out + begin + t, y + sum);
     }
@@ -363,7 +387,7 @@ cudaError_t constrain_plan(ConstrainParams p, int sms, cudaStream_t stream)
     const bool ranked = COUNTS && threads < 1024;
     p.counts = COUNTS ? ((ranked ? p.list : tokens) / (32 / COUNTS) + 4) / 4 * 4 : 0;
     p.over = BWD && p.logits == p.dst && p.logits != p.src;
-    const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * ((p.n_bias + 3) / 4 * 4)) +
+    const size_t smem = 4 * static_cast<size_t>((p.n_bias ? 4 : 3) * p.words + p.counts + 2 * p.n_bias) +
                         2 * static_cast<size_t>(p.list + (ranked ? p.words : 0));
     if constexpr (COUNTS == 32) {   // (histories of 65536 ids and more)
         return constrain<T, BWD, COUNTS, 1024, true>(p, parts, smem, stream);

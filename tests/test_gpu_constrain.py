@@ -276,6 +276,16 @@ def test_biases_that_name_a_token_again(biases):
     assert same_bits(a, run(x, g, c, "f32"))   # sums of a token's entries in their order
 
 
+@pytest.mark.parametrize("n", [2, 25])
+@pytest.mark.parametrize("V,biases", [(60001, 1000), (5003, 300), (700, 300), (97, 333)])
+def test_few_and_many_tokens_biased_again(V, biases, n):
+    rng = np.random.default_rng(V + n)
+    x, g = H.logits(rng, n, V, "f32"), H.rounded(rng.standard_normal((n, V)), "f32")
+    c = limits(rng, n, V, 60, biases=biases, masks=2)
+    c["bias_ids"][0, -1] = c["bias_ids"][0, 0]
+    run(x, g, c, "f32")
+
+
 def test_strided_histories_and_masks():
     rng = np.random.default_rng(11)
     n, V = 4, 2000
