@@ -337,8 +337,9 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     """What cola_constrain_logits_* imposes on n rows of logits (include/cola.h):
     history [n x width] int64 token ids, the first history_len [n] of a row used,
     its first prompt_len [n] the prompt; repetition, frequency, presence [n] fp32;
-    bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x ceil(vocab / 32)]
-    int32 words of bits, mask_of [n] int64 the mask of each row.  Keeps the tensors."""
+    bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x at least
+    ceil(vocab / 32)] int32 words of bits, mask_of [n] int64 the mask of each row.
+    Keeps the tensors."""
     kept = dict(history=_of("history", history, torch.int64, 2), history_len=_of("history_len", history_len, torch.int64, 1),
                 prompt_len=_of("prompt_len", prompt_len, torch.int64, 1), repetition=_of("repetition", repetition, torch.float32, 1),
                 frequency=_of("frequency", frequency, torch.float32, 1), presence=_of("presence", presence, torch.float32, 1),
@@ -358,14 +359,16 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     if masks is not None:
         c.n_masks, c.ld_masks = masks.shape[0], _pitch(masks)
     c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
-    c.tensors, c.rows = kept, rows.pop() if rows else None
+    c.tensors, c.rows, c.words = kept, rows.pop() if rows else None, masks.shape[1] if masks is not None else None
     return c
 
 
 def _limits(d, c):
-    rows = getattr(c, "rows", None)
+    rows, words, need = getattr(c, "rows", None), getattr(c, "words", None), -(-d.vocab // 32)
     if rows is not None and rows != d.n:
         raise ValueError(f"constraints of {rows} rows for {d.n} rows of logits")
+    if words is not None and words < need:
+        raise ValueError(f"masks of {words} words for a vocabulary of {d.vocab}, which takes {need}")
     return ctypes.byref(c)
 
 

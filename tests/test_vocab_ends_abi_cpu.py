@@ -167,3 +167,15 @@ def test_bindings_raise(L):   # noqa: F811
         L.cola_embed_fwd(L.embed_desc(0, 1, 8), FAKE, FAKE, FAKE, stream=0)
     with pytest.raises(L.ColaError, match="cola_constrain_logits_fwd"):
         L.cola_constrain_logits_fwd(L.vocab_desc(0, 1), L.constraints(), FAKE, FAKE, stream=0)
+
+
+# a call compares the masks' words with the vocabulary: of one mask, whose pitch says nothing, and of a view narrower than its pitch
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+@pytest.mark.parametrize("vocab,have,need", [(32000, 1, 1000), (32000, 999, 1000), (33, 1, 2), (97, 0, 4)])
+def test_masks_narrower_than_the_vocabulary(L, name, vocab, have, need):   # noqa: F811
+    call, args = getattr(L, name), [FAKE] * CONSTRAIN[name]
+    which = torch.zeros(2, dtype=torch.int64)
+    for masks, rows in ((torch.zeros((1, have), dtype=torch.int32), 1), (torch.zeros((2, 2000), dtype=torch.int32)[:, :have], 2),
+                        (torch.zeros((1, 2000), dtype=torch.int32)[:, :have], 1)):
+        with pytest.raises(ValueError, match=f"masks of {have} words for a vocabulary of {vocab}, which takes {need}"):
+            call(L.vocab_desc(rows, vocab), L.constraints(masks=masks, mask_of=which[:rows]), *args, stream=0)
