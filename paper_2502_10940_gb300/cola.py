@@ -339,7 +339,7 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     its first prompt_len [n] the prompt; repetition, frequency, presence [n] fp32;
     bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x at least
     ceil(vocab / 32)] int32 words of bits, mask_of [n] int64 the mask of each row.
-    Keeps the tensors."""
+    Keeps the tensors, which are on the GPU (or pinned) when they are used."""
     kept = dict(history=_of("history", history, torch.int64, 2), history_len=_of("history_len", history_len, torch.int64, 1),
                 prompt_len=_of("prompt_len", prompt_len, torch.int64, 1), repetition=_of("repetition", repetition, torch.float32, 1),
                 frequency=_of("frequency", frequency, torch.float32, 1), presence=_of("presence", presence, torch.float32, 1),
@@ -360,6 +360,7 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
         c.n_masks, c.ld_masks = masks.shape[0], _pitch(masks)
     c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
     c.tensors, c.rows, c.words = kept, rows.pop() if rows else None, masks.shape[1] if masks is not None else None
+    c.host = ", ".join(name for name, t in kept.items() if t is not None and not (t.is_cuda or t.is_pinned()))
     return c
 
 
@@ -369,6 +370,8 @@ def _limits(d, c):
         raise ValueError(f"constraints of {rows} rows for {d.n} rows of logits")
     if words is not None and words < need:
         raise ValueError(f"masks of {words} words for a vocabulary of {d.vocab}, which takes {need}")
+    if getattr(c, "host", None):
+        raise ValueError(f"{c.host}: on the host, in memory that is not pinned")
     return ctypes.byref(c)
 
 

@@ -179,3 +179,15 @@ def test_masks_narrower_than_the_vocabulary(L, name, vocab, have, need):   # noq
                         (torch.zeros((1, 2000), dtype=torch.int32)[:, :have], 1)):
         with pytest.raises(ValueError, match=f"masks of {have} words for a vocabulary of {vocab}, which takes {need}"):
             call(L.vocab_desc(rows, vocab), L.constraints(masks=masks, mask_of=which[:rows]), *args, stream=0)
+
+
+# one that is wide enough passes that check (what comes next is that the tensors are the host's)
+@pytest.mark.parametrize("vocab,have", [(32000, 1000), (33, 2), (32, 1), (32, 2)])
+def test_tensors_of_the_host(L, vocab, have):   # noqa: F811
+    d, args = L.vocab_desc(1, vocab), [FAKE, FAKE]
+    one = torch.ones(1)
+    for kw, name in ((dict(masks=torch.zeros((1, have), dtype=torch.int32)), "masks"),
+                     (dict(history=torch.zeros((1, 4), dtype=torch.int64), repetition=one), "history, repetition"),
+                     (dict(bias_ids=torch.zeros((1, 2), dtype=torch.int64), bias=torch.ones((1, 2))), "bias_ids, bias")):
+        with pytest.raises(ValueError, match=f"{name}: on the host"):
+            L.cola_constrain_logits_fwd(d, L.constraints(**kw), *args, stream=0)
