@@ -442,7 +442,8 @@ typedef struct {
 cola_status_t cola_embed_fwd(const cola_embed_desc_t* desc, const void* E, const int64_t* ids, void* X, void* stream);
 
 /* Bytes of workspace cola_embed_bwd needs on the current device (ws as for the
- * layer's calls; the same workspace may serve both, one call at a time). */
+ * layer's calls; the same workspace may serve both, one call at a time).  Of fewer
+ * tokens n they are no more: the longest batch's workspace serves the others. */
 cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* bytes);
 
 /* dE_v = scale sum of dX_t over the tokens t with ids_t = v, [vocab x d] (ld_de).

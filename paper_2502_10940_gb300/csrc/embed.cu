@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "vocab_rows.cuh"
@@ -1084,6 +1085,9 @@ cudaError_t join(const EmbedParams& p, int sms, cudaStream_t stream)
 
 }  // namespace
 
+// Sorted tokens of the longest chunk, eight at a time (a place behind it still has 32 bits).
+constexpr double CHUNK_MOST = 1e6;
+
 EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, size_t at)
 {
     EmbedLayout l = {};
@@ -1095,26 +1099,33 @@ EmbedLayout embed_layout(long long n, int vocab, int d, int dtype_x, int sms, si
     const Groups g = groups(d, dtype_x == 0 ? COLS<__nv_bfloat16> : COLS<float>);
     // twelve CTAs' worth of groups for every SM, of eight tokens at least (131072 x 4096 bf16:
     // 209 us, with eight 217, five 233, three 262)
-    const double per = static_cast<double>(n) * (g.tiles << g.shift) / (12.0 * sms * 256);
-    l.chunk = std::max(8, static_cast<int>(std::min(per / 8 + 1, 1e6)) * 8);
+    const double threads = 12.0 * sms * 256, per = static_cast<double>(n) * (g.tiles << g.shift) / threads;
+    l.chunk = std::max(8, static_cast<int>(std::min(per / 8 + 1, CHUNK_MOST)) * 8);
     l.chunks = static_cast<int>((n + l.chunk - 1) / l.chunk);
+    // Room for the chunks of n or of any fewer tokens, so that a batch's workspace serves shorter
+    // ones: lengths go in steps, and fewer tokens may have more chunks.  A length is 8 or more,
+    // and more than `per` unless it is the longest.
+    const long long most_chunks = std::min((n + 7) / 8, std::max(static_cast<long long>(std::ceil(threads / (g.tiles << g.shift))),
+                                                                 static_cast<long long>(n / (8 * CHUNK_MOST)) + 1));
     l.sorted = take(n * sizeof(uint2));
     l.counts = take(2 * sizeof(unsigned int));
-    l.long_sums = take(l.chunks * sizeof(uint4));
-    l.partials = take(sizeof(float) * 2 * l.chunks * static_cast<size_t>((d + 7) / 8 * 8));
+    l.long_sums = take(most_chunks * sizeof(uint4));
+    l.partials = take(sizeof(float) * 2 * most_chunks * static_cast<size_t>((d + 7) / 8 * 8));
     l.present = take((vocab + 31) / 32 * sizeof(unsigned int));
     if (n > EMBED_FEW) {
         int bits = 1;
         while ((1 << bits) < vocab) ++bits;
         l.low = bits > 10 ? (bits + 1) / 2 : bits, l.high = bits - l.low;
         // up to 64 CTAs of few rounds, then up to 256 of many
-        const long long rounds = std::max((n + 64 * SORT_THREADS - 1) / (64 * SORT_THREADS), 1ll);
-        const long long most = (n + 256 * SORT_THREADS - 1) / (256 * SORT_THREADS);
+        const auto ctas = [&](long long tokens) { return (n + tokens - 1) / tokens; };   // of so many each
+        const long long rounds = std::max(ctas(64 * SORT_THREADS), 1ll), most = ctas(256 * SORT_THREADS);
         l.sort_each = static_cast<unsigned int>(std::max(std::min<long long>(rounds, ROUNDS), most) * 32);
-        l.sort_ctas = static_cast<int>((n + l.sort_each * SORT_WARPS - 1) / (l.sort_each * SORT_WARPS));
+        l.sort_ctas = static_cast<int>(ctas(l.sort_each * SORT_WARPS));
+        // (room as above: fewer tokens have up to 64 CTAs, or up to 256 of ROUNDS)
+        const size_t most_ctas = std::min(ctas(SORT_THREADS), std::max(64ll, std::min(256ll, ctas(ROUNDS * SORT_THREADS))));
         l.between = take(n * sizeof(uint2));
-        l.hist[0] = take(sizeof(unsigned int) * l.sort_ctas << l.low);
-        l.hist[1] = take(sizeof(unsigned int) * l.sort_ctas << l.high);
+        l.hist[0] = take(sizeof(unsigned int) * most_ctas << l.low);
+        l.hist[1] = take(sizeof(unsigned int) * most_ctas << l.high);
     }
     l.total = at;
     return l;

@@ -332,3 +332,30 @@ def test_short_workspace():
     ws = cola.embed_workspace(m)
     with pytest.raises(cola.ColaError, match="WORKSPACE"):
         cola.cola_embed_bwd(m, I, X, X, ws[:-256])
+
+
+@pytest.mark.parametrize("t_x", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab,d", [(32000, 4096), (32000, 512), (50021, 1000), (300, 64), (1 << 20, 8), (5, 1 << 20)])
+def test_workspace_sizes_grow_with_the_tokens(vocab, d, t_x):
+    """Up to 20000 tokens, on both sides of later steps of the chunks and of the
+    sort's CTAs, and at the limit."""
+    some = set(range(1, 20000)) | {int(1.013 ** k) for k in range(1, 1490)} | {65536 * k + j for k in range(1, 70) for j in (-1, 0, 1)}
+    last = 0
+    for n in sorted(some | {(1 << 28) - 1}):
+        if n >= 1 << 28 or n * (d // 8) > 1 << 38:
+            break
+        size = cola.cola_embed_workspace_size(cola.embed_desc(n, vocab, d, dtype_x=t_x))
+        assert size >= last, n
+        last = size
+
+
+@pytest.mark.parametrize("n,most,vocab,d", [(7000, 8192, 3000, 4096), (7295, 7296, 500, 4096), (2500, 30000, 9000, 1024), (8192, 8193, 2000, 72),
+                                            (65536, 65537, 3000, 8), (260000, 270000, 70000, 16), (9, 5000, 40, 2056)])
+def test_few_tokens_in_the_workspace_of_more(n, most, vocab, d):
+    ids = torch.as_tensor(tokens(np.random.default_rng(n), n, vocab, "zipf"), dtype=torch.int64, device="cuda")
+    dX = torch.randn((n, d), device="cuda").to(torch.bfloat16)
+    m = cola.embed_desc(n, vocab, d)
+    own, other = (torch.full((vocab, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cola.cola_embed_bwd(m, ids, dX, own, cola.embed_workspace(m))
+    cola.cola_embed_bwd(m, ids, dX, other, cola.embed_workspace(cola.embed_desc(most, vocab, d)))
+    assert not bool(torch.isnan(own).any()) and torch.equal(own, other)
