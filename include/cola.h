@@ -379,7 +379,8 @@ cola_status_t cola_topk_distill_step(const cola_vocab_desc_t* desc, const void* 
  * pitch ld of the logits and ld_grad of out, dout and dlogits, and their type;
  * its temperatures, k and rest are checked but not used.  Integers are int64. */
 typedef struct {
-    const int64_t* history;      /* [n x history_width] (ld_history) token ids, prompt first; NULL: none */
+    const int64_t* history;      /* [n x history_width] (ld_history) token ids, prompt first; NULL: none, with
+                                    history_width 0 or without lengths and penalties */
     const int64_t* history_len;  /* [n] ids of each row (held to 0 .. history_width); NULL: all */
     const int64_t* prompt_len;   /* [n] of those, how many are the prompt; NULL: 0 */
     const float* repetition;     /* [n]; NULL: 1 */
@@ -391,7 +392,7 @@ typedef struct {
                                     allows token j; NULL: none */
     const int64_t* mask_of;      /* [n] the mask of each row, none where outside [0, n_masks);
                                     NULL: row i has mask i */
-    int64_t history_width;       /* ids a row of the history has room for, < 2^28 */
+    int64_t history_width;       /* ids a row of the history has room for, < 2^28; 0: history is NULL */
     int64_t ld_history;          /* row pitch of the history (0: history_width) */
     int64_t n_masks;
     int64_t ld_masks;            /* row pitch of the masks in words (0: ceil(vocab / 32)) */

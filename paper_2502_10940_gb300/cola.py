@@ -335,11 +335,11 @@ def _pitch(t):
 def constraints(history=None, history_len=None, prompt_len=None, *, repetition=None, frequency=None, presence=None, bias_ids=None,
                 bias=None, masks=None, mask_of=None):
     """What cola_constrain_logits_* imposes on n rows of logits (include/cola.h):
-    history [n x width] int64 token ids, the first history_len [n] of a row used,
-    its first prompt_len [n] the prompt; repetition, frequency, presence [n] fp32;
-    bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x at least
-    ceil(vocab / 32)] int32 words of bits, mask_of [n] int64 the mask of each row.
-    Keeps the tensors, which are on the GPU (or pinned) when they are used."""
+    history [n x width] int64 token ids (width 0: none yet), the first history_len
+    [n] of a row used, its first prompt_len [n] the prompt; repetition, frequency,
+    presence [n] fp32; bias_ids [n x b] int64 with bias [n x b] fp32; masks [m x at
+    least ceil(vocab / 32)] int32 words of bits, mask_of [n] int64 the mask of each
+    row.  Keeps the tensors; a call refuses those in host memory that is not pinned."""
     kept = dict(history=_of("history", history, torch.int64, 2), history_len=_of("history_len", history_len, torch.int64, 1),
                 prompt_len=_of("prompt_len", prompt_len, torch.int64, 1), repetition=_of("repetition", repetition, torch.float32, 1),
                 frequency=_of("frequency", frequency, torch.float32, 1), presence=_of("presence", presence, torch.float32, 1),
@@ -348,6 +348,8 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     if (bias_ids is None) != (bias is None) or (bias is not None and not (bias_ids.is_contiguous() and bias.is_contiguous()
                                                                            and bias.shape == bias_ids.shape)):
         raise ValueError("bias_ids and bias: both or neither, contiguous, of one shape")
+    if history is None and any(t is not None for t in (history_len, prompt_len, repetition, frequency, presence)):
+        raise ValueError("lengths or penalties without a history (of no ids: [n x 0])")
     rows = {t.shape[0] for name, t in kept.items() if t is not None and name != "masks"}
     if len(rows) > 1:
         raise ValueError(f"tensors of {sorted(rows)} rows")
@@ -360,7 +362,7 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
         c.n_masks, c.ld_masks = masks.shape[0], _pitch(masks)
     c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
     c.tensors, c.rows, c.words = kept, rows.pop() if rows else None, masks.shape[1] if masks is not None else None
-    c.host = ", ".join(name for name, t in kept.items() if t is not None and not (t.is_cuda or t.is_pinned()))
+    c.host = ", ".join(name for name, t in kept.items() if t is not None and t.numel() and not (t.is_cuda or t.is_pinned()))
     return c
 
 

@@ -1770,8 +1770,9 @@ cola_status_t constrain_params(const cola_vocab_desc_t* d, const cola_constraint
         return COLA_ERR_INVALID;
     const int64_t ld_history = c->ld_history ? c->ld_history : c->history_width;
     const int64_t ld_masks = c->ld_masks ? c->ld_masks : (d->vocab + 31) / 32;
+    // (rows without room for an id: no pointer, and the lengths and penalties are of no token)
     if (c->history ? c->history_width < 1 || ld_history < c->history_width
-                   : c->history_len || c->prompt_len || c->repetition || c->frequency || c->presence)
+                   : c->history_width && (c->history_len || c->prompt_len || c->repetition || c->frequency || c->presence))
         return COLA_ERR_INVALID;
     if ((c->bias_ids != nullptr) != (c->bias != nullptr) || (c->bias != nullptr) != (c->n_bias > 0)) return COLA_ERR_INVALID;
     if (c->masks ? c->n_masks < (c->mask_of ? 1 : d->n) || ld_masks < (d->vocab + 31) / 32 : c->mask_of != nullptr)
@@ -1845,7 +1846,7 @@ cola_status_t cola_constrain_logits_bwd(const cola_vocab_desc_t* desc, const col
     ConstrainParams p;
     COLA_TRY(constrain_params(desc, constraints, logits, dout, dlogits, &p));
     if (!constraints->repetition) p.history = nullptr;   // nothing else scales a gradient
-    if (p.history && !logits) return COLA_ERR_INVALID;
+    else if (!logits) return COLA_ERR_INVALID;
     if (logits == dlogits && p.ld != p.ld_dst) return COLA_ERR_INVALID;
     p.n_bias = 0;
     return run_constrain(desc, p, true, stream);

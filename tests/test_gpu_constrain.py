@@ -364,3 +364,20 @@ def test_traced_launches():
         cola.cola_constrain_logits_fwd(cola.vocab_desc(2, 100, dtype="f32"), C, X, X)
         cola.cola_constrain_logits_bwd(cola.vocab_desc(2, 100, dtype="f32"), C, X, X, torch.empty_like(X))
     assert [r[0] for r in t.records()] == ["constrain", "constrain"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(1, 1), (3, 5003), (90, 1001)])
+def test_histories_of_no_ids(n, V, dtype):
+    """The first token of a sequence without a prompt: penalties of no token."""
+    rng = np.random.default_rng(n)
+    x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
+    c = limits(rng, n, V, 0, biases=3, masks=2)
+    run(x, g, c, dtype)
+    run(x, g, {k: v for k, v in c.items() if k in ("history", "repetition", "presence")}, dtype, "odd")
+    room = torch.zeros((n, 7), dtype=torch.int64, device="cuda")
+    C = cola.constraints(room[:, :0], repetition=torch.full((n,), 2.0, device="cuda"))
+    X = H.place(x, dtype)
+    out = torch.empty_like(X)
+    cola.cola_constrain_logits_fwd(cola.vocab_desc(n, V, dtype=dtype), C, X, out)
+    assert same_bits(X, out)

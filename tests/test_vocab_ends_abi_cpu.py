@@ -191,3 +191,25 @@ def test_tensors_of_the_host(L, vocab, have):   # noqa: F811
                      (dict(bias_ids=torch.zeros((1, 2), dtype=torch.int64), bias=torch.ones((1, 2))), "bias_ids, bias")):
         with pytest.raises(ValueError, match=f"{name}: on the host"):
             L.cola_constrain_logits_fwd(d, L.constraints(**kw), *args, stream=0)
+
+
+# rows without ids (an empty tensor's pointer is NULL) have no named token; a width without ids stays refused
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+@pytest.mark.parametrize("ld", [0, 5])
+def test_histories_of_no_ids(L, name, ld):   # noqa: F811
+    d, args = L.vocab_desc(4, 100), [FAKE] * CONSTRAIN[name]
+    of = lambda width: _limits(L, history=None, history_width=width, ld_history=ld, bias=FAKE + 2)   # noqa: E731
+    assert _constrain(L, name, d, of(0), args) == 2      # what comes next is that the biases are misaligned
+    assert _constrain(L, name, d, of(1), args) == 1
+    ids, r = torch.zeros((2, 5), dtype=torch.int64), torch.ones(2)
+    for none in (ids[:, :0], torch.zeros((2, 0), dtype=torch.int64)):
+        c = L.constraints(none, torch.zeros(2, dtype=torch.int64), repetition=r)
+        assert (c.history, c.history_width, c.repetition) == (None, 0, r.data_ptr())
+    for kw in (dict(repetition=r), dict(history_len=ids[:, 0].clone()), dict(presence=r), dict(frequency=r)):
+        with pytest.raises(ValueError, match="without a history"):
+            L.constraints(**kw)
+
+
+def test_gradient_of_no_ids_still_takes_the_logits(L):   # noqa: F811
+    d, args = L.vocab_desc(4, 100), [None, FAKE, FAKE]
+    assert _constrain(L, "cola_constrain_logits_bwd", d, _limits(L, history=None, history_width=0), args) == 1
