@@ -389,7 +389,7 @@ typedef struct {
     const int64_t* bias_ids;     /* [n x n_bias]; NULL: none */
     const float* bias;           /* [n x n_bias] */
     const uint32_t* masks;       /* [n_masks x ceil(vocab / 32)] (ld_masks): bit j % 32 of word j / 32
-                                    allows token j; NULL: none */
+                                    allows token j; NULL: none, with n_masks 0 or without mask_of */
     const int64_t* mask_of;      /* [n] the mask of each row, none where outside [0, n_masks);
                                     NULL: row i has mask i */
     int64_t history_width;       /* ids a row of the history has room for, < 2^28; 0: history is NULL */

@@ -321,9 +321,9 @@ def cola_topk_distill_step(d, logits, t_ids, t_vals, t_lse, dloss, loss, dlogits
 def _of(name, t, dtype, dim):
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if t.dtype != dtype or t.dim() != dim or (t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name}: {dim} dimension(s) of {dtype} with unit stride along the last, got {t.dtype} of strides {t.stride()}")
-    if dim == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if dim == 2 and t.numel() and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
         raise ValueError(f"{name}: rows that overlap, strides {t.stride()}")
     return t
 
@@ -350,6 +350,8 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
         raise ValueError("bias_ids and bias: both or neither, contiguous, of one shape")
     if history is None and any(t is not None for t in (history_len, prompt_len, repetition, frequency, presence)):
         raise ValueError("lengths or penalties without a history (of no ids: [n x 0])")
+    if masks is None and mask_of is not None:
+        raise ValueError("mask_of without masks (none of them: [0 x ...])")
     rows = {t.shape[0] for name, t in kept.items() if t is not None and name != "masks"}
     if len(rows) > 1:
         raise ValueError(f"tensors of {sorted(rows)} rows")
@@ -361,7 +363,7 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
     if masks is not None:
         c.n_masks, c.ld_masks = masks.shape[0], _pitch(masks)
     c.n_bias = bias_ids.shape[1] if bias_ids is not None else 0
-    c.tensors, c.rows, c.words = kept, rows.pop() if rows else None, masks.shape[1] if masks is not None else None
+    c.tensors, c.rows, c.words = kept, rows.pop() if rows else None, masks.shape[1] if c.n_masks else None
     c.host = ", ".join(name for name, t in kept.items() if t is not None and t.numel() and not (t.is_cuda or t.is_pinned()))
     return c
 

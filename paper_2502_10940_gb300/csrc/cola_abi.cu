@@ -1770,12 +1770,13 @@ cola_status_t constrain_params(const cola_vocab_desc_t* d, const cola_constraint
         return COLA_ERR_INVALID;
     const int64_t ld_history = c->ld_history ? c->ld_history : c->history_width;
     const int64_t ld_masks = c->ld_masks ? c->ld_masks : (d->vocab + 31) / 32;
-    // (rows without room for an id: no pointer, and the lengths and penalties are of no token)
+    // (rows without room for an id, or no masks: no pointer; lengths and penalties are of no
+    // token, mask_of names no mask)
     if (c->history ? c->history_width < 1 || ld_history < c->history_width
                    : c->history_width && (c->history_len || c->prompt_len || c->repetition || c->frequency || c->presence))
         return COLA_ERR_INVALID;
     if ((c->bias_ids != nullptr) != (c->bias != nullptr) || (c->bias != nullptr) != (c->n_bias > 0)) return COLA_ERR_INVALID;
-    if (c->masks ? c->n_masks < (c->mask_of ? 1 : d->n) || ld_masks < (d->vocab + 31) / 32 : c->mask_of != nullptr)
+    if (c->masks ? c->n_masks < (c->mask_of ? 1 : d->n) || ld_masks < (d->vocab + 31) / 32 : c->n_masks && c->mask_of)
         return COLA_ERR_INVALID;
     const int64_t lim = (int64_t(1) << 31) - 256;
     if (c->history_width > HISTORY_MAX || ld_history > lim || ld_masks > lim || c->n_masks > lim || c->n_bias > BIAS_MAX)

@@ -381,3 +381,13 @@ def test_histories_of_no_ids(n, V, dtype):
     out = torch.empty_like(X)
     cola.cola_constrain_logits_fwd(cola.vocab_desc(n, V, dtype=dtype), C, X, out)
     assert same_bits(X, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V", [(1, 33), (90, 1001)])
+def test_no_masks(n, V, dtype):
+    """A batch none of whose rows has a grammar."""
+    rng = np.random.default_rng(n + 1)
+    x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
+    c = limits(rng, n, V, 40, biases=3)
+    run(x, g, dict(c, masks=np.zeros((0, (V + 31) // 32), np.int32), mask_of=rng.integers(-1, 2, n)), dtype)

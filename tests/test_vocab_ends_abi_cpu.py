@@ -213,3 +213,21 @@ def test_histories_of_no_ids(L, name, ld):   # noqa: F811
 def test_gradient_of_no_ids_still_takes_the_logits(L):   # noqa: F811
     d, args = L.vocab_desc(4, 100), [None, FAKE, FAKE]
     assert _constrain(L, "cola_constrain_logits_bwd", d, _limits(L, history=None, history_width=0), args) == 1
+
+
+# no masks (an empty tensor's pointer is NULL): mask_of names none for any row
+@pytest.mark.parametrize("name", sorted(CONSTRAIN))
+def test_no_masks(L, name):   # noqa: F811
+    d, args = L.vocab_desc(4, 100), [FAKE] * CONSTRAIN[name]
+    of = lambda **kw: _limits(L, masks=None, mask_of=FAKE + 4, **kw)   # noqa: E731
+    assert _constrain(L, name, d, of(n_masks=0), args) == 2      # what comes next is that mask_of is misaligned
+    assert _constrain(L, name, d, of(n_masks=1), args) == 1
+    which = torch.zeros(2, dtype=torch.int64)
+    for none in (torch.zeros((0, 4), dtype=torch.int32), torch.empty_strided((0, 4), (0, 0), dtype=torch.int32)):
+        c = L.constraints(masks=none, mask_of=which)
+        assert (c.masks, c.n_masks, c.mask_of, c.rows) == (None, 0, which.data_ptr(), 2)
+    with pytest.raises(ValueError, match="without masks"):
+        L.constraints(mask_of=which)
+    with pytest.raises(ValueError, match="on the host"):         # no masks are not too narrow
+        L.cola_constrain_logits_fwd(L.vocab_desc(2, 100), L.constraints(masks=torch.zeros((0, 0), dtype=torch.int32), mask_of=which), FAKE,
+                                    FAKE, stream=0)
