@@ -359,3 +359,13 @@ def test_few_tokens_in_the_workspace_of_more(n, most, vocab, d):
     cola.cola_embed_bwd(m, ids, dX, own, cola.embed_workspace(m))
     cola.cola_embed_bwd(m, ids, dX, other, cola.embed_workspace(cola.embed_desc(most, vocab, d)))
     assert not bool(torch.isnan(own).any()) and torch.equal(own, other)
+
+
+@pytest.mark.parametrize("t_x", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,d,kind", [(20000, 9000, 136, "zipf"), (40000, 300, 40, "same"), (9000, 50021, 33, "uniform"),
+                                            (30000, 700, 1003, "zipf"), (8193, 70, 64, "none"), (70000, 1 << 20, 8, "rising"),
+                                            (2200001, 1000, 8, "zipf"), (2100001, 50021, 7, "zipf")])
+def test_accumulated_of_many(n, vocab, d, kind, t_x):
+    """Digit by digit sorted: one pass and two, rounds that come again, sums that
+    cross many chunks; rows of no token stay as they were."""
+    backward(tokens(np.random.default_rng(n), n, vocab, kind), vocab, d, t_x, "f32", scale=1.5, pad=True, accumulate=True)
