@@ -91,6 +91,8 @@ struct Elem<float> {
     static constexpr uint32_t FILL = 0xff800000u;   // -inf
     __device__ static float get(const float* p) { return *p; }
     __device__ static void put(float* p, float x) { *p = x; }
+    // number `e` of a vector, in its word (a NaN keeps its bits)
+    __device__ __forceinline__ static void put_bits(float* p, uint32_t word, int) { *p = __uint_as_float(word); }
     __device__ __forceinline__ static void unpack(const uint4& u, float (&x)[4])
     {
         x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
@@ -157,6 +159,10 @@ struct Elem<__nv_bfloat16> {
     static constexpr uint32_t FILL = 0xff80ff80u;
     __device__ static float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     __device__ static void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+    __device__ __forceinline__ static void put_bits(__nv_bfloat16* p, uint32_t word, int e)
+    {
+        *p = __ushort_as_bfloat16(static_cast<unsigned short>(word >> e % 2 * 16));
+    }
     __device__ __forceinline__ static void unpack(const uint4& u, float (&x)[8])
     {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -286,11 +292,9 @@ __device__ __forceinline__ void store_apart(T* dst, const uint4& p, bool mine)
                           __funnelshift_r(b[3], b[4], bits)));
     if (mine && (lane == 0 || !next)) {
         const int first = static_cast<int>(cut / sizeof(T));
-        float x[E];
-        Elem<T>::unpack(p, x);
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e < first ? lane == 0 : !next) Elem<T>::put(dst + e, x[e]);
+            if (e < first ? lane == 0 : !next) Elem<T>::put_bits(dst + e, c[e * sizeof(T) / 4], e);
     }
 }
 

@@ -391,3 +391,23 @@ def test_no_masks(n, V, dtype):
     x, g = H.logits(rng, n, V, dtype), H.rounded(rng.standard_normal((n, V)), dtype)
     c = limits(rng, n, V, 40, biases=3)
     run(x, g, dict(c, masks=np.zeros((0, (V + 31) // 32), np.int32), mask_of=rng.integers(-1, 2, n)), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift", [0, 1, 2, 5])
+@pytest.mark.parametrize("n,V", [(1, 7), (3, 1001), (2, 40003), (400, 517)])
+def test_other_logits_keep_their_bits(n, V, shift, dtype):
+    """Every bit pattern, the NaNs' signs and payloads among them, wherever a row begins."""
+    rng = np.random.default_rng(V)
+    ints, width = (torch.int16, 16) if dtype == "bf16" else (torch.int32, 32)
+    bits = rng.integers(0, 1 << width, (n, V))
+    nan = 0x7f81 + rng.integers(0, 127, (n, V)) | rng.integers(0, 2, (n, V)) << 15
+    bits = np.where(rng.random((n, V)) < 0.3, nan << width - 16, bits)
+    bits = torch.as_tensor(np.where(bits >= 1 << width - 1, bits - (1 << width), bits), device="cuda").to(ints)
+    X = bits.view(H.TORCH[dtype])
+    history = torch.as_tensor(rng.integers(0, V, (n, 3)), device="cuda")
+    named = torch.zeros((n, V), dtype=torch.bool, device="cuda").scatter_(1, history, True)
+    C = cola.constraints(history, repetition=torch.full((n,), 2.0, device="cuda"))
+    out, _ = H.like(X, shift=shift)
+    cola.cola_constrain_logits_fwd(cola.vocab_desc(n, V, dtype=dtype), C, X, out)
+    assert torch.equal(out.contiguous().view(ints)[~named], bits[~named])
