@@ -351,13 +351,16 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
 // limit what one holds.
 //   - Many rows: CTAs of 256 threads, as many as run at once, four an SM (with counts, bf16,
 //     histories of 4096: 64 x 128000 13.9 us, twice as many 19.6, 256 x 50021 fp32 26.4 and
-//     29.4).  Without counts, where rows leave no more than one each, two times as many: the
+//     29.4), of 32768 tokens at most: 256 x 128000 takes four a row, which is 1.7 waves, 36.4
+//     us; two a row of 64000 tokens 39.3 (512 rows 71 and 68).  Without counts, where rows leave no more than one each, two times as many: the
 //     gradient of 509 x 50021 fp32 51 us against 53; of 256 x 128000 bf16 30 against 34.
 //   - Many rows of longer histories, with counts up to 16384: 512 threads, two an SM, of up
 //     to 65024 tokens (histories of 8192: 256 x 128000 bf16 41 us against 55 on 1024 threads,
 //     its gradient 38 against 54; 64 rows 15.4 against 15.9, 32 rows 13.4 against 10.6; 16384:
 //     256 rows 58 against 65; 32768: 51 against 49 for 128 rows, but gradients of 512 x 32000
-//     59 against 63).
+//     59 against 63).  256 and 512 threads are even at 2000 to 2600 ids (fp32, gradients
+//     of 1024 rows and more), at 5000 to 6000 (64, 1024 and 4096 rows of bf16).  At 4096, us: 64 x
+//     128000 13.2 and 14.1, 1024 x 32000 47 and 47, but their gradients 12.1 and 12.4, 50 and 39.
 //   - Few rows, and other histories beyond 4096 ids: 1024 threads, an SM each, and a vector
 //     for every sixteenth id at least (1 x 128000: 4.8 us against 6.0 on 256 threads).  Of
 //     long histories the list is made after the loop: 15 us against 22 for 32 x 50021 and 32768

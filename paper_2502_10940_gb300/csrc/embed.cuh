@@ -4,9 +4,12 @@
 // Mathematics (table E [vocab x d], scale s, tokens t < n):
 //   X_t = s E[id_t]   (0 where id_t names no token)
 //   dE_v = s sum_{t: id_t = v} dX_t
-// The sum's rows are found by sorting (id, t) by id, stably, so that every
-// token's rows are added in the order of the tokens: no atomics on values,
-// and the same bits from every call.
+// The sum's rows are found by sorting (id, t) by id, stably.  A token's rows are added
+// in fp32 in the order of the tokens, or, where a sum crosses bounds between warps or
+// chunks, in parts, which are added then.  The parts depend on the ids, n, vocab, d, the
+// type of dX and the device alone, no two of them meet in an atomic: the same bits from
+// every call.  A finished sum is scaled, rounded to fp32 and then to dE's type, or
+// added to dE (most columns by a reduction in memory, nobody else's there).
 #pragma once
 #include <cuda_runtime.h>
 
