@@ -451,8 +451,8 @@ cola_status_t cola_embed_workspace_size(const cola_embed_desc_t* desc, size_t* b
 /* dE_v = scale sum of dX_t over the tokens t with ids_t = v, [vocab x d] (ld_de).
  * The tokens are sorted by id, and each row's sum is taken in fp32 in an order
  * that depends on the ids, n, vocab, d, the type of dX and the device alone: two
- * calls give the same bits.  The scaled sum is fp32 before it is rounded to dE's type
- * or added to dE.  A tied table accumulates this onto the output embedding's
+ * calls give the same bits.  It is scaled in fp32, then rounded to dE's type or added
+ * to dE.  A tied table accumulates this onto the output embedding's
  * gradient.  Columns of dE between d and its pitch are left alone. */
 cola_status_t cola_embed_bwd(const cola_embed_desc_t* desc, const int64_t* ids, const void* dX, void* dE, void* ws,
                              size_t ws_bytes, void* stream);

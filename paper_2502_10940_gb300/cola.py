@@ -369,11 +369,11 @@ def constraints(history=None, history_len=None, prompt_len=None, *, repetition=N
 
 
 def _limits(d, c):
-    rows, words, need = getattr(c, "rows", None), getattr(c, "words", None), -(-d.vocab // 32)
+    rows, words = getattr(c, "rows", None), getattr(c, "words", None)
     if rows is not None and rows != d.n:
         raise ValueError(f"constraints of {rows} rows for {d.n} rows of logits")
-    if words is not None and words < need:
-        raise ValueError(f"masks of {words} words for a vocabulary of {d.vocab}, which takes {need}")
+    if words is not None and words * 32 < d.vocab:
+        raise ValueError(f"masks of {words} words for a vocabulary of {d.vocab}, which takes {-(-d.vocab // 32)}")
     if getattr(c, "host", None):
         raise ValueError(f"{c.host}: on the host, in memory that is not pinned")
     return ctypes.byref(c)

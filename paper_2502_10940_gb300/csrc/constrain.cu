@@ -352,8 +352,9 @@ cudaError_t constrain(const ConstrainParams& p, int parts, size_t smem, cudaStre
 //   - Many rows: CTAs of 256 threads, as many as run at once, four an SM (with counts, bf16,
 //     histories of 4096: 64 x 128000 13.9 us, twice as many 19.6, 256 x 50021 fp32 26.4 and
 //     29.4), of 32768 tokens at most: 256 x 128000 takes four a row, which is 1.7 waves, 36.4
-//     us; two a row of 64000 tokens 39.3 (512 rows 71 and 68).  Without counts, where rows leave no more than one each, two times as many: the
-//     gradient of 509 x 50021 fp32 51 us against 53; of 256 x 128000 bf16 30 against 34.
+//     us; two a row of 64000 tokens 39.3 (512 rows 71 and 68).  Without counts, where rows
+//     leave no more than one each, two times as many: the gradient of 509 x 50021 fp32 51 us
+//     against 53; of 256 x 128000 bf16 30 against 34.
 //   - Many rows of longer histories, with counts up to 16384: 512 threads, two an SM, of up
 //     to 65024 tokens (histories of 8192: 256 x 128000 bf16 41 us against 55 on 1024 threads,
 //     its gradient 38 against 54; 64 rows 15.4 against 15.9, 32 rows 13.4 against 10.6; 16384:

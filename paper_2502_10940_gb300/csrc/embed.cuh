@@ -8,8 +8,8 @@
 // in fp32 in the order of the tokens, or, where a sum crosses bounds between warps or
 // chunks, in parts, which are added then.  The parts depend on the ids, n, vocab, d, the
 // type of dX and the device alone, no two of them meet in an atomic: the same bits from
-// every call.  A finished sum is scaled, rounded to fp32 and then to dE's type, or
-// added to dE (most columns by a reduction in memory, nobody else's there).
+// every call.  A finished sum is scaled in fp32, then rounded to dE's type or added to dE
+// (most columns by a reduction in memory, where no other sum goes).
 #pragma once
 #include <cuda_runtime.h>
 
